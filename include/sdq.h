@@ -370,6 +370,100 @@ size_t sdq_noalloc_scratch_bytes(void);
  * this size can have run), CUDA. */
 int sdq_noalloc_status(sdq_plan plan, int32_t M, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Around the linears of a decoder layer: a paged cache of keys and values,
+ * attention over it, and the choice of a token.  No counterpart in the paper
+ * (its layers run inside an ordinary decoder); they take what the q/k/v plan
+ * writes (fp32 rows) and hand the o plan what it reads (bf16 rows).
+ *
+ * The cache.  Keys and values of one layer live in two device arrays of the
+ * caller's, [n_pages][kv_heads][page_tokens][head_dim] bf16 each, that is, a
+ * page holds page_tokens consecutive tokens of every key head.  Which pages a
+ * sequence owns is the caller's table; a page may belong to several sequences
+ * as long as only one appends to it.  head_dim 64 or 128; page_tokens 16, 32,
+ * 64 or 128; n_pages * kv_heads * page_tokens < 2^31.  Both arrays 128-byte
+ * aligned.  A handle is immutable, holds no device memory of its own (the
+ * arrays must outlive it) and may be used from several threads and streams. */
+typedef enum { SDQ_F32 = 0, SDQ_BF16 = 1 } sdq_dtype;
+
+typedef struct {
+  int32_t kv_heads;    /* 1 .. 1024 */
+  int32_t head_dim;    /* 64 or 128 */
+  int32_t page_tokens; /* 16, 32, 64 or 128 */
+  int32_t n_pages;
+} sdq_cache_desc;
+
+typedef struct sdq_cache_s* sdq_cache;
+
+/* Bytes of each of the two arrays; 0 for an invalid descriptor.  Host only. */
+size_t sdq_cache_bytes(const sdq_cache_desc* desc);
+/* Errors: INVALID_ARG, UNSUPPORTED (current device is not compute capability
+ * 10.3, or no tensor-map encoder in the driver), ALLOC, CUDA. */
+int sdq_cache_create(const sdq_cache_desc* desc, uint16_t* k_pages, uint16_t* v_pages, sdq_cache* out);
+int sdq_cache_destroy(sdq_cache cache);
+
+/* One step's batch: sequence s brings the tokens [token_start[s],
+ * token_start[s + 1]) of the step's n_tokens rows (none, one, or a prompt's
+ * worth) and has own_len[s] tokens of its own in the cache once they are
+ * appended (own_len counts the new ones), on pages pages[s * page_stride +
+ * i].  All sequences also share prefix_len tokens on prefix_pages, ahead of
+ * their own (0: none); the prefix may end inside a page, a sequence's own
+ * tokens begin on a page of their own.  So new token i of n_s stands at place
+ * a = own_len[s] - n_s + i among its sequence's own tokens, sees the prefix
+ * and own places 0 .. a, and has position max(0, prefix_len + a).  An empty
+ * slot of a serving batch is a token with own_len 0: it keeps nothing and
+ * sees the prefix alone (without one its output is 0).
+ * The four arrays are device memory and are read when the kernels run, so a
+ * captured graph follows their contents; the integers are fixed at the call:
+ * max_new and max_own are upper bounds of the new and own tokens of any
+ * sequence (what lies beyond them is ignored), max_own <= page_stride *
+ * page_tokens.  token_start must not decrease, from 0 to n_tokens.  A page
+ * index outside the cache is not followed: nothing is written there, and it
+ * reads as zeros. */
+typedef struct {
+  int32_t n_seqs;      /* 1 .. 65535 */
+  int32_t n_tokens;    /* 1 .. 2^20 */
+  int32_t max_new;     /* 1 .. n_tokens */
+  int32_t max_own;     /* 0 .. 2^30 - 1 */
+  int32_t page_stride;
+  int32_t prefix_len;  /* 0 .. 2^30 - 1 */
+  const int32_t* token_start;  /* n_seqs + 1 */
+  const int32_t* own_len;      /* n_seqs */
+  const int32_t* pages;        /* n_seqs x page_stride */
+  const int32_t* prefix_pages; /* ceil(prefix_len / page_tokens); unused without a prefix */
+} sdq_batch;
+
+/* Position rotation: elements (j, j + dim / 2) of a head, or (2 j, 2 j + 1)
+ * where interleaved, j < dim / 2, are turned by the angle whose cosine and
+ * sine stand at [position][j] of the tables (device, fp32, n_pos x dim / 2):
+ * (x1, x2) -> (x1 cos - x2 sin, x2 cos + x1 sin).  Elements from dim on stay.
+ * dim: a multiple of 8 up to head_dim, 0 for none; n_pos >= prefix_len +
+ * max_own (and 1). */
+typedef struct {
+  const float* cos;
+  const float* sin;
+  int32_t n_pos;
+  int32_t dim;
+  int32_t interleaved;
+} sdq_rope;
+
+/* Host-only: the usual tables, cos and sin of p * base^(-2 j / dim), formed in
+ * fp64, into host arrays of n_pos x dim / 2. */
+int sdq_rope_table(int32_t n_pos, int32_t dim, double base, float* cos_host, float* sin_host);
+
+/* Append a batch's new keys and values to the cache, rotated, and write its
+ * rotated queries in bf16 (q_out: n_tokens x q_heads x head_dim).  q, k and v
+ * hold one row per token (q_heads or kv_heads x head_dim, `type` fp32 or bf16)
+ * with row strides ldq, ldk, ldv in elements: three results, or the three
+ * parts of one q/k/v plan's rows.  Rotation in fp32, each result rounded to
+ * bf16 once (nearest even).  q_heads a multiple of kv_heads.  Pointers and
+ * row strides multiples of 16 bytes.  One kernel, launched with programmatic
+ * dependent launch.  Errors: INVALID_ARG (also when the current device is not
+ * the cache's), CUDA. */
+int sdq_cache_append(sdq_cache cache, const sdq_batch* batch, int32_t q_heads, const void* q, int64_t ldq,
+                     const void* k, int64_t ldk, const void* v, int64_t ldv, int32_t type, const sdq_rope* rope,
+                     uint16_t* q_out, void* stream);
+
 /* Static string for a status code. */
 const char* sdq_status_string(int status);
 

@@ -7,6 +7,9 @@ no code, tables or constants with the CUDA library in
 ``paper_2510_03275_gb300/``; the two meet only through the seeded inputs made
 by ``paper_2510_03275_gb300.workloads``.
 
-See ``oracle/sdq_oracle.py`` for the definitions and their citations.
+See ``oracle/sdq_oracle.py`` for the definitions and their citations, and
+``oracle/serving_oracle.py`` for the attention cache, attention and sampling
+around the linears.
 """
 from .sdq_oracle import *  # noqa: F401,F403
+from . import serving_oracle as serving  # noqa: F401

@@ -26,6 +26,8 @@ __all__ = [
     "sdq_prep_activations", "sdq_contract", "sdq_contract_add", "sdq_linear_forward", "sdq_read_prep",
     "sdq_workspace_status", "sdq_linear_forward_noalloc", "sdq_noalloc_scratch_bytes", "sdq_noalloc_status",
     "sdq_forward_kernels", "sdq_forward_route", "sdq_status_string", "Plan",
+    "SDQ_F32", "SDQ_BF16", "CacheDesc", "Batch", "Rope", "KVCache",
+    "sdq_cache_bytes", "sdq_cache_create", "sdq_cache_destroy", "sdq_rope_table", "sdq_cache_append",
 ]
 
 SDQ_OK = 0
@@ -33,6 +35,8 @@ SDQ_BINARY = 1
 SDQ_TERNARY = 2
 SDQ_ALPHA_MAXABS = 0
 SDQ_ALPHA_MEANABS = 1
+SDQ_F32 = 0
+SDQ_BF16 = 1
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 library_path = os.path.join(_HERE, "libsdq.so")
@@ -72,6 +76,37 @@ class LayerDesc:
         return int(self.block * Fraction(self.osr))
 
 
+class _CacheDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("kv_heads", "head_dim", "page_tokens", "n_pages")]
+
+
+class _Batch(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("n_seqs", "n_tokens", "max_new", "max_own", "page_stride", "prefix_len")]
+                + [(n, ctypes.c_void_p) for n in ("token_start", "own_len", "pages", "prefix_pages")])
+
+
+class _Rope(ctypes.Structure):
+    _fields_ = [("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p), ("n_pos", ctypes.c_int32), ("dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32)]
+
+
+@dataclass(frozen=True)
+class CacheDesc:
+    """Mirror of ``sdq_cache_desc``."""
+    kv_heads: int
+    head_dim: int
+    page_tokens: int
+    n_pages: int
+
+    def c(self) -> _CacheDesc:
+        return _CacheDesc(self.kv_heads, self.head_dim, self.page_tokens, self.n_pages)
+
+    @property
+    def shape(self):
+        """Of each of the two arrays: (page, key head, token of the page, element)."""
+        return self.n_pages, self.kv_heads, self.page_tokens, self.head_dim
+
+
 _lib = None
 _vp, _sz, _i32, _i64 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32, ctypes.c_int64
 _SIGS = {
@@ -103,6 +138,11 @@ _SIGS = {
     "sdq_linear_forward_noalloc": (ctypes.c_int, [_vp, _vp, _vp, _vp, _i32, _vp, _vp]),
     "sdq_noalloc_status": (ctypes.c_int, [_vp, _i32, _vp]),
     "sdq_noalloc_scratch_bytes": (_sz, []),
+    "sdq_cache_bytes": (_sz, [ctypes.POINTER(_CacheDesc)]),
+    "sdq_cache_create": (ctypes.c_int, [ctypes.POINTER(_CacheDesc), _vp, _vp, ctypes.POINTER(_vp)]),
+    "sdq_cache_destroy": (ctypes.c_int, [_vp]),
+    "sdq_rope_table": (ctypes.c_int, [_i32, _i32, ctypes.c_double, _vp, _vp]),
+    "sdq_cache_append": (ctypes.c_int, [_vp, _vp, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _vp, _vp, _vp]),
     "sdq_status_string": (ctypes.c_char_p, [ctypes.c_int]),
 }
 
@@ -329,6 +369,44 @@ def sdq_noalloc_status(plan, M, stream=None) -> int:
     return lib().sdq_noalloc_status(plan, M, _stream(stream))
 
 
+def sdq_cache_bytes(desc: CacheDesc) -> int:
+    return lib().sdq_cache_bytes(ctypes.byref(desc.c()))
+
+
+def sdq_cache_create(desc: CacheDesc, k_pages, v_pages) -> int:
+    h = ctypes.c_void_p()
+    _check(lib().sdq_cache_create(ctypes.byref(desc.c()), _ptr(k_pages), _ptr(v_pages), ctypes.byref(h)),
+           "sdq_cache_create")
+    return h.value
+
+
+def sdq_cache_destroy(cache: int):
+    _check(lib().sdq_cache_destroy(cache), "sdq_cache_destroy")
+
+
+def sdq_rope_table(n_pos: int, dim: int, base: float = 10000.0):
+    """Host-only: (cos, sin) as float32 numpy arrays (n_pos x dim / 2)."""
+    import numpy as np
+    cos, sin = (np.zeros((max(n_pos, 0), max(dim, 0) // 2), np.float32) for _ in range(2))
+    _check(lib().sdq_rope_table(n_pos, dim, base, cos.ctypes.data_as(_vp), sin.ctypes.data_as(_vp)), "sdq_rope_table")
+    return cos, sin
+
+
+def _dtype(t) -> int:
+    """The ``sdq_dtype`` of a tensor; -1 (which every entry point refuses) for other types."""
+    import torch
+    return SDQ_F32 if t.dtype == torch.float32 else SDQ_BF16 if t.dtype == torch.bfloat16 else -1
+
+
+def sdq_cache_append(cache, batch, q_heads, q, k, v, rope, q_out, stream=None):
+    """q, k, v: one row per token, of one type; their row strides are the tensors'."""
+    kind = _dtype(q) if k.dtype == v.dtype == q.dtype else -1
+    # (a single row has no stride of its own)
+    ldq, ldk, ldv = (t.stride(0) if t.shape[0] > 1 else t.shape[1] for t in (q, k, v))
+    _check(lib().sdq_cache_append(cache, batch.ref, q_heads, q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
+                                  kind, rope.ref, _ptr(q_out), _stream(stream)), "sdq_cache_append")
+
+
 def sdq_status_string(status: int) -> str:
     return lib().sdq_status_string(status).decode()
 
@@ -397,3 +475,103 @@ class Plan:
         y = torch.empty((M, self.desc.n_out), dtype=torch.float32, device=x.device)
         sdq_linear_forward(self.handle, tiled, alpha, x.contiguous(), M, y, ws, stream)
         return y
+
+
+class Batch:
+    """Mirror of ``sdq_batch``: one step's tokens, the pages of their sequences
+    and the prefix that all of them share.  Holds the four int32 tensors."""
+
+    def __init__(self, token_start, own_len, pages, n_tokens, max_new, max_own, prefix_pages=None, prefix_len=0):
+        import torch
+        for name, t, dims in (("token_start", token_start, 1), ("own_len", own_len, 1), ("pages", pages, 2),
+                              ("prefix_pages", prefix_pages, 1)):
+            if t is not None and (t.dtype != torch.int32 or t.dim() != dims or not t.is_cuda
+                                  or (t.numel() > 0 and t.stride(-1) != 1)):
+                raise ValueError(f"Batch: {name} must be a {dims}-d int32 CUDA tensor with adjacent elements")
+        n_seqs = own_len.shape[0]
+        if token_start.shape[0] != n_seqs + 1 or pages.shape[0] != n_seqs:
+            raise ValueError("Batch: token_start needs one entry more than own_len, pages one row for each")
+        self.n_seqs, self.n_tokens, self.max_new, self.max_own = n_seqs, n_tokens, max_new, max_own
+        self.prefix_len = prefix_len
+        self.tensors = (token_start, own_len, pages, prefix_pages)
+        self.page_columns = pages.shape[1]
+        self._c = _Batch(n_seqs, n_tokens, max_new, max_own, pages.stride(0) if n_seqs > 1 else pages.shape[1], prefix_len,
+                         token_start.data_ptr(), own_len.data_ptr(), pages.data_ptr() or None,
+                         None if prefix_pages is None else prefix_pages.data_ptr() or None)
+        self.ref = ctypes.addressof(self._c)
+
+    def check(self, page_tokens: int):
+        """Raise where the page tables are too short for max_own or prefix_len."""
+        if self.max_own > self.page_columns * page_tokens:
+            raise ValueError("Batch: pages has too few columns for max_own")
+        if self.prefix_len > (0 if self.tensors[3] is None else self.tensors[3].shape[0]) * page_tokens:
+            raise ValueError("Batch: prefix_pages is too short for prefix_len")
+
+
+class Rope:
+    """Mirror of ``sdq_rope``: cos and sin tables (n_pos x dim / 2, fp32,
+    device); ``Rope.table`` makes the usual ones, ``Rope()`` rotates nothing."""
+
+    def __init__(self, cos=None, sin=None, interleaved=False):
+        import torch
+        if (cos is None) != (sin is None):
+            raise ValueError("Rope: cos and sin come together")
+        if cos is not None:
+            for t in (cos, sin):
+                if t.dtype != torch.float32 or t.dim() != 2 or not t.is_cuda or not t.is_contiguous() or t.shape != cos.shape:
+                    raise ValueError("Rope: cos and sin must be contiguous 2-d float32 CUDA tensors of one shape")
+        self.tensors = (cos, sin)
+        self._c = _Rope(_ptr(cos), _ptr(sin), 0 if cos is None else cos.shape[0], 0 if cos is None else 2 * cos.shape[1],
+                        int(interleaved))
+        self.ref = ctypes.addressof(self._c)
+
+    @classmethod
+    def table(cls, n_pos, dim, base=10000.0, interleaved=False, device="cuda"):
+        import torch
+        cos, sin = sdq_rope_table(n_pos, dim, base)
+        return cls(torch.from_numpy(cos).to(device), torch.from_numpy(sin).to(device), interleaved)
+
+
+class KVCache:
+    """Owns an ``sdq_cache`` and holds its two arrays (allocated here, zeroed,
+    unless given: bf16, ``desc.shape``, contiguous)."""
+
+    def __init__(self, desc: CacheDesc, k_pages=None, v_pages=None, device="cuda"):
+        import torch
+        self.handle = None
+        self.desc = desc
+        if k_pages is None and v_pages is None:
+            k_pages, v_pages = (torch.zeros(desc.shape, dtype=torch.bfloat16, device=device) for _ in range(2))
+        for t in (k_pages, v_pages):
+            if t is None or t.dtype != torch.bfloat16 or tuple(t.shape) != desc.shape or not t.is_contiguous() or not t.is_cuda:
+                raise ValueError("KVCache: both arrays must be contiguous bfloat16 CUDA tensors of desc.shape")
+        self.k_pages, self.v_pages = k_pages, v_pages
+        self.handle = sdq_cache_create(desc, k_pages, v_pages)
+
+    def close(self):
+        if self.handle:
+            sdq_cache_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def append(self, batch: Batch, q, k, v, rope: Rope, stream=None):
+        """q, k, v: one row per token (fp32 or bf16; rows may be strided) ->
+        the rotated queries (tokens x q_heads x head_dim, bf16); keys and
+        values go to the cache."""
+        import torch
+        d = self.desc
+        for t, width in ((q, q.shape[-1]), (k, d.kv_heads * d.head_dim), (v, d.kv_heads * d.head_dim)):
+            if t.dim() != 2 or t.shape[0] != batch.n_tokens or t.shape[1] != width or t.stride(1) != 1 or not t.is_cuda:
+                raise ValueError("KVCache.append: q, k and v need one row of heads x head_dim elements per token")
+        q_heads, rest = divmod(q.shape[1], d.head_dim)
+        if rest:
+            raise ValueError("KVCache.append: q's rows are not whole heads")
+        batch.check(d.page_tokens)
+        out = torch.empty((batch.n_tokens, q_heads, d.head_dim), dtype=torch.bfloat16, device=q.device)
+        sdq_cache_append(self.handle, batch, q_heads, q, k, v, rope, out, stream)
+        return out
