@@ -464,6 +464,38 @@ int sdq_cache_append(sdq_cache cache, const sdq_batch* batch, int32_t q_heads, c
                      const void* k, int64_t ldk, const void* v, int64_t ldv, int32_t type, const sdq_rope* rope,
                      uint16_t* q_out, void* stream);
 
+/* Attention of a batch's new tokens over the cache: for every token and
+ * query head, out = sum_j softmax_j(scale q . k_j) v_j over the keys that the
+ * token sees (sdq_batch), query head i reading key head i / (q_heads /
+ * kv_heads).  The prefix is computed once for all sequences: its keys and
+ * values are read once for the whole batch, and joined with each sequence's
+ * own part by the parts' maxima and sums.  q: bf16, q_heads x head_dim per
+ * token, token stride ldq in elements (sdq_cache_append's q_out has ldq =
+ * q_heads * head_dim); out: bf16, n_tokens x q_heads x head_dim; lse (may be
+ * NULL): fp32, n_tokens x q_heads, the natural logarithm of the sum of
+ * exp(scale q . k_j), for a caller that joins further parts.  A token that
+ * sees nothing: out 0, lse -inf.  Scores, maxima, sums and outputs are kept in
+ * fp32; the softmax weights are rounded to bf16 for their product with v, the
+ * output once at the end.  Results do not depend on timing: partial sums are
+ * joined in a fixed order.  scale: positive and finite.  q, out 16-byte
+ * aligned, ldq a multiple of 8, ws 256-byte aligned.  Kernels are launched
+ * with programmatic dependent launch.  A value that is not finite at a place
+ * that a token sees reaches that token; at the places of its sequence's later
+ * tokens of the same call it may too (their weight is 0, and 0 times it is
+ * not); free places of a page may hold anything.
+ * sdq_attention_workspace_bytes: for a batch of these integers (the device
+ * arrays are not read); grows with each of them; 0 on invalid input.  The
+ * workspace needs no initialization and may serve any calls in turn.
+ * Errors: INVALID_ARG (also when the current device is not the cache's),
+ * WORKSPACE, CUDA. */
+size_t sdq_attention_workspace_bytes(sdq_cache cache, const sdq_batch* batch, int32_t q_heads);
+int sdq_attention(sdq_cache cache, const sdq_batch* batch, int32_t q_heads, const uint16_t* q, int64_t ldq,
+                  float scale, uint16_t* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+/* Wait for `stream`, then report whether the last sdq_attention call on `ws`
+ * completed its bounded device-side waits: SDQ_OK or SDQ_ERR_TIMEOUT (as
+ * sdq_workspace_status). */
+int sdq_attention_status(const void* ws, void* stream);
+
 /* Static string for a status code. */
 const char* sdq_status_string(int status);
 

@@ -28,6 +28,7 @@ __all__ = [
     "sdq_forward_kernels", "sdq_forward_route", "sdq_status_string", "Plan",
     "SDQ_F32", "SDQ_BF16", "CacheDesc", "Batch", "Rope", "KVCache",
     "sdq_cache_bytes", "sdq_cache_create", "sdq_cache_destroy", "sdq_rope_table", "sdq_cache_append",
+    "sdq_attention_workspace_bytes", "sdq_attention", "sdq_attention_status",
 ]
 
 SDQ_OK = 0
@@ -143,6 +144,9 @@ _SIGS = {
     "sdq_cache_destroy": (ctypes.c_int, [_vp]),
     "sdq_rope_table": (ctypes.c_int, [_i32, _i32, ctypes.c_double, _vp, _vp]),
     "sdq_cache_append": (ctypes.c_int, [_vp, _vp, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _vp, _vp, _vp]),
+    "sdq_attention_workspace_bytes": (_sz, [_vp, _vp, _i32]),
+    "sdq_attention": (ctypes.c_int, [_vp, _vp, _i32, _vp, _i64, ctypes.c_float, _vp, _vp, _vp, _sz, _vp]),
+    "sdq_attention_status": (ctypes.c_int, [_vp, _vp]),
     "sdq_status_string": (ctypes.c_char_p, [ctypes.c_int]),
 }
 
@@ -407,6 +411,20 @@ def sdq_cache_append(cache, batch, q_heads, q, k, v, rope, q_out, stream=None):
                                   kind, rope.ref, _ptr(q_out), _stream(stream)), "sdq_cache_append")
 
 
+def sdq_attention_workspace_bytes(cache, batch, q_heads) -> int:
+    return lib().sdq_attention_workspace_bytes(cache, batch.ref, q_heads)
+
+
+def sdq_attention(cache, batch, q_heads, q, ldq, scale, out, lse, ws, stream=None):
+    _check(lib().sdq_attention(cache, batch.ref, q_heads, q.data_ptr(), ldq, scale, out.data_ptr(), _ptr(lse),
+                               ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream)), "sdq_attention")
+
+
+def sdq_attention_status(ws, stream=None) -> int:
+    """Synchronize and return the status of the last attention call on ``ws``."""
+    return lib().sdq_attention_status(_ptr(ws), _stream(stream))
+
+
 def sdq_status_string(status: int) -> str:
     return lib().sdq_status_string(status).decode()
 
@@ -574,4 +592,34 @@ class KVCache:
         batch.check(d.page_tokens)
         out = torch.empty((batch.n_tokens, q_heads, d.head_dim), dtype=torch.bfloat16, device=q.device)
         sdq_cache_append(self.handle, batch, q_heads, q, k, v, rope, out, stream)
+        return out
+
+    def alloc_workspace(self, batch: Batch, q_heads: int):
+        """For ``attend`` on this batch, and on any whose integers are no larger."""
+        import torch
+        n = sdq_attention_workspace_bytes(self.handle, batch, q_heads)
+        if n == 0:
+            raise SdqError(-1, "sdq_attention_workspace_bytes")
+        return torch.empty(n, dtype=torch.uint8, device=self.k_pages.device)
+
+    def attend(self, batch: Batch, q, scale=None, ws=None, lse=None, stream=None):
+        """q (tokens x q_heads x head_dim, bf16; tokens may be strided) ->
+        outputs of the same shape in bf16.  scale: 1 / sqrt(head_dim) unless
+        given; lse: fp32 (tokens x q_heads), written if given."""
+        import torch
+        d = self.desc
+        if q.dim() != 3 or q.shape[0] != batch.n_tokens or q.shape[2] != d.head_dim or q.dtype != torch.bfloat16 or not q.is_cuda:
+            raise ValueError("KVCache.attend: q must be a bfloat16 CUDA tensor (tokens, q_heads, head_dim)")
+        heads = q.shape[1]
+        if q.stride(2) != 1 or (heads > 1 and q.stride(1) != d.head_dim):
+            raise ValueError("KVCache.attend: the heads of a token of q must be adjacent")
+        if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (batch.n_tokens, heads)
+                                or not lse.is_contiguous() or not lse.is_cuda):
+            raise ValueError("KVCache.attend: lse must be a contiguous float32 CUDA tensor (tokens, q_heads)")
+        batch.check(d.page_tokens)
+        if ws is None:
+            ws = self.alloc_workspace(batch, heads)
+        out = torch.empty((batch.n_tokens, heads, d.head_dim), dtype=torch.bfloat16, device=q.device)
+        sdq_attention(self.handle, batch, heads, q, q.stride(0) if batch.n_tokens > 1 else heads * d.head_dim,
+                      d.head_dim ** -0.5 if scale is None else scale, out, lse, ws, stream)
         return out
