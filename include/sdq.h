@@ -496,6 +496,29 @@ int sdq_attention(sdq_cache cache, const sdq_batch* batch, int32_t q_heads, cons
  * sdq_workspace_status). */
 int sdq_attention_status(const void* ws, void* stream);
 
+/* One token per row of logits (device, fp32 or bf16 as `type`, rows x vocab
+ * with row stride ld in elements), from one random number per row, u in [0,
+ * 1).  With z the row's logits, T = temperature, w_i = exp((z_i - max z) / T)
+ * and the row ordered by z, largest first, equal ones by index, kept are
+ *   top_k > 0    the first top_k;
+ *   top_p < 1    of those, the ones before which less than top_p of their
+ *                mass (sum of w) lies;
+ *   min_p > 0    of those, the ones with w_i >= min_p;
+ * and always the first.  The token is the lowest kept index at which the
+ * running sum of the kept w, in index order, exceeds u times their mass.  T
+ * <= 0 (or NaN): the first of the largest logits.  NaN logits count as -inf;
+ * a row without a logit above -inf gives -1; with logits of +inf only those
+ * have a weight.  temperature, top_k, top_p, min_p: one per row (device), or
+ * NULL for 1, 0, 1, 0.  Weights are fp32 (exp, one quotient), masses whole
+ * multiples of 2^-44 of the largest weight, so that sums are exact and the
+ * token depends on nothing but its inputs; weights below 2^-45 count as 0.
+ * vocab up to 393216, rows up to 65535; no workspace; one kernel, launched
+ * with programmatic dependent launch.  Errors: INVALID_ARG, UNSUPPORTED
+ * (current device is not compute capability 10.3), CUDA. */
+int sdq_sample(const void* logits, int32_t type, int32_t rows, int32_t vocab, int64_t ld, const float* u,
+               const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+               int32_t* tokens, void* stream);
+
 /* Static string for a status code. */
 const char* sdq_status_string(int status);
 

@@ -29,6 +29,7 @@ __all__ = [
     "SDQ_F32", "SDQ_BF16", "CacheDesc", "Batch", "Rope", "KVCache",
     "sdq_cache_bytes", "sdq_cache_create", "sdq_cache_destroy", "sdq_rope_table", "sdq_cache_append",
     "sdq_attention_workspace_bytes", "sdq_attention", "sdq_attention_status",
+    "sdq_sample", "sample",
 ]
 
 SDQ_OK = 0
@@ -147,6 +148,7 @@ _SIGS = {
     "sdq_attention_workspace_bytes": (_sz, [_vp, _vp, _i32]),
     "sdq_attention": (ctypes.c_int, [_vp, _vp, _i32, _vp, _i64, ctypes.c_float, _vp, _vp, _vp, _sz, _vp]),
     "sdq_attention_status": (ctypes.c_int, [_vp, _vp]),
+    "sdq_sample": (ctypes.c_int, [_vp, _i32, _i32, _i32, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
     "sdq_status_string": (ctypes.c_char_p, [ctypes.c_int]),
 }
 
@@ -425,6 +427,14 @@ def sdq_attention_status(ws, stream=None) -> int:
     return lib().sdq_attention_status(_ptr(ws), _stream(stream))
 
 
+def sdq_sample(logits, u, temperature, top_k, top_p, min_p, tokens, stream=None):
+    """logits: rows x vocab, adjacent in a row; any of the four settings may be None."""
+    rows, vocab = logits.shape
+    _check(lib().sdq_sample(logits.data_ptr(), _dtype(logits), rows, vocab, logits.stride(0) if rows > 1 else vocab,
+                            u.data_ptr(), _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), tokens.data_ptr(),
+                            _stream(stream)), "sdq_sample")
+
+
 def sdq_status_string(status: int) -> str:
     return lib().sdq_status_string(status).decode()
 
@@ -623,3 +633,19 @@ class KVCache:
         sdq_attention(self.handle, batch, heads, q, q.stride(0) if batch.n_tokens > 1 else heads * d.head_dim,
                       d.head_dim ** -0.5 if scale is None else scale, out, lse, ws, stream)
         return out
+
+
+def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
+    """One token per row of logits (rows x vocab, fp32 or bf16; rows may be
+    strided) from one random number per row -> int32 tokens.  The settings:
+    one per row (float32, top_k int32), or None for none."""
+    import torch
+    if logits.dim() != 2 or logits.stride(1) != 1 or not logits.is_cuda:
+        raise ValueError("sample: logits must be a CUDA tensor (rows, vocab) with adjacent elements in a row")
+    for t, dtype in ((u, torch.float32), (temperature, torch.float32), (top_k, torch.int32), (top_p, torch.float32),
+                     (min_p, torch.float32)):
+        if t is not None and (t.dtype != dtype or t.shape != logits.shape[:1] or not t.is_contiguous() or not t.is_cuda):
+            raise ValueError("sample: u, temperature, top_p and min_p are float32, top_k int32, one per row, on the GPU")
+    tokens = torch.empty(logits.shape[0], dtype=torch.int32, device=logits.device)
+    sdq_sample(logits, u, temperature, top_k, top_p, min_p, tokens, stream)
+    return tokens

@@ -63,3 +63,23 @@ def test_oracle_append_and_attend_by_hand():
     assert np.allclose(lse[:, 0], np.log([4, 8]))
     out, lse, _ = O.serving.attend(q[:1], kp, vp, [0, 1], [0], [[1]], [], 0, 1.0)
     assert np.all(out == 0) and np.all(lse == -np.inf)
+
+
+def test_oracle_sampling_by_hand():
+    """Weights 8 : 4 : 2 : 1 : 1 at indices 3, 0, 4, 1, 2."""
+    z = np.log([4.0, 1.0, 1.0, 8.0, 2.0])
+    pick = lambda u, *a: O.serving.sample_row(z, u, *a)[0]
+    assert [pick(u) for u in (0.0, 0.24, 0.26, 0.32, 0.4, 0.8, 0.95)] == [0, 0, 1, 2, 3, 3, 4]
+    assert pick(0.9, 0.0) == 3 and pick(0.9, 1.0, 1) == 3
+    assert [pick(u, 1.0, 2) for u in (0.3, 0.4)] == [0, 3]
+    assert [pick(u, 1.0, 4) for u in (0.28, 0.9)] == [1, 4]                     # index 2 ties with 1 and is out
+    assert [pick(u, 1.0, 0, 0.7) for u in (0.3, 0.34)] == [0, 3]                # 8 of 16 lie before index 0, 12 before 4
+    assert [pick(u, 1.0, 0, 1.0, 0.2) for u in (0.28, 0.3, 0.9)] == [0, 3, 4]
+    assert [pick(u, 0.5, 3) for u in (0.15, 0.25, 0.97)] == [0, 3, 4]           # squares: 64 : 16 : 4
+    assert O.serving.sample_row([-np.inf, np.nan], 0.5)[0] == -1
+
+
+def test_sample_null_pointers_are_refused(sdq):
+    assert sdq.lib().sdq_sample(None, 0, 1, 10, 10, None, None, None, None, None, None, None) == -1
+    assert sdq.lib().sdq_attention(None, None, 1, None, 0, 1.0, None, None, None, 0, None) == -1
+    assert sdq.lib().sdq_attention_workspace_bytes(None, None, 1) == 0
