@@ -456,7 +456,8 @@ int sdq_rope_table(int32_t n_pos, int32_t dim, double base, float* cos_host, flo
  * hold one row per token (q_heads or kv_heads x head_dim, `type` fp32 or bf16)
  * with row strides ldq, ldk, ldv in elements: three results, or the three
  * parts of one q/k/v plan's rows.  Rotation in fp32, each result rounded to
- * bf16 once (nearest even).  q_heads a multiple of kv_heads.  Pointers and
+ * bf16 once (nearest even).  q_heads a multiple of kv_heads, n_tokens *
+ * q_heads < 2^31.  Pointers and
  * row strides multiples of 16 bytes.  One kernel, launched with programmatic
  * dependent launch.  Errors: INVALID_ARG (also when the current device is not
  * the cache's), CUDA. */

@@ -485,7 +485,7 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendParams p) {
   for (int part = kPrefix; part >= kOwn; --part) {
     int n = 0, slot0 = 0, r = 0;   // partials: p.splits[part] by row, then slots slot0 ..
     if (p.wide[part]) {
-      n = part == kPrefix || (live && q.own > 0) ? p.splits[part] : 0;
+      n = part == kPrefix || (live && (p.chained || q.own > 0)) ? p.splits[part] : 0;
     } else if (p.narrow[part]) {
       int64_t a = 0;
       int tiles = 0, rr = 0;
@@ -558,24 +558,35 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendParams p) {
 
 // ------------------------------------------------------------------- host
 struct Route {
-  int nt;              // 8-row groups of the narrow kernel's row blocks
+  int nt;              // 8-row groups of the narrow kernel's row blocks (0: not used)
   int rows, ctas;      // its row block, its thread blocks
 };
 
-constexpr int kMaxNt = 4;
+constexpr int kMaxNt = 4;   // the narrow kernel takes up to 32 rows of a key head
 
+// The wide kernel takes the parts with more rows per key head than the narrow
+// one's blocks hold.  Where a sequence brings 128 rows and more on the
+// average, its row blocks run over the prefix and its own keys in one line;
+// below that the batch's rows share blocks against the prefix.
 Route route_of(const sdq_cache_s* c, const sdq_batch* b, int q_heads, AttendParams* p) {
   const int group = q_heads / c->desc.kv_heads;
+  const int64_t own_rows = b->max_own > 0 ? (int64_t)b->max_new * group : 0;
+  const int64_t prefix_rows = b->prefix_len > 0 ? (int64_t)b->n_tokens * group : 0;
+  const bool own_wide = own_rows > 8 * kMaxNt;
+  p->chained = own_wide && prefix_rows > 0 && prefix_rows >= 128ll * b->n_seqs;
+  p->wide[kOwn] = own_wide;
+  p->narrow[kOwn] = own_rows > 0 && !own_wide;
+  p->wide[kPrefix] = prefix_rows > 8 * kMaxNt && !p->chained;
+  p->narrow[kPrefix] = prefix_rows > 0 && prefix_rows <= 8 * kMaxNt;
+  for (int part = 0; part < 2; ++part)
+    p->splits[part] = p->wide[part] ? wide_splits(c, b, q_heads, part, p->chained) : p->narrow[part];
+  const bool both = (p->wide[kOwn] || p->narrow[kOwn]) && (p->wide[kPrefix] || p->narrow[kPrefix]);
+  p->direct = !both && p->splits[kOwn] <= 1 && p->splits[kPrefix] <= 1;
   Route r{};
-  p->narrow[kOwn] = b->max_own > 0;
-  p->narrow[kPrefix] = b->prefix_len > 0;
-  p->wide[kOwn] = p->wide[kPrefix] = 0;
-  p->direct = !(p->narrow[kOwn] && p->narrow[kPrefix]);
-  const int64_t most = std::max(p->narrow[kOwn] ? (int64_t)b->max_new * group : 0, p->narrow[kPrefix] ? (int64_t)b->n_tokens * group : 0);
-  r.nt = (int)std::max<int64_t>(1, std::min<int64_t>(kMaxNt, (most + 7) / 8));
+  const int64_t most = std::max(p->narrow[kOwn] ? own_rows : 0, p->narrow[kPrefix] ? prefix_rows : 0);
+  r.nt = (int)((most + 7) / 8);
   r.rows = 8 * r.nt;
-  r.ctas = c->sm_count * (r.nt == 1 ? 2 : 1);
-  for (int part = 0; part < 2; ++part) p->splits[part] = p->narrow[part] ? 1 : 0;
+  r.ctas = c->sm_count * (r.nt == 0 ? 0 : r.nt == 1 ? 2 : 1);
   return r;
 }
 
@@ -600,6 +611,12 @@ AttendWs attend_workspace(const sdq_cache_s* c, const sdq_batch* b, int q_heads,
   return L;
 }
 
+template <int D, int R, int KT>
+cudaError_t launch_join(const AttendParams& p, cudaStream_t st) {
+  const int64_t rows = (int64_t)p.b.n_tokens * p.q_heads;
+  return launch_pdl(join_kernel<D, R, KT>, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, st, p);
+}
+
 template <int D, int NT>
 cudaError_t launch_narrow(const sdq_cache_s* c, const AttendParams& p, cudaStream_t st) {
   using S = NarrowShape<D, NT>;
@@ -607,14 +624,18 @@ cudaError_t launch_narrow(const sdq_cache_s* c, const AttendParams& p, cudaStrea
   cudaError_t e = smem_limit_once(narrow_kernel<D, NT>, S::kSmem, c->device, smem_set);
   if (e != cudaSuccess) return e;
   e = launch_pdl(narrow_kernel<D, NT>, dim3((unsigned)p.ctas), dim3(S::kThreads), (size_t)S::kSmem, st, c->kmap, c->vmap, p);
-  if (e != cudaSuccess) return e;
-  const int64_t rows = (int64_t)p.b.n_tokens * p.q_heads;
-  return launch_pdl(join_kernel<D, S::kRows, S::kTile>, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, st, p);
+  return e == cudaSuccess ? launch_join<D, S::kRows, S::kTile>(p, st) : e;
 }
 
 template <int D>
 cudaError_t launch_parts(const sdq_cache_s* c, const AttendParams& p, const Route& r, cudaStream_t st) {
+  for (int part = kPrefix; part >= kOwn; --part)
+    if (p.wide[part]) {
+      const cudaError_t e = launch_wide(c, p, part, st);
+      if (e != cudaSuccess) return e;
+    }
   switch (r.nt) {
+    case 0: return p.direct && (p.wide[kOwn] || p.wide[kPrefix]) ? cudaSuccess : launch_join<D, 8, 64>(p, st);
     case 1: return launch_narrow<D, 1>(c, p, st);
     case 2: return launch_narrow<D, 2>(c, p, st);
     case 3: return launch_narrow<D, 3>(c, p, st);

@@ -32,6 +32,7 @@ struct AttendParams {
   int q_heads, kv_heads, group, page_shift, box_shift, n_pages;
   int narrow[2], wide[2];   // which kernel takes a part (neither: it has no keys)
   int direct;               // one part only: whole rows may go straight to `out`
+  int chained;              // the wide kernel's rows of kOwn run over the prefix first (no kPrefix part)
   int splits[2];            // partials by row of each part that the join reads
   uint64_t* rec;
   uint64_t call;
@@ -51,5 +52,10 @@ __device__ __forceinline__ float log2_approx(float x) {
   asm("lg2.approx.f32 %0, %1;\n" : "=f"(r) : "f"(x));
   return r;
 }
+
+// The wide kernel on `part`, and how many ways it splits the keys of a row
+// block (p.splits[part]).
+int wide_splits(const sdq_cache_s* c, const sdq_batch* b, int q_heads, int part, bool chained);
+cudaError_t launch_wide(const sdq_cache_s* c, const AttendParams& p, int part, cudaStream_t st);
 
 }  // namespace sdq

@@ -1,0 +1,435 @@
+// Attention over the paged cache: the kernel for many query rows per key head
+// (prompts, and a batch's rows against the shared prefix).
+#include <algorithm>
+
+#include "attention.cuh"
+
+namespace sdq {
+
+namespace {
+
+// ----------------------------------------------------------- wide kernel
+// A thread block takes 256 query rows of one key head (new token major, then
+// head of the group) and a line of key tiles (128 keys each: the prefix's,
+// then the sequence's own, or one of the two); the tensor cores bound it, 2 x
+// 128 x 128 x head_dim products a tile and 128 rows:
+//   warps 0-3, 4-7  rows 0-127, 128-255, a row per thread: S from tensor
+//                   memory, running maximum and sum, P (bf16) back into S's
+//                   place; O is rescaled there only when a row's maximum has
+//                   grown by more than 2^8 (weights stay below 2^8, sums in
+//                   fp32 lose nothing by it)
+//   warp 8          S = Q K^T (both from shared memory) and O += P V (P from
+//                   tensor memory, V as the transposed operand) on tcgen05;
+//                   while one half's softmax runs, the other half's products do
+//   warp 9          K and V tiles, page by page, into a ring (TMA, 128-byte
+//                   swizzle); warps 10 and 11 only complete its warpgroup
+// The MMAs of a thread block run in the order of their issue, so that S of the
+// next tile may overwrite P once the product that reads it is issued.
+// Registers: 384 threads hold 168 each at launch; the first two warpgroups go
+// to 224 once the third has gone down to 56 (224 + 224 + 56 = 3 x 168).
+constexpr int kWideThreads = 384;
+constexpr int kKeys = 128;             // of a tile
+constexpr int kHalf = kKeys * 128;     // bytes: 128 rows x 64 elements
+
+template <int D> struct WideShape {
+  static constexpr int kMat = (D / 64) * kHalf;              // 128 rows of Q, K or V
+  static constexpr int kRing = D == 128 ? 5 : 8;
+  static constexpr int kSmem = 1024 + (2 + kRing) * kMat;
+};
+
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr));
+}
+
+// Operand with its second dimension contiguous (V: keys x 64 elements per
+// 128-byte row, 128-byte swizzle): 8-key groups 1024 bytes apart, the next 64
+// elements kHalf bytes on.
+__device__ __forceinline__ uint64_t sw128_mn_desc(uint32_t saddr) {
+  uint64_t d = 0;
+  d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)(kHalf >> 4) << 16;
+  d |= (uint64_t)(1024 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+
+// What a thread block works on.
+struct WideItem {
+  int first, rows, r0;       // first token, rows of the (sequence, head) or of the batch, first row of the block
+  int h, split;
+  int s;                     // sequence, -1: the whole batch
+  int own, count;            // its own tokens and new tokens
+  int prefix_tiles, t0, t1;  // of the line: the prefix's tiles, this block's [t0, t1)
+};
+
+// (a whole warp; false: nothing to do)
+__device__ __forceinline__ bool wide_item(const AttendParams& p, int part, WideItem* w) {
+  const int splits = p.splits[part];
+  const int id = blockIdx.x / (p.kv_heads * splits), rest = blockIdx.x % (p.kv_heads * splits);
+  w->h = rest / splits;
+  w->split = rest % splits;
+  const int ptiles = (p.b.prefix_len + kKeys - 1) / kKeys;
+  int tiles;
+  if (part == kPrefix) {
+    w->s = -1;
+    w->first = 0;
+    w->rows = p.b.n_tokens * p.group;
+    w->r0 = id * 256;
+    w->own = w->count = 0;
+    w->prefix_tiles = tiles = ptiles;
+    if (w->r0 >= w->rows) return false;
+  } else {
+    // block `id` counted over the sequences' row blocks
+    const int lane = threadIdx.x & 31;
+    int base = 0, s = -1, rb = 0;
+    for (int s0 = 0; s0 < p.b.n_seqs && s < 0; s0 += 32) {
+      const int n = s0 + lane < p.b.n_seqs ? (seq_span(p.b, s0 + lane).count * p.group + 255) / 256 : 0;
+      int end = n;
+      for (int d = 1; d < 32; d <<= 1) {
+        const int o = __shfl_up_sync(0xffffffffu, end, d);
+        if (lane >= d) end += o;
+      }
+      const uint32_t past = __ballot_sync(0xffffffffu, base + end > id);
+      if (past) {
+        const int l = __ffs(past) - 1;
+        s = s0 + l;
+        rb = id - base - __shfl_sync(0xffffffffu, end - n, l);
+        rb = __shfl_sync(0xffffffffu, n, l) - 1 - rb;   // the blocks that see the most keys first
+      }
+      base += __shfl_sync(0xffffffffu, end, 31);
+    }
+    if (s < 0) return false;
+    const SeqSpan q = seq_span(p.b, s);
+    w->s = s;
+    w->first = q.first;
+    w->count = q.count;
+    w->own = q.own;
+    w->rows = q.count * p.group;
+    w->r0 = rb * 256;
+    w->prefix_tiles = p.chained ? ptiles : 0;
+    const int last = min(w->rows, w->r0 + 256) - 1;   // its last row sees the most
+    tiles = w->prefix_tiles + (max(0, q.own - q.count + last / p.group + 1) + kKeys - 1) / kKeys;
+  }
+  const int per = (tiles + splits - 1) / splits;
+  w->t0 = min(tiles, w->split * per);
+  w->t1 = min(tiles, w->t0 + per);
+  return true;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kWideThreads, 1)
+    wide_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const AttendParams p,
+                const int part) {
+  using S = WideShape<D>;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t full[S::kRing], empty[S::kRing], q_full, s_full[2], p_full[2], mma_done;
+  __shared__ uint32_t tmem_base;
+  const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
+  const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t ring = sbase + 2 * S::kMat;
+  uint8_t* ring_ptr = smem_raw + (ring - smem_u32(smem_raw));
+  pdl_wait();
+  pdl_launch_dependents();
+  call_record_start(p.rec, p.call, blockIdx.x == 0 && tid == 0);
+  WideItem w;
+  if (!wide_item(p, part, &w)) return;   // (all warps alike)
+  const int n = w.t1 - w.t0, halves = w.rows - w.r0 > 128 ? 2 : 1;
+  if (tid == 0) {
+    for (int i = 0; i < S::kRing; ++i) {
+      mbar_init(&full[i], 1);
+      mbar_init(&empty[i], 1);
+    }
+    mbar_init(&q_full, 128 * halves);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&s_full[i], 1);
+      mbar_init(&p_full[i], 128);
+    }
+    mbar_init(&mma_done, 1);
+    fence_mbar_init();
+  }
+  if (warp == 8) {
+    tmem_alloc(&tmem_base, 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_base;
+  bool ok = true;
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;\n");
+    if (warp == 9) {
+      // ------------------------------------------------------------ loads
+      const int box = 1 << p.box_shift, per_page = 1 << (p.page_shift - p.box_shift), per_tile = kKeys >> p.box_shift;
+      const int32_t* own_table = p.b.pages + (int64_t)(w.s < 0 ? 0 : w.s) * p.b.page_stride;
+      // the page of the lane's box of line tile t (-1: past the last token), and the tile's boxes
+      auto boxes_of = [&](int t) {
+        const int keys = t < w.prefix_tiles ? p.b.prefix_len : w.own, at = (t < w.prefix_tiles ? t : t - w.prefix_tiles) * per_tile;
+        return max(0, min(per_tile, ((keys + box - 1) >> p.box_shift) - at));
+      };
+      auto row_of = [&](int t) {
+        const int at = (t < w.prefix_tiles ? t : t - w.prefix_tiles) * per_tile + lane;
+        const int pg = t < w.t1 && lane < boxes_of(t) ? __ldg((t < w.prefix_tiles ? p.b.prefix_pages : own_table) + at / per_page) : -1;
+        // (a page outside the cache: rows outside the arrays, which read as zeros)
+        return pg >= 0 && pg < p.n_pages ? ((pg * p.kv_heads + w.h) << p.page_shift) + ((at & (per_page - 1)) << p.box_shift) : -box;
+      };
+      int y_next = row_of(w.t0), slot = 0;
+      for (int t = w.t0; t < w.t1 && ok; ++t) {
+        const int y = y_next, nb = boxes_of(t);
+        y_next = row_of(t + 1);
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv, ++slot) {
+          const int st = slot % S::kRing, r = slot / S::kRing;
+          if (r > 0 && !mbar_wait_warp(&empty[st], (r - 1) & 1)) {
+            ok = false;
+            break;
+          }
+          mbar_expect_tx_warp(&full[st], (uint32_t)((nb << p.box_shift) * 128 * (D / 64)));
+          for (int i = 0; i < nb; ++i) {
+            const int yi = __shfl_sync(0xffffffffu, y, i);
+#pragma unroll
+            for (int half = 0; half < D / 64; ++half)
+              tma_load_2d_warp(ring_ptr + st * S::kMat + half * kHalf + ((i * box) << 7), kv ? &vmap : &kmap, 64 * half, yi, &full[st]);
+          }
+        }
+      }
+      // the copies in flight have landed before the thread block ends
+      for (int j = max(0, slot - S::kRing); j < slot; ++j)
+        if (!mbar_wait_warp(&full[j % S::kRing], (j / S::kRing) & 1)) ok = false;
+    } else if (warp == 8) {
+      // --------------------------------------------------------- products
+      constexpr uint32_t kF32Bf16 = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(128 >> 4) << 24);   // M = 128
+      constexpr uint32_t qk_idesc = kF32Bf16 | ((uint32_t)(kKeys >> 3) << 17);
+      constexpr uint32_t pv_idesc = kF32Bf16 | ((uint32_t)(D >> 3) << 17) | (1u << 16);   // B with its N contiguous
+      auto scores = [&](int half, int st) {
+        const uint64_t a = sw128_desc(sbase + half * S::kMat), b = sw128_desc(ring + st * S::kMat);
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          const uint64_t off = (uint64_t)((k >> 2) * (kHalf >> 4) + 2 * (k & 3));
+          umma_bf16_warp(tmem + 128 * half, a + off, b + off, qk_idesc, k > 0);
+        }
+        umma_commit_warp(&s_full[half]);
+      };
+      if (n > 0) {
+        ok = mbar_wait_warp(&q_full, 0) && mbar_wait_warp(&full[0], 0);
+        tc_fence_after();
+        if (ok) {
+          for (int half = 0; half < halves; ++half) scores(half, 0);
+          umma_commit_warp(&empty[0]);
+        }
+        for (int i = 0; i < n && ok; ++i) {
+          const int kn = 2 * i + 2, vs = (2 * i + 1) % S::kRing, ks = kn % S::kRing;
+          for (int half = 0; half < halves && ok; ++half) {
+            ok = mbar_wait_warp(&p_full[half], i & 1);
+            if (ok && half == 0) ok = mbar_wait_warp(&full[vs], ((2 * i + 1) / S::kRing) & 1);
+            if (!ok) break;
+            tc_fence_after();
+            const uint64_t b = sw128_mn_desc(ring + vs * S::kMat);
+#pragma unroll
+            for (int k = 0; k < kKeys / 16; ++k)
+              umma_bf16_ts_warp(tmem + 256 + D * half, tmem + 128 * half + 8 * k, b + (uint64_t)(k * (2048 >> 4)), pv_idesc, (i | k) != 0);
+            if (half == halves - 1) umma_commit_warp(&empty[vs]);
+            if (i + 1 < n) {
+              if (half == 0) ok = mbar_wait_warp(&full[ks], (kn / S::kRing) & 1);
+              if (!ok) break;
+              tc_fence_after();
+              scores(half, ks);
+              if (half == halves - 1) umma_commit_warp(&empty[ks]);
+            }
+          }
+        }
+        umma_commit_warp(&mma_done);
+        if (!mbar_wait_warp(&mma_done, 0)) ok = false;
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 224;\n");
+    if ((warp >> 2) < halves) {
+      // ---------------------------------------------------------- softmax
+      const int half = warp >> 2, wtid = tid & 127;
+      const uint32_t qb = sbase + half * S::kMat;
+      for (int i = wtid; i < 128 * (D / 8); i += 128) {
+        const int r = i / (D / 8), c = i % (D / 8), row = w.r0 + 128 * half + r;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (row < w.rows) {
+          const int tok = row / p.group, g = row - tok * p.group;
+          v = __ldg(reinterpret_cast<const uint4*>(p.q + (int64_t)(w.first + tok) * p.ldq + (int64_t)(w.h * p.group + g) * D) + c);
+        }
+        const uint32_t a = qb + (uint32_t)((c >> 3) * kHalf + r * 128 + (((c & 7) ^ (r & 7)) << 4));
+        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};\n" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+      }
+      fence_proxy_async_smem();
+      mbar_arrive(&q_full);
+      const int row = w.r0 + 128 * half + wtid, tok = row / p.group, g = row - tok * p.group;
+      const bool live = row < w.rows;
+      // own keys that this row sees, and that every row of its half does
+      const int lim = live ? w.own - w.count + tok + 1 : w.own;
+      const int all = w.own - w.count + (w.r0 + 128 * half) / p.group + 1;
+      const uint32_t ts = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + 128 * half;
+      const uint32_t to = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + 256 + D * half;
+      float m = -INFINITY, l = 0.f;   // reference maximum (log2 units) and sum
+      for (int i = 0; i < n; ++i) {
+        if (!mbar_wait_warp(&s_full[half], i & 1)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        uint32_t x[128];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_ld32(ts + 32 * c, x + 32 * c);
+        tmem_ld_wait();
+        const int t = w.t0 + i;
+        const bool pre = t < w.prefix_tiles;
+        const int k0 = (pre ? t : t - w.prefix_tiles) * kKeys, keys = pre ? p.b.prefix_len : w.own;
+        if (k0 + kKeys > (pre ? keys : all)) {
+          const int see = (pre ? keys : lim) - k0;   // of this tile
+#pragma unroll
+          for (int j = 0; j < 128; ++j)
+            if (j >= see) x[j] = 0xFF800000u;
+          if (k0 + kKeys > keys) {
+            // values past the last key are leftovers (perhaps NaN): zero times them has to be zero
+            const int vs = (2 * i + 1) % S::kRing;
+            if (!mbar_wait_warp(&full[vs], ((2 * i + 1) / S::kRing) & 1)) {
+              ok = false;
+              break;
+            }
+            if (k0 + wtid >= keys) {
+#pragma unroll
+              for (int c = 0; c < D / 8; ++c)
+                asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};\n" ::"r"(
+                                 (uint32_t)(ring + vs * S::kMat + (c >> 3) * kHalf + wtid * 128 + ((c & 7) << 4))), "r"(0) : "memory");
+            }
+            fence_proxy_async_smem();
+          }
+        }
+        float mx[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) mx[c] = __uint_as_float(x[c]);
+#pragma unroll
+        for (int j = 4; j < 128; ++j) mx[j & 3] = fmaxf(mx[j & 3], __uint_as_float(x[j]));
+        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale;
+        const bool grow = top > m + 8.f;   // (also from -inf)
+        if (__any_sync(0xffffffffu, grow)) {
+          const float f = grow ? exp2_approx(m - top) : 1.f;
+          if (grow) m = top;
+          l *= f;
+          if (i > 0) {   // (the product before this tile's scores is complete)
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) {
+              uint32_t o[32];
+              tmem_ld32(to + 32 * c, o);
+              tmem_ld_wait();
+#pragma unroll
+              for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+              tmem_st32(to + 32 * c, o);
+            }
+          }
+        }
+        const float neg = m == -INFINITY ? 0.f : -m;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          uint32_t e[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) {
+            const float a = exp2_approx(fmaf(__uint_as_float(x[64 * c + 2 * j]), p.scale, neg));
+            const float b = exp2_approx(fmaf(__uint_as_float(x[64 * c + 2 * j + 1]), p.scale, neg));
+            sum[2 * (j & 1)] += a;
+            sum[2 * (j & 1) + 1] += b;
+            e[j] = pack_bf16x2(a, b);
+          }
+          tmem_st32(ts + 32 * c, e);
+        }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        tmem_st_wait();
+        tc_fence_before();
+        mbar_arrive(&p_full[half]);
+      }
+      // ------------------------------------------------------------- out
+      if (n > 0 && ok) ok = mbar_wait_warp(&mma_done, 0);
+      tc_fence_after();
+      if (ok) {
+        const int64_t at = (int64_t)(w.first + tok) * p.q_heads + w.h * p.group + g;
+        const int64_t rows = (int64_t)p.b.n_tokens * p.q_heads, pr = w.split * rows + at;
+        const float k = p.direct ? (l > 0.f ? 1.f / l : l) : 1.f;   // (0 where nothing is seen; NaN stays)
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t o[32];
+          if (n > 0) {
+            tmem_ld32(to + 32 * c, o);
+            tmem_ld_wait();
+          } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) o[j] = 0;
+          }
+          if (live && p.direct) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 8) {
+              uint4 v;
+              v.x = pack_bf16x2(__uint_as_float(o[j]) * k, __uint_as_float(o[j + 1]) * k);
+              v.y = pack_bf16x2(__uint_as_float(o[j + 2]) * k, __uint_as_float(o[j + 3]) * k);
+              v.z = pack_bf16x2(__uint_as_float(o[j + 4]) * k, __uint_as_float(o[j + 5]) * k);
+              v.w = pack_bf16x2(__uint_as_float(o[j + 6]) * k, __uint_as_float(o[j + 7]) * k);
+              *reinterpret_cast<uint4*>(p.out + at * D + 32 * c + j) = v;
+            }
+          } else if (live && n > 0) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 4)
+              *reinterpret_cast<uint4*>(p.o[part] + pr * D + 32 * c + j) = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+          }
+          __syncwarp();
+        }
+        if (live) {
+          if (!p.direct) p.ml[part][pr] = make_float2(m, l);
+          else if (p.lse) p.lse[at] = m == -INFINITY ? m : (m + log2_approx(l)) * 0.69314718056f;
+        }
+      }
+    }
+  }
+  if (!ok && lane == 0) call_record_fail(p.rec, p.call);
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 8) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+// Row blocks that the grid has to hold: of all tokens, or at most those of the
+// sequences (each ends in a block of its own).
+int64_t wide_blocks(const sdq_batch* b, int group, int part) {
+  const int64_t rows = (int64_t)b->n_tokens * group;
+  return part == kPrefix ? (rows + 255) / 256 : rows / 256 + std::min(b->n_seqs, b->n_tokens);
+}
+
+template <int D>
+cudaError_t launch(const sdq_cache_s* c, const AttendParams& p, int part, cudaStream_t st) {
+  static std::atomic<int> smem_set[64];
+  const cudaError_t e = smem_limit_once(wide_kernel<D>, WideShape<D>::kSmem, c->device, smem_set);
+  if (e != cudaSuccess) return e;
+  const int64_t grid = wide_blocks(&p.b, p.group, part) * p.kv_heads * p.splits[part];
+  return launch_pdl(wide_kernel<D>, dim3((unsigned)grid), dim3(kWideThreads), (size_t)WideShape<D>::kSmem, st, c->kmap, c->vmap, p, part);
+}
+
+}  // namespace
+
+int wide_splits(const sdq_cache_s* c, const sdq_batch* b, int q_heads, int part, bool chained) {
+  const int64_t items = wide_blocks(b, q_heads / c->desc.kv_heads, part) * c->desc.kv_heads;
+  const int64_t tiles = (part == kPrefix || chained ? ((int64_t)b->prefix_len + kKeys - 1) / kKeys : 0) +
+                        (part == kOwn ? ((int64_t)b->max_own + kKeys - 1) / kKeys : 0);
+  return (int)std::max<int64_t>(1, std::min<int64_t>({c->sm_count / items, tiles, 64}));
+}
+
+cudaError_t launch_wide(const sdq_cache_s* c, const AttendParams& p, int part, cudaStream_t st) {
+  return c->desc.head_dim == 128 ? launch<128>(c, p, part, st) : launch<64>(c, p, part, st);
+}
+
+}  // namespace sdq

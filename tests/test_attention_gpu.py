@@ -60,6 +60,9 @@ CASES = {
     # prompts: more rows than one block holds
     "prompt": (H70, [70, 1, 37], [70, 50, 200], 0, 32),
     "prompt-mha": (H7, [150], [300], 0, 16),
+    "prompt-long": (H7, [500, 3], [700, 300], 0, 16),
+    "prompt-behind": ((4, 4, 64), [300, 260], [300, 700], 257, 32),
+    "prompt-short-behind": (H70, [9, 20, 5, 1], [9, 400, 5, 1], 140, 16),
     "prompt-odd": (ODD, [33, 129], [40, 129], 0, 16),
     # prefixes: alone, ending inside a page and a tile, with everything behind them
     "prefix-only": (H70, [1, 1, 1], [0, 0, 0], 77, 16),
@@ -69,6 +72,7 @@ CASES = {
     "prefix-draft": (ODD, [3, 1, 5], [3, 90, 5], 515, 128),
     "prefix-prompt": (H70, [100, 1, 20], [100, 30, 25], 150, 16),
     "prefix-many": (H70, [1] * 40, [(7 * i) % 50 for i in range(40)], 270, 32),
+    "prefix-split": (H70, [1] * 33, [(3 * i) % 20 for i in range(33)], 2900, 64),
     "prefix-64": (H125, [1] * 140, [1 + i % 9 for i in range(140)], 200, 16),
     "many": (H125, [1] * 70, [(5 * i) % 97 for i in range(70)], 0, 16),
 }
