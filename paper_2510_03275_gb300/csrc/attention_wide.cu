@@ -14,13 +14,15 @@ namespace {
 // then the sequence's own, or one of the two); the tensor cores bound it, 2 x
 // 128 x 128 x head_dim products a tile and 128 rows:
 //   warps 0-3, 4-7  rows 0-127, 128-255, a row per thread: S from tensor
-//                   memory, running maximum and sum, P (bf16) back into S's
-//                   place; O is rescaled there only when a row's maximum has
-//                   grown by more than 2^8 (weights stay below 2^8, sums in
-//                   fp32 lose nothing by it)
+//                   memory 64 keys at a time, running maximum and sum, P (bf16)
+//                   back into S's place; O is rescaled there only when a row's
+//                   maximum has grown by more than 2^8 (weights stay below
+//                   2^8, sums in fp32 lose nothing by it)
 //   warp 8          S = Q K^T (both from shared memory) and O += P V (P from
 //                   tensor memory, V as the transposed operand) on tcgen05;
-//                   while one half's softmax runs, the other half's products do
+//                   the first 64 keys' product runs while the row's thread
+//                   works on the other 64, and one half's products while the
+//                   other's softmax runs
 //   warp 9          K and V tiles, page by page, into a ring (TMA, 128-byte
 //                   swizzle); warps 10 and 11 only complete its warpgroup
 // The MMAs of a thread block run in the order of their issue, so that S of the
@@ -29,6 +31,7 @@ namespace {
 // to 224 once the third has gone down to 56 (224 + 224 + 56 = 3 x 168).
 constexpr int kWideThreads = 384;
 constexpr int kKeys = 128;             // of a tile
+constexpr int kSub = 64;               // keys of one P
 constexpr int kHalf = kKeys * 128;     // bytes: 128 rows x 64 elements
 
 template <int D> struct WideShape {
@@ -46,6 +49,45 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
         "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
         "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(taddr));
+}
+
+// Two fp32 in a 64-bit register, and arithmetic on both at once.
+__device__ __forceinline__ uint64_t pair_of(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};\n" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpair(uint64_t p, float& a, float& b) {
+  asm("mov.b64 {%0, %1}, %2;\n" : "=f"(a), "=f"(b) : "l"(p));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;\n" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;\n" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;\n" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
+__device__ __forceinline__ void st_shared16(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};\n" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+__device__ __forceinline__ uint4 ld_shared16(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  return v;
 }
 
 // Operand with its second dimension contiguous (V: keys x 64 elements per
@@ -130,7 +172,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                 const int part) {
   using S = WideShape<D>;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t full[S::kRing], empty[S::kRing], q_full, s_full[2], p_full[2], mma_done;
+  __shared__ __align__(8) uint64_t full[S::kRing], empty[S::kRing], q_full, s_full[2], p_full[2][2], pv_done[2], mma_done;
   __shared__ uint32_t tmem_base;
   const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
   const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -150,7 +192,8 @@ __global__ void __launch_bounds__(kWideThreads, 1)
     mbar_init(&q_full, 128 * halves);
     for (int i = 0; i < 2; ++i) {
       mbar_init(&s_full[i], 1);
-      mbar_init(&p_full[i], 128);
+      for (int j = 0; j < 2; ++j) mbar_init(&p_full[i][j], 128);
+      mbar_init(&pv_done[i], 1);
     }
     mbar_init(&mma_done, 1);
     fence_mbar_init();
@@ -207,6 +250,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
     } else if (warp == 8) {
       // --------------------------------------------------------- products
       constexpr uint32_t kF32Bf16 = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(128 >> 4) << 24);   // M = 128
+      // (64 keys an MMA for S would read Q twice as often: shared memory would bound it, 128 bytes a cycle)
       constexpr uint32_t qk_idesc = kF32Bf16 | ((uint32_t)(kKeys >> 3) << 17);
       constexpr uint32_t pv_idesc = kF32Bf16 | ((uint32_t)(D >> 3) << 17) | (1u << 16);   // B with its N contiguous
       auto scores = [&](int half, int st) {
@@ -228,17 +272,22 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         for (int i = 0; i < n && ok; ++i) {
           const int kn = 2 * i + 2, vs = (2 * i + 1) % S::kRing, ks = kn % S::kRing;
           for (int half = 0; half < halves && ok; ++half) {
-            ok = mbar_wait_warp(&p_full[half], i & 1);
-            if (ok && half == 0) ok = mbar_wait_warp(&full[vs], ((2 * i + 1) / S::kRing) & 1);
-            if (!ok) break;
-            tc_fence_after();
-            const uint64_t b = sw128_mn_desc(ring + vs * S::kMat);
 #pragma unroll
-            for (int k = 0; k < kKeys / 16; ++k)
-              umma_bf16_ts_warp(tmem + 256 + D * half, tmem + 128 * half + 8 * k, b + (uint64_t)(k * (2048 >> 4)), pv_idesc, (i | k) != 0);
+            for (int j = 0; j < 2; ++j) {
+              if (ok) ok = mbar_wait_warp(&p_full[half][j], i & 1);
+              if (ok && j + half == 0) ok = mbar_wait_warp(&full[vs], ((2 * i + 1) / S::kRing) & 1);
+              if (!ok) break;
+              tc_fence_after();
+              const uint64_t b = sw128_mn_desc(ring + vs * S::kMat + j * (kSub * 128));
+#pragma unroll
+              for (int k = 0; k < kSub / 16; ++k)
+                umma_bf16_ts_warp(tmem + 256 + D * half, tmem + 128 * half + kSub * j + 8 * k, b + (uint64_t)(k * (2048 >> 4)),
+                                  pv_idesc, (i | j | k) != 0);
+              if (j == 0) umma_commit_warp(&pv_done[half]);
+            }
             if (half == halves - 1) umma_commit_warp(&empty[vs]);
             if (i + 1 < n) {
-              if (half == 0) ok = mbar_wait_warp(&full[ks], (kn / S::kRing) & 1);
+              if (ok && half == 0) ok = mbar_wait_warp(&full[ks], (kn / S::kRing) & 1);
               if (!ok) break;
               tc_fence_after();
               scores(half, ks);
@@ -246,7 +295,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
             }
           }
         }
-        umma_commit_warp(&mma_done);
+      umma_commit_warp(&mma_done);
         if (!mbar_wait_warp(&mma_done, 0)) ok = false;
       }
     }
@@ -256,16 +305,15 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       // ---------------------------------------------------------- softmax
       const int half = warp >> 2, wtid = tid & 127;
       const uint32_t qb = sbase + half * S::kMat;
+#pragma unroll
       for (int i = wtid; i < 128 * (D / 8); i += 128) {
         const int r = i / (D / 8), c = i % (D / 8), row = w.r0 + 128 * half + r;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (row < w.rows) {
-          const int tok = row / p.group, g = row - tok * p.group;
-          v = __ldg(reinterpret_cast<const uint4*>(p.q + (int64_t)(w.first + tok) * p.ldq + (int64_t)(w.h * p.group + g) * D) + c);
-        }
-        const uint32_t a = qb + (uint32_t)((c >> 3) * kHalf + r * 128 + (((c & 7) ^ (r & 7)) << 4));
-        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};\n" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+        const int tok = row / p.group, g = row - tok * p.group;
+        const bool in = row < w.rows;   // (rows past the last: zeros)
+        const uint16_t* src = p.q + (int64_t)(in ? w.first + tok : 0) * p.ldq + (int64_t)(w.h * p.group + (in ? g : 0)) * D + 8 * c;
+        cp_async16(smem_raw + (qb - smem_u32(smem_raw)) + (c >> 3) * kHalf + r * 128 + (((c & 7) ^ (r & 7)) << 4), src, in ? 16 : 0);
       }
+      cp_async_wait_all();
       fence_proxy_async_smem();
       mbar_arrive(&q_full);
       const int row = w.r0 + 128 * half + wtid, tok = row / p.group, g = row - tok * p.group;
@@ -275,115 +323,145 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       const int all = w.own - w.count + (w.r0 + 128 * half) / p.group + 1;
       const uint32_t ts = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + 128 * half;
       const uint32_t to = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + 256 + D * half;
-      float m = -INFINITY, l = 0.f;   // reference maximum (log2 units) and sum
-      for (int i = 0; i < n; ++i) {
-        if (!mbar_wait_warp(&s_full[half], i & 1)) {
+      float m = -INFINITY;        // reference maximum (log2 units)
+      uint64_t l2 = 0;            // two sums
+      const uint64_t scale2 = pair_of(p.scale, p.scale);
+      for (int q = 0; q < 2 * n; ++q) {
+        const int i = q >> 1, j = q & 1;
+        if (j == 0 && !mbar_wait_warp(&s_full[half], i & 1)) {
           ok = false;
           break;
         }
         tc_fence_after();
-        uint32_t x[128];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_ld32(ts + 32 * c, x + 32 * c);
+        uint32_t x[kSub];
+        tmem_ld32(ts + kSub * j, x);
+        tmem_ld32(ts + kSub * j + 32, x + 32);
         tmem_ld_wait();
         const int t = w.t0 + i;
         const bool pre = t < w.prefix_tiles;
-        const int k0 = (pre ? t : t - w.prefix_tiles) * kKeys, keys = pre ? p.b.prefix_len : w.own;
-        if (k0 + kKeys > (pre ? keys : all)) {
-          const int see = (pre ? keys : lim) - k0;   // of this tile
+        const int k0 = (pre ? t : t - w.prefix_tiles) * kKeys + kSub * j, keys = pre ? p.b.prefix_len : w.own;
+        if (k0 + kSub > (pre ? keys : all)) {
+          const int see = (pre ? keys : lim) - k0;   // of these 64
 #pragma unroll
-          for (int j = 0; j < 128; ++j)
-            if (j >= see) x[j] = 0xFF800000u;
-          if (k0 + kKeys > keys) {
+          for (int c = 0; c < kSub; ++c)
+            if (c >= see) x[c] = 0xFF800000u;
+          if (k0 + kSub > keys) {
             // values past the last key are leftovers (perhaps NaN): zero times them has to be zero
-            const int vs = (2 * i + 1) % S::kRing;
+            const int vs = (2 * i + 1) % S::kRing, r = kSub * j + wtid;
             if (!mbar_wait_warp(&full[vs], ((2 * i + 1) / S::kRing) & 1)) {
               ok = false;
               break;
             }
-            if (k0 + wtid >= keys) {
+            if (wtid < kSub && k0 + wtid >= keys) {
 #pragma unroll
               for (int c = 0; c < D / 8; ++c)
                 asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};\n" ::"r"(
-                                 (uint32_t)(ring + vs * S::kMat + (c >> 3) * kHalf + wtid * 128 + ((c & 7) << 4))), "r"(0) : "memory");
+                                 (uint32_t)(ring + vs * S::kMat + (c >> 3) * kHalf + r * 128 + ((c & 7) << 4))), "r"(0) : "memory");
             }
             fence_proxy_async_smem();
           }
         }
         float mx[4];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) mx[c] = __uint_as_float(x[c]);
+        for (int c = 0; c < 4; ++c) mx[c] = max3(__uint_as_float(x[3 * c]), __uint_as_float(x[3 * c + 1]), __uint_as_float(x[3 * c + 2]));
 #pragma unroll
-        for (int j = 4; j < 128; ++j) mx[j & 3] = fmaxf(mx[j & 3], __uint_as_float(x[j]));
-        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale;
+        for (int c = 12; c < kSub; c += 2) mx[(c >> 1) & 3] = max3(mx[(c >> 1) & 3], __uint_as_float(x[c]), __uint_as_float(x[c + 1]));
+        const float top = max3(mx[0], mx[1], fmaxf(mx[2], mx[3])) * p.scale;
         const bool grow = top > m + 8.f;   // (also from -inf)
         if (__any_sync(0xffffffffu, grow)) {
           const float f = grow ? exp2_approx(m - top) : 1.f;
           if (grow) m = top;
-          l *= f;
-          if (i > 0) {   // (the product before this tile's scores is complete)
+          l2 = mul2(l2, pair_of(f, f));
+          if (q > 0) {   // once the products so far are in O (those of the tiles before are, with this one's S)
+            if (j == 1 && !mbar_wait_warp(&pv_done[half], i & 1)) {
+              ok = false;
+              break;
+            }
+            tc_fence_after();
 #pragma unroll
             for (int c = 0; c < D / 32; ++c) {
               uint32_t o[32];
               tmem_ld32(to + 32 * c, o);
               tmem_ld_wait();
 #pragma unroll
-              for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+              for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
               tmem_st32(to + 32 * c, o);
             }
           }
         }
         const float neg = m == -INFINITY ? 0.f : -m;
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        const uint64_t neg2 = pair_of(neg, neg);
+        uint64_t sum[2] = {0, 0};
+        uint32_t e[kSub / 2];
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          uint32_t e[32];
-#pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            const float a = exp2_approx(fmaf(__uint_as_float(x[64 * c + 2 * j]), p.scale, neg));
-            const float b = exp2_approx(fmaf(__uint_as_float(x[64 * c + 2 * j + 1]), p.scale, neg));
-            sum[2 * (j & 1)] += a;
-            sum[2 * (j & 1) + 1] += b;
-            e[j] = pack_bf16x2(a, b);
-          }
-          tmem_st32(ts + 32 * c, e);
+        for (int c = 0; c < kSub / 2; ++c) {
+          float a, b;
+          unpair(fma2(pair_of(__uint_as_float(x[2 * c]), __uint_as_float(x[2 * c + 1])), scale2, neg2), a, b);
+          a = exp2_approx(a);
+          b = exp2_approx(b);
+          sum[c & 1] = add2(sum[c & 1], pair_of(a, b));
+          e[c] = pack_bf16x2(a, b);
         }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        tmem_st32(ts + kSub * j, e);
+        l2 = add2(l2, add2(sum[0], sum[1]));
         tmem_st_wait();
         tc_fence_before();
-        mbar_arrive(&p_full[half]);
+        mbar_arrive(&p_full[half][j]);
       }
+      float l, lb;
+      unpair(l2, l, lb);
+      l += lb;
       // ------------------------------------------------------------- out
       if (n > 0 && ok) ok = mbar_wait_warp(&mma_done, 0);
       tc_fence_after();
       if (ok) {
+        // rows to memory over the place of Q, which nothing reads any more: a
+        // thread's row would go out in 16-byte pieces, 32 rows at a time
         const int64_t at = (int64_t)(w.first + tok) * p.q_heads + w.h * p.group + g;
         const int64_t rows = (int64_t)p.b.n_tokens * p.q_heads, pr = w.split * rows + at;
         const float k = p.direct ? (l > 0.f ? 1.f / l : l) : 1.f;   // (0 where nothing is seen; NaN stays)
+        constexpr int kChunks = D / 8;                             // 16-byte pieces of a row: D bf16, or half as many fp32
+        const uint32_t stage = qb + (uint32_t)(32 * (warp & 3) * 2 * D);
+        const uint32_t mine = stage + (uint32_t)(lane * 2 * D);
+        const uint32_t lives = __ballot_sync(0xffffffffu, live);
+        uint8_t* base = p.direct ? reinterpret_cast<uint8_t*>(p.out) : reinterpret_cast<uint8_t*>(p.o[part]);
+        const int64_t row_at = p.direct ? at * (2 * D) : pr * (4 * D);   // bytes
+        for (int pass = 0; pass < (p.direct ? 1 : 2); ++pass) {
+          if (!p.direct && n == 0) break;
 #pragma unroll
-        for (int c = 0; c < D / 32; ++c) {
-          uint32_t o[32];
-          if (n > 0) {
-            tmem_ld32(to + 32 * c, o);
-            tmem_ld_wait();
-          } else {
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t o[32];
+            if (!p.direct && c >= D / 64) break;
+            const int col = p.direct ? 32 * c : pass * (D / 2) + 32 * c;
+            if (n > 0) {
+              tmem_ld32(to + col, o);
+              tmem_ld_wait();
+            } else {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) o[j] = 0;
-          }
-          if (live && p.direct) {
-#pragma unroll
-            for (int j = 0; j < 32; j += 8) {
-              uint4 v;
-              v.x = pack_bf16x2(__uint_as_float(o[j]) * k, __uint_as_float(o[j + 1]) * k);
-              v.y = pack_bf16x2(__uint_as_float(o[j + 2]) * k, __uint_as_float(o[j + 3]) * k);
-              v.z = pack_bf16x2(__uint_as_float(o[j + 4]) * k, __uint_as_float(o[j + 5]) * k);
-              v.w = pack_bf16x2(__uint_as_float(o[j + 6]) * k, __uint_as_float(o[j + 7]) * k);
-              *reinterpret_cast<uint4*>(p.out + at * D + 32 * c + j) = v;
+              for (int j = 0; j < 32; ++j) o[j] = 0;
             }
-          } else if (live && n > 0) {
+            if (p.direct) {
 #pragma unroll
-            for (int j = 0; j < 32; j += 4)
-              *reinterpret_cast<uint4*>(p.o[part] + pr * D + 32 * c + j) = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+              for (int j = 0; j < 4; ++j) {
+                const uint32_t v0 = pack_bf16x2(__uint_as_float(o[8 * j]) * k, __uint_as_float(o[8 * j + 1]) * k);
+                const uint32_t v1 = pack_bf16x2(__uint_as_float(o[8 * j + 2]) * k, __uint_as_float(o[8 * j + 3]) * k);
+                const uint32_t v2 = pack_bf16x2(__uint_as_float(o[8 * j + 4]) * k, __uint_as_float(o[8 * j + 5]) * k);
+                const uint32_t v3 = pack_bf16x2(__uint_as_float(o[8 * j + 6]) * k, __uint_as_float(o[8 * j + 7]) * k);
+                st_shared16(mine + (((4 * c + j) ^ (lane & 7)) << 4), v0, v1, v2, v3);
+              }
+            } else {
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+                st_shared16(mine + (((8 * c + j) ^ (lane & 7)) << 4), o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+            }
+          }
+          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < kChunks; ++i) {
+            const int r = (32 / kChunks) * i + lane / kChunks, c = lane % kChunks;
+            const int64_t off = __shfl_sync(0xffffffffu, row_at, r);
+            const uint4 v = ld_shared16(stage + (uint32_t)(r * 2 * D) + ((c ^ (r & 7)) << 4));
+            if (lives >> r & 1) *reinterpret_cast<uint4*>(base + off + pass * (2 * D) + 16 * c) = v;
           }
           __syncwarp();
         }
