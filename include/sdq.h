@@ -485,7 +485,8 @@ int sdq_cache_append(sdq_cache cache, const sdq_batch* batch, int32_t q_heads, c
  * tokens of the same call it may too (their weight is 0, and 0 times it is
  * not); free places of a page may hold anything.
  * sdq_attention_workspace_bytes: for a batch of these integers (the device
- * arrays are not read); grows with each of them; 0 on invalid input.  The
+ * arrays are not read; a smaller batch may need more, as it splits the keys
+ * further); 0 on invalid input.  The
  * workspace needs no initialization and may serve any calls in turn.
  * Errors: INVALID_ARG (also when the current device is not the cache's),
  * WORKSPACE, CUDA. */

@@ -605,7 +605,7 @@ class KVCache:
         return out
 
     def alloc_workspace(self, batch: Batch, q_heads: int):
-        """For ``attend`` on this batch, and on any whose integers are no larger."""
+        """For ``attend`` on this batch (or one of the same integers)."""
         import torch
         n = sdq_attention_workspace_bytes(self.handle, batch, q_heads)
         if n == 0:

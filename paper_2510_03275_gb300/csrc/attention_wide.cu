@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
             }
           }
         }
-      umma_commit_warp(&mma_done);
+        umma_commit_warp(&mma_done);
         if (!mbar_wait_warp(&mma_done, 0)) ok = false;
       }
     }
@@ -466,7 +466,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
           __syncwarp();
         }
         if (live) {
-          if (!p.direct) p.ml[part][pr] = make_float2(m, l);
+          if (!p.direct) p.ml[part][pr] = make_float2(l == l ? m : l, l);   // (NaN scores leave no maximum)
           else if (p.lse) p.lse[at] = m == -INFINITY ? m : (m + log2_approx(l)) * 0.69314718056f;
         }
       }

@@ -151,16 +151,20 @@ extern "C" int sdq_cache_create(const sdq_cache_desc* desc, uint16_t* k_pages, u
   c->k = k_pages;
   c->v = v_pages;
   c->rows = (int64_t)desc->n_pages * desc->kv_heads * desc->page_tokens;
-  const cuuint64_t dims[2] = {(cuuint64_t)desc->head_dim, (cuuint64_t)c->rows};
-  const cuuint64_t strides[1] = {(cuuint64_t)desc->head_dim * 2};
-  const cuuint32_t box[2] = {64, (cuuint32_t)cache_box_rows(*desc)}, estr[2] = {1, 1};
-  for (int i = 0; i < 2; ++i)
-    if (enc(i ? &c->vmap : &c->kmap, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, i ? v_pages : k_pages, dims, strides, box, estr,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+  const cuuint64_t row = (cuuint64_t)desc->head_dim * 2, halves = (cuuint64_t)desc->head_dim / 64;
+  const cuuint64_t dims[3] = {(cuuint64_t)desc->head_dim, (cuuint64_t)c->rows, 0}, tdims[3] = {64, (cuuint64_t)c->rows, halves};
+  const cuuint64_t strides[2] = {row, 128};
+  const cuuint32_t box[2] = {64, (cuuint32_t)cache_box_rows(*desc)}, tbox[3] = {64, 16, (cuuint32_t)halves}, estr[3] = {1, 1, 1};
+  for (int i = 0; i < 4; ++i) {
+    const bool tile = i >= 2;
+    CUtensorMap* map = i == 0 ? &c->kmap : i == 1 ? &c->vmap : i == 2 ? &c->ktile : &c->vtile;
+    if (enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, tile ? 3 : 2, i & 1 ? v_pages : k_pages, tile ? tdims : dims, strides,
+            tile ? tbox : box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) {
       delete c;
       return SDQ_ERR_CUDA;
     }
+  }
   *out = c;
   return SDQ_OK;
 }

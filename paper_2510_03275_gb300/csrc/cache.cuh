@@ -8,7 +8,8 @@ struct sdq_cache_s {
   int device, sm_count;
   uint16_t *k, *v;
   int64_t rows;          // token rows of each array: n_pages * kv_heads * page_tokens
-  CUtensorMap kmap, vmap;   // rows x head_dim in boxes of min(page_tokens, 64) rows x 64 elements, 128-byte swizzle
+  CUtensorMap kmap, vmap;     // rows x head_dim in boxes of min(page_tokens, 64) rows x 64 elements, 128-byte swizzle
+  CUtensorMap ktile, vtile;   // 64 elements x rows x halves of a row in boxes of 16 rows, all of their elements
 };
 
 namespace sdq {

@@ -205,6 +205,36 @@ def test_pages_outside_the_cache_read_as_zeros(sdq):
     _check(zero, out, lse)
 
 
+@pytest.mark.parametrize("new,prefix", [(1, 0), (1, 200), (1, 3000), (2, 40), (40, 0), (40, 200)])
+@pytest.mark.parametrize("where", ["own", "prefix", "query"])
+def test_nan_reaches_the_rows_that_see_it(sdq, new, prefix, where):
+    """A NaN key reaches the tokens that see it, all of its sequence's for the oldest own key, every one's for a
+    prefix's; a NaN query its own head; other rows keep their values."""
+    import torch
+    if where == "prefix" and prefix == 0:
+        pytest.skip("no prefix")
+    for dim_heads in (H70, H125):
+        c = Case(dim_heads, [new, new, new], [new + 70, new + 33, 700 + new], prefix, 16, seed=41)
+        clean = Case(dim_heads, [new, new, new], [new + 70, new + 33, 700 + new], prefix, 16, seed=41)
+        bad = np.zeros((c.tokens, c.q_heads), bool)
+        group = c.q_heads // c.kv_heads
+        if where == "own":
+            c.k[c.pages[1, 0], 0, 0] = np.nan
+            bad[new:2 * new, :group] = True
+        elif where == "prefix":
+            c.k[c.prefix_pages[0], 1, 3] = np.nan
+            bad[:, group:2 * group] = True
+        else:
+            c.q[new, 1] = np.nan
+            bad[new, 1] = True
+        out, _ = _run(sdq, torch, c)
+        want, _ = _run(sdq, torch, clean)
+        nan = torch.isnan(out).any(-1).cpu().numpy()
+        assert np.array_equal(nan, bad)
+        good = torch.from_numpy(~bad).cuda()
+        assert torch.equal(out[good], want[good])
+
+
 def test_lengths_beyond_the_bounds_are_cut(sdq):
     import torch
     c = Case(H70, [1], [90], 0, 16, seed=31)
