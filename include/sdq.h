@@ -417,7 +417,8 @@ int sdq_cache_destroy(sdq_cache cache);
  * captured graph follows their contents; the integers are fixed at the call:
  * max_new and max_own are upper bounds of the new and own tokens of any
  * sequence (what lies beyond them is ignored), max_own <= page_stride *
- * page_tokens.  token_start must not decrease, from 0 to n_tokens.  A page
+ * page_tokens, and (max_own or prefix_len, + 64) * kv_heads < 2^31.
+ * token_start must not decrease, from 0 to n_tokens.  A page
  * index outside the cache is not followed: nothing is written there, and it
  * reads as zeros. */
 typedef struct {

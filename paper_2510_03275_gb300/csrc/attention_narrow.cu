@@ -24,6 +24,10 @@ namespace {
 // P is rounded to bf16 for its product (relative 2^-8 at most per weight, as
 // the values themselves carry); sums, maxima and outputs are fp32.
 constexpr int kWarps = 8, kThreads = 32 * kWarps, kTile = 16;
+// A (sequence, head) takes as many places of the line as it has tiles, and
+// kUnitCost more: its queries, its output and the join cost its warp about as
+// much time as that many tiles.
+constexpr int kUnitCost = 2;
 
 template <int D, int NT> struct NarrowShape {
   static constexpr int kRows = 8 * NT;
@@ -60,7 +64,7 @@ struct Unit {
   int s, h;                  // sequence (-1: the batch)
   int first, rows, keys, count;
   int tiles;
-  int64_t a;                 // its first tile of the line
+  int64_t a;                 // its first place in the line (its tiles', then kUnitCost more)
 };
 
 // The line of units that have tiles.  All of it by whole warps: a lane holds
@@ -79,14 +83,16 @@ struct Walk {
     if (s < p.b.n_seqs) held = seq_span(p.b, s);
   }
   __device__ static int tiles_of(const SeqSpan& q) { return q.count > 0 ? (q.own + kTile - 1) / kTile : 0; }   // per key head
-  // All tiles.
+  __device__ static int places_of(int tiles) { return tiles > 0 ? tiles + kUnitCost : 0; }
+  // All places.
   __device__ int64_t total() {
-    if (part == kPrefix) return (int64_t)p.kv_heads * ((p.b.prefix_len + kTile - 1) / kTile);
+    if (part == kPrefix) return (int64_t)p.kv_heads * places_of((p.b.prefix_len + kTile - 1) / kTile);
     int64_t n = 0;
     for (int s0 = (p.b.n_seqs - 1) & ~31; s0 >= 0; s0 -= 32) {   // (the first 32 last: a search begins there)
       hold(s0);
-      n += tiles_of(held);
+      n += places_of(tiles_of(held));
     }
+    if (p.b.n_seqs == 1) return __shfl_sync(0xffffffffu, n, 0) * p.kv_heads;
     for (int d = 16; d; d >>= 1) n += __shfl_xor_sync(0xffffffffu, n, d);
     return n * p.kv_heads;
   }
@@ -99,7 +105,7 @@ struct Walk {
     u.rows = u.count * p.group;
     u.tiles = tiles_of(SeqSpan{u.first, u.count, u.keys});
   }
-  // The unit of tile t, which is below total().
+  // The unit of place t, which is below total().
   __device__ Unit find(int64_t t) {
     Unit u;
     if (part == kPrefix) {
@@ -109,17 +115,17 @@ struct Walk {
       u.rows = p.b.n_tokens * p.group;
       u.keys = p.b.prefix_len;
       u.tiles = (p.b.prefix_len + kTile - 1) / kTile;
-      u.h = (int)(t / u.tiles);
-      u.a = (int64_t)u.h * u.tiles;
+      u.h = (int)((uint32_t)t / (uint32_t)places_of(u.tiles));   // (kv_heads times the places of a head: below 2^31, as below)
+      u.a = (int64_t)u.h * places_of(u.tiles);
       return u;
     }
     int64_t before = 0;
     for (int s0 = 0; s0 < p.b.n_seqs; s0 += 32) {
       const int lane = threadIdx.x & 31;
       hold(s0);
-      const int64_t n = (int64_t)tiles_of(held) * p.kv_heads;
+      const int64_t n = (int64_t)places_of(tiles_of(held)) * p.kv_heads;
       int64_t end = n;
-      for (int d = 1; d < 32; d <<= 1) {
+      for (int d = 1; d < 32 && s0 + d < p.b.n_seqs; d <<= 1) {
         const int64_t o = __shfl_up_sync(0xffffffffu, end, d);
         if (lane >= d) end += o;
       }
@@ -128,8 +134,9 @@ struct Walk {
         const int l = __ffs(past) - 1;
         const int64_t a = before + __shfl_sync(0xffffffffu, end - n, l);
         enter(u, s0 + l);
-        u.h = (int)((t - a) / u.tiles);
-        u.a = a + (int64_t)u.h * u.tiles;
+        // (a sequence's keys of all heads are fewer than 2^31: check_batch)
+        u.h = (int)((uint32_t)(t - a) / (uint32_t)places_of(u.tiles));
+        u.a = a + (int64_t)u.h * places_of(u.tiles);
         return u;
       }
       before += __shfl_sync(0xffffffffu, end, 31);
@@ -141,7 +148,7 @@ struct Walk {
   }
   // The next unit with tiles (there is one).
   __device__ void next(Unit& u) {
-    u.a += u.tiles;
+    u.a += places_of(u.tiles);
     if (++u.h < p.kv_heads || part == kPrefix) return;
     u.h = 0;
     for (int s = u.s + 1; s < p.b.n_seqs; ++s) {
@@ -161,11 +168,13 @@ __device__ __forceinline__ int piece_at(int r, int d) {
 
 // Pieces e of a thread block: 2 w the unit that warp w's share ends, 2 w + 1
 // the last of its share, 2 kWarps + w a whole unit of it (8 rows at a time).
+// open: the units that lie in other thread blocks too, the one from before
+// (0) and the one that goes on (1).
 constexpr int kPieces = 3 * kWarps;
 template <int NT> struct Pieces {
   float m[kPieces][8 * NT], l[kPieces][8 * NT];
-  Unit unit[kPieces];
-  int set[kPieces];
+  Unit open[2];
+  int is_open[2];
 };
 
 // What is joined: pieces e0 .. e1 - 1 of this thread block, or parts first ..
@@ -297,7 +306,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int i = 0; i < ST; ++i) mbar_init(&full[w][i], 1);
     fence_mbar_init();
   }
-  if (tid < kPieces) pc.set[tid] = 0;
+  if (tid < 2) pc.is_open[tid] = 0;
   static_assert(sizeof(AttendParams) % 4 == 0 && sizeof(AttendParams) / 4 <= kThreads, "copied a word per thread");
   if (tid < (int)(sizeof(AttendParams) / 4)) reinterpret_cast<uint32_t*>(&sp)[tid] = reinterpret_cast<const uint32_t*>(&p)[tid];
   __syncthreads();
@@ -314,17 +323,20 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t ring_a = sbase + warp * S::kRing;
   float* scratch = reinterpret_cast<float*>(smem + kWarps * S::kRing + warp * S::kScratch);
   bool ok = true, waited = !late;
+  Unit head, tail;   // units whose pieces this warp joins: one that ends here, one that goes on behind this share
+  bool head_set = false, tail_set = false;
   if (t0 < t1) {
     Unit u = walk.find(t0), ui = u;
-    const int nk = (int)min(t1 - t0, (int64_t)0x7FFFFFFF);
-    // ---- copies: tile ti of unit ui is the next; `page` of tile pb + lane of sequence ps
+    // ---- copies: tile ti of unit ui is the next, if it is one of this share's; `page` of tile pb + lane of sequence ps
     int ti = (int)(t0 - u.a), ki = 0, pb = 0, ps = -2, page = -1;
     const int per_page = p.page_shift - 4;   // log2 of tiles per page
     auto issue = [&]() {
-      if (ti == ui.tiles) {
+      if (ti >= ui.tiles) {
+        if (ui.a + Walk::places_of(ui.tiles) >= t1) return;
         walk.next(ui);
         ti = 0;
       }
+      if (ui.a + ti >= t1) return;
       if (ui.s != ps || ti < pb || ti >= pb + 32) {
         ps = ui.s;
         pb = ti;
@@ -342,11 +354,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       ++ti;
       ++ki;
     };
-    while (ki < min(ST, nk)) issue();
+#pragma unroll 1
+    for (int i = 0; i < ST; ++i) issue();
     const int g8 = lane >> 2, c2 = 2 * (lane & 3);
     int k = 0;
-    while (k < nk) {
-      const int lo = (int)(max(u.a, t0) - u.a), hi = (int)(min(u.a + u.tiles, t1) - u.a);
+    for (; u.a < t1; walk.next(u)) {
+      const int lo = (int)(max(u.a, t0) - u.a), hi = (int)min((int64_t)u.tiles, t1 - u.a);
+      if (lo < hi) {
       // query rows as the products' B operand; rows past the last are zero
       uint32_t qf[NT][D / 16][2];
       int lim[NT][2];   // keys that this lane's two queries of each 8 see
@@ -453,7 +467,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int n = 0; n < NT; ++n) mma_bf16_16816(o[n][d], a, pf[n][0], pf[n][1]);
         }
         __syncwarp();   // every lane has read the stage
-        if (ki < nk) issue();
+        issue();
       }
       if (!ok) break;
       // ---- the end of the unit, or of the share
@@ -463,24 +477,47 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int j = 0; j < 2; ++j)
 #pragma unroll
           for (int d = 4; d < 32; d <<= 1) l[n][j] += __shfl_xor_sync(0xffffffffu, l[n][j], d);
-      const bool starts = u.a >= t0, ends = u.a + u.tiles <= t1;
+      const bool starts = lo == 0, ends = hi == u.tiles;
       if (ends && !waited) {   // (results of the prefix; and the workspace's pieces may still be read)
         pdl_wait();
         waited = true;
       }
+      const bool whole = starts && ends;
+      if (whole && p.parts == 1) {
+        // a whole unit, nothing to join: O^T is turned by movmatrix as P was, a row's 4 lanes write 16 bytes at a time
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          float inv[2];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) inv[j] = l[n][j] > 0.f ? 1.f / l[n][j] : l[n][j];   // (0 where nothing is seen; NaN stays)
+          const int r = 8 * n + g8, tok = r / p.group;
+          const int64_t row = (int64_t)(u.first + tok) * p.q_heads + u.h * p.group + r - tok * p.group;
+#pragma unroll
+          for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const uint32_t v = movmatrix(pack_bf16x2(o[n][d][2 * j] * inv[0], o[n][d][2 * j + 1] * inv[1]));
+              if (r < u.rows) *reinterpret_cast<uint32_t*>(p.out + row * D + 16 * d + 8 * j + c2) = v;
+            }
+          if (p.lse && g8 == 0)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const int rj = 8 * n + c2 + j, tj = rj / p.group;
+              if (rj < u.rows)
+                p.lse[(int64_t)(u.first + tj) * p.q_heads + u.h * p.group + rj - tj * p.group] =
+                    m[n][j] == -INFINITY && l[n][j] == l[n][j] ? m[n][j] : (m[n][j] + log2_approx(l[n][j])) * 0.69314718056f;
+            }
+        }
+        continue;
+      }
       // a whole unit leaves 8 rows at a time through the scratch; a piece of the
       // unit that ends here goes into the workspace (the ring is in use), the
       // last one into the ring, whose copies are all read
-      const bool whole = starts && ends;
       const int e = whole ? 2 * kWarps + warp : 2 * warp + (ends ? 0 : 1);
       float* dst = whole  ? scratch
                    : ends ? p.warp_o + ((int64_t)blockIdx.x * kWarps + warp) * (R * D)
                           : reinterpret_cast<float*>(ring);
       __syncwarp();
-      if (lane == 0) {
-        pc.unit[e] = u;
-        pc.set[e] = 1;
-      }
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         const int at = whole ? 0 : 8 * n;
@@ -501,7 +538,17 @@ __global__ void __launch_bounds__(kThreads, 1)
           __syncwarp();
         }
       }
-      if (ends && k < nk) walk.next(u);
+      if (!whole) {
+        // the first warp of the thread block that has pieces of the unit joins them below
+        if (ends) {
+          if (warp == 0) head = u;
+          head_set = warp == 0;
+        } else if (starts || warp == 0) {
+          tail = u;
+          tail_set = true;
+        }
+      }
+      }
     }
     // the copies in flight have landed before the thread block ends
     if (!ok)
@@ -513,34 +560,31 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int64_t ct0 = (int64_t)blockIdx.x * kWarps * share, ct1 = min(total, ct0 + kWarps * share);
   const int64_t block_share = kWarps * share;
   if (all_ok) {
-    // each unit with pieces here: a warp per 8 rows.  Units that lie in other
-    // thread blocks too (at most the one from before and the one that goes
-    // on) are kept as parts
-    int open0 = -1, open1 = -1, turn = 0;
-    for (int e0 = 0; e0 < 2 * kWarps;) {
-      if (!pc.set[e0]) {
-        ++e0;
-        continue;
-      }
-      const Unit& u = pc.unit[e0];
-      int e1 = e0 + 1;
-      while (e1 < 2 * kWarps && (!pc.set[e1] || pc.unit[e1].a == u.a)) ++e1;
-      while (!pc.set[e1 - 1]) --e1;
-      const bool before = u.a < ct0, after = u.a + u.tiles > ct1;
-      if (before) open0 = e0;
-      else if (after) open1 = e0;
+    // the units with pieces here, each by one warp.  Those that lie in other
+    // thread blocks too are kept as parts
+    if (head_set)
+      for (int n = 0; n < NT; ++n) finish<D, NT, D / 16>(sp, pc, smem, part, head, n, Source{0, 1, 0, 0}, 2 * (int64_t)blockIdx.x, 0);
+    if (tail_set) {
+      const bool before = tail.a < ct0, after = tail.a + tail.tiles > ct1;
+      const int last = after ? kWarps - 1 : (int)((tail.a + tail.tiles - 1 - ct0) / share);   // the last warp with tiles of it
+      const Source src{2 * warp + 1, after ? 2 * kWarps : 2 * last + 1, 0, 0};
       const int64_t slot = before || after ? 2 * (int64_t)blockIdx.x + (before ? 0 : 1) : -1;
-      for (int n = 0; n < NT; ++n, ++turn)
-        if (turn % kWarps == warp) finish<D, NT, D / 16>(sp, pc, smem, part, u, n, Source{e0, e1, 0, 0}, slot, 0);
-      e0 = e1;
+      for (int n = 0; n < NT; ++n) finish<D, NT, D / 16>(sp, pc, smem, part, tail, n, src, slot, 0);
+      if (slot >= 0 && lane == 0) {
+        pc.open[before ? 0 : 1] = tail;
+        pc.is_open[before ? 0 : 1] = 1;
+      }
     }
-    if (open0 >= 0 || open1 >= 0) {
-      __syncthreads();
+    if (head_set && lane == 0) {
+      pc.open[0] = head;
+      pc.is_open[0] = 1;
+    }
+    __syncthreads();
+    if (pc.is_open[0] | pc.is_open[1]) {
       if (tid < 2) {
         arrived[tid] = 0;
-        const int e = tid == 0 ? open0 : open1;
-        if (e >= 0) {
-          const Unit& u = pc.unit[e];
+        if (pc.is_open[tid]) {
+          const Unit& u = pc.open[tid];
           const uint32_t n = (uint32_t)((u.a + u.tiles - 1) / block_share - u.a / block_share + 1);
           uint64_t* tk = p.tickets[part] + (part == kPrefix ? u.h : (int64_t)u.s * p.kv_heads + u.h);
           const uint32_t got = ticket_take(tk, p.call, n);
@@ -552,7 +596,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int i = 0; i < 2; ++i) {
         if (!arrived[i]) continue;
         // the last to arrive: all thread blocks' parts, a chunk group a warp
-        const Unit& u = pc.unit[i == 0 ? open0 : open1];
+        const Unit& u = pc.open[i];
         const int first = (int)(u.a / block_share), n = (int)((u.a + u.tiles - 1) / block_share) - first + 1;
         constexpr int kPer = kWarps / (D / 16);   // warps on a chunk group, each of its own rows
         for (int m = warp % kPer; m < NT; m += kPer)

@@ -116,6 +116,7 @@ int check_batch(const sdq_cache_s* c, const sdq_batch* b, int32_t q_heads) {
   if ((int64_t)b->n_tokens * q_heads >= (1ll << 31)) return SDQ_ERR_INVALID_ARG;
   if (b->max_new < 1 || b->max_new > b->n_tokens || b->max_own < 0 || b->max_own >= (1 << 30)) return SDQ_ERR_INVALID_ARG;
   if (b->page_stride < 0 || b->max_own > (int64_t)b->page_stride * c->desc.page_tokens) return SDQ_ERR_INVALID_ARG;
+  if (((int64_t)std::max(b->max_own, b->prefix_len) + 64) * c->desc.kv_heads >= (1ll << 31)) return SDQ_ERR_INVALID_ARG;
   if (b->prefix_len < 0 || b->prefix_len >= (1 << 30) || (b->prefix_len > 0 && !b->prefix_pages)) return SDQ_ERR_INVALID_ARG;
   return SDQ_OK;
 }
