@@ -1,5 +1,5 @@
-// Attention over the paged cache: the join of partial results and the host
-// side (include/sdq.h).
+// Attention over the paged cache: which kernel takes what, the workspace, the
+// entry points (include/sdq.h).
 #include <algorithm>
 #include <cmath>
 
@@ -9,8 +9,7 @@ namespace sdq {
 
 namespace {
 
-// One warp per row: the sum of the partial results that the wide kernel left
-// of both parts.
+// One warp per row: the prefix's result and the own part's.
 template <int D>
 __global__ void __launch_bounds__(256) join_kernel(const AttendParams p) {
   pdl_wait();
@@ -18,41 +17,66 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendParams p) {
   constexpr int V = D / 32;
   const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
   if (row >= (int64_t)p.b.n_tokens * p.q_heads) return;
+  // (a token that no sequence counts as its own has no own result: seq_span)
   const int tok = (int)(row / p.q_heads);
   const SeqSpan q = seq_span(p.b, seq_of_token(p.b.token_start, p.b.n_seqs, tok));
-  const bool own = tok < q.first + q.count && (p.chained || q.own > 0);   // its part was computed
-  float acc[V], top = -INFINITY, sum = 0.f;
+  float2 ml[2];
+  float v[2][V], acc[V], sum = 0.f;
 #pragma unroll
-  for (int i = 0; i < V; ++i) acc[i] = 0.f;
-  join_rows<D, V>(p, kPrefix, row, p.splits[kPrefix], acc, top, sum);
-  if (own) join_rows<D, V>(p, kOwn, row, p.splits[kOwn], acc, top, sum);
+  for (int i = 0; i < 2; ++i) {
+    ml[i] = __ldcg(p.ml[i] + row);
+    load_row<D, V>(p.o[i] + row * D, v[i]);
+  }
+  if (tok >= q.first + q.count) ml[kOwn] = make_float2(-INFINITY, 0.f);
+  const float top = fmaxf(ml[0].x, ml[1].x), base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+  for (int k = 0; k < V; ++k) acc[k] = 0.f;
+#pragma unroll
+  for (int i = kPrefix; i >= kOwn; --i) {
+    const float f = exp2_approx(ml[i].x - base);
+    if (f == 0.f) continue;   // (a part that saw nothing holds anything)
+    sum += ml[i].y * f;
+#pragma unroll
+    for (int k = 0; k < V; ++k) acc[k] += f * v[i][k];
+  }
   write_row<D, V>(p, row, acc, top, sum);
 }
 
 // ------------------------------------------------------------------- host
-// The wide kernel takes the parts with more rows per key head than the narrow
-// one's registers hold.  Where a sequence brings 128 rows and more on the
-// average, its row blocks run over the prefix and its own keys in one line;
-// below that the batch's rows share blocks against the prefix.
+// A prefix's rows go to the wide kernel from 9 on (16 rows of 32 heads against
+// 2051 keys: 25 us on the narrow one, whose warps then hold 16 rows each and
+// spend more on them than on the keys), a sequence's from 33 on, since the wide
+// kernel takes a thread block for every 256 of them, or fewer.  Where a sequence
+// brings 128 rows and more on the average, its row blocks run over the prefix
+// and its own keys in one line; below that the batch's rows share blocks against
+// the prefix, and the two parts' results are joined.
+constexpr int kPrefixNarrowRows = 8;
+
 void set_route(const sdq_cache_s* c, const sdq_batch* b, int q_heads, AttendParams* p) {
   const int group = q_heads / c->desc.kv_heads;
   const int64_t own_rows = b->max_own > 0 ? (int64_t)b->max_new * group : 0;
   const int64_t prefix_rows = b->prefix_len > 0 ? (int64_t)b->n_tokens * group : 0;
   const bool own_wide = own_rows > kNarrowRows;
+  p->b = *b;
+  p->group = group;
   p->chained = own_wide && prefix_rows > 0 && prefix_rows >= 128ll * b->n_seqs;
   p->wide[kOwn] = own_wide;
   // (a call without any keys goes through the narrow kernel too: it writes the zeros)
   p->narrow[kOwn] = !own_wide && (own_rows > 0 || prefix_rows == 0);
-  p->wide[kPrefix] = prefix_rows > kNarrowRows && !p->chained;
-  p->narrow[kPrefix] = prefix_rows > 0 && prefix_rows <= kNarrowRows;
+  p->wide[kPrefix] = prefix_rows > kPrefixNarrowRows && !p->chained;
+  p->narrow[kPrefix] = prefix_rows > 0 && prefix_rows <= kPrefixNarrowRows;
   p->parts = p->wide[kOwn] + p->narrow[kOwn] + p->wide[kPrefix] + p->narrow[kPrefix];
-  for (int part = 0; part < 2; ++part)
+  for (int part = 0; part < 2; ++part) {
     p->splits[part] = p->wide[part] ? wide_splits(c, b, q_heads, part, p->chained) : 0;
-  if (p->narrow[kPrefix] && p->parts > 1) p->splits[kPrefix] = 1;
-  p->direct = p->parts == 1 && p->splits[kOwn] <= 1 && p->splits[kPrefix] <= 1;
+  }
   p->ctas = c->sm_count;
-  p->b = *b;
-  p->group = group;
+  // Beside a wide kernel that leaves SMs free, the narrow one's first thread
+  // blocks start at once and the others as the wide kernel's end: the first
+  // take ahead what they can read until then (40 bytes a ns and SM).
+  if (p->wide[kPrefix] && p->narrow[kOwn]) {
+    p->early = c->sm_count - (int)std::min<int64_t>(wide_grid(c, *p, kPrefix), c->sm_count);
+    p->ahead = (int)(wide_time(c, b, q_heads, kPrefix, false, p->splits[kPrefix]) * 40e3 / (64.0 * c->desc.head_dim * narrow_warps()));
+  }
 }
 
 AttendWs attend_workspace(const sdq_cache_s* c, const sdq_batch* b, int q_heads, const AttendParams& p) {
@@ -68,32 +92,33 @@ AttendWs attend_workspace(const sdq_cache_s* c, const sdq_batch* b, int q_heads,
   L.tickets[kOwn] = take(p.narrow[kOwn] ? sizeof(uint64_t) * b->n_seqs * c->desc.kv_heads : 0);
   L.tickets[kPrefix] = take(p.narrow[kPrefix] ? sizeof(uint64_t) * c->desc.kv_heads : 0);
   for (int part = 0; part < 2; ++part) {
-    L.ml[part] = take(sizeof(float2) * p.splits[part] * rows);
-    L.o[part] = take(sizeof(float) * p.splits[part] * rows * d);
+    L.ml[part] = take(p.parts > 1 ? sizeof(float2) * rows : 0);
+    L.o[part] = take(p.parts > 1 ? sizeof(float) * rows * d : 0);
+    L.split_ml[part] = take(p.splits[part] > 1 ? sizeof(float2) * p.splits[part] * rows : 0);
+    L.split_o[part] = take(p.splits[part] > 1 ? sizeof(float) * p.splits[part] * rows * d : 0);
+    const size_t slots = p.narrow[part] ? (size_t)p.ctas * 8 * narrow_groups(b, p.group, part) : 0;
+    L.warp_o[part] = take(sizeof(float) * slots * narrow_warps() * d);
+    L.block_ml[part] = take(sizeof(float2) * 2 * slots);
+    L.block_o[part] = take(sizeof(float) * 2 * slots * d);
   }
-  // (as for the largest row blocks: the size grows with the batch)
-  const size_t blocks = p.narrow[kOwn] || p.narrow[kPrefix] ? (size_t)p.ctas * kNarrowRows : 0;
-  L.warp_o = take(sizeof(float) * blocks * narrow_warps() * d);
-  L.block_ml = take(sizeof(float2) * 2 * blocks);
-  L.block_o = take(sizeof(float) * 2 * blocks * d);
   L.total = off;
   return L;
 }
 
 template <int D>
-cudaError_t launch_parts(const sdq_cache_s* c, const AttendParams& p, cudaStream_t st) {
-  bool late = false;
-  for (int part = kPrefix; part >= kOwn; --part) {
-    cudaError_t e = cudaSuccess;
-    if (p.wide[part]) e = launch_wide(c, p, part, st);
-    else if (p.narrow[part]) e = launch_narrow(c, p, part, late, st);
-    if (e != cudaSuccess) return e;
-    late = p.wide[part] || p.narrow[part];
-  }
-  // the narrow kernel on the sequences' own keys joins the prefix's results itself; a single part may need no join
-  if (p.narrow[kOwn] || (p.parts == 1 && (p.direct || p.narrow[kPrefix]))) return cudaSuccess;
+cudaError_t launch_join(const AttendParams& p, cudaStream_t st) {
   const int64_t rows = (int64_t)p.b.n_tokens * p.q_heads;
   return launch_pdl(join_kernel<D>, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, st, p);
+}
+
+cudaError_t launch_parts(const sdq_cache_s* c, const AttendParams& p, cudaStream_t st) {
+  cudaError_t e = cudaSuccess;
+  for (int part = kPrefix; part >= kOwn && e == cudaSuccess; --part) {
+    if (p.wide[part]) e = launch_wide(c, p, part, st);
+    else if (p.narrow[part]) e = launch_narrow(c, p, part, part == kOwn && p.parts > 1, st);
+  }
+  if (e != cudaSuccess || p.parts == 1) return e;
+  return c->desc.head_dim == 128 ? launch_join<128>(p, st) : launch_join<64>(p, st);
 }
 
 int log2_of(int v) {
@@ -142,11 +167,13 @@ extern "C" int sdq_attention(sdq_cache c, const sdq_batch* b, int32_t q_heads, c
     p.tickets[part] = reinterpret_cast<uint64_t*>(w + L.tickets[part]);
     p.o[part] = reinterpret_cast<float*>(w + L.o[part]);
     p.ml[part] = reinterpret_cast<float2*>(w + L.ml[part]);
+    p.split_o[part] = reinterpret_cast<float*>(w + L.split_o[part]);
+    p.split_ml[part] = reinterpret_cast<float2*>(w + L.split_ml[part]);
+    p.warp_o[part] = reinterpret_cast<float*>(w + L.warp_o[part]);
+    p.block_o[part] = reinterpret_cast<float*>(w + L.block_o[part]);
+    p.block_ml[part] = reinterpret_cast<float2*>(w + L.block_ml[part]);
   }
-  p.warp_o = reinterpret_cast<float*>(w + L.warp_o);
-  p.block_o = reinterpret_cast<float*>(w + L.block_o);
-  p.block_ml = reinterpret_cast<float2*>(w + L.block_ml);
-  const cudaError_t e = d == 128 ? launch_parts<128>(c, p, (cudaStream_t)stream) : launch_parts<64>(c, p, (cudaStream_t)stream);
+  const cudaError_t e = launch_parts(c, p, (cudaStream_t)stream);
   return e == cudaSuccess ? SDQ_OK : SDQ_ERR_CUDA;
 }
 

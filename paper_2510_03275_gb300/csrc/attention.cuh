@@ -19,9 +19,10 @@ constexpr int kNarrowRows = 32;   // query rows per key head that the narrow ker
 struct AttendWs {
   size_t rec;                // call record
   size_t tickets[2];         // of (sequence, key head) and of the prefix's key heads
-  size_t o[2], ml[2];        // partials by row: [split][row][head_dim], [split][row]
-  size_t warp_o;             // narrow kernel: a piece per warp
-  size_t block_o, block_ml;  // and two parts per thread block
+  size_t o[2], ml[2];        // two parts' results by row, for their join
+  size_t split_o[2], split_ml[2];   // wide kernel: [thread block of the cluster][row]
+  size_t warp_o[2];          // narrow kernel: a piece per warp
+  size_t block_o[2], block_ml[2];   // and two parts per thread block
   size_t total;
 };
 
@@ -35,14 +36,14 @@ struct AttendParams {
   int q_heads, kv_heads, group, page_shift, box_shift, n_pages;
   int narrow[2], wide[2];   // which kernel takes a part (neither: it has no keys)
   int parts;                // parts that are computed apart (1, 2)
-  int direct;               // the wide kernel writes `out` itself
   int chained;              // the wide kernel's rows of kOwn run over the prefix first (no kPrefix part)
-  int splits[2];            // partials by row that a part leaves
+  int splits[2];            // thread blocks that share a row block's keys in the wide kernel
   uint64_t* rec;
   uint64_t call;
   uint64_t* tickets[2];
-  float *o[2], *warp_o, *block_o;
-  float2 *ml[2], *block_ml;
+  int early, ahead;         // narrow kernel: thread blocks that start beside the wide one, places that a warp of them takes ahead
+  float *o[2], *split_o[2], *warp_o[2], *block_o[2];
+  float2 *ml[2], *split_ml[2], *block_ml[2];
   int ctas;                 // thread blocks of the narrow kernel
 };
 
@@ -57,73 +58,30 @@ __device__ __forceinline__ float log2_approx(float x) {
   return r;
 }
 
-// Adds n partial results (`ml(i)`, `src(i)`: this lane's V columns of partial
-// i) to a row whose sums so far are acc, top, sum: a whole warp per row, in
-// the order of i, so that results do not depend on timing.
-template <int V, class Ml, class Src>
-__device__ __forceinline__ void join_partials(int n, Ml ml_of, Src src, float (&acc)[V], float& top, float& sum) {
-  const int lane = threadIdx.x & 31;
-  for (int i0 = 0; i0 < n; i0 += 32) {
-    float2 ml = make_float2(-INFINITY, 0.f);
-    if (i0 + lane < n) ml = ml_of(i0 + lane);
-    float mx = ml.x;
-    for (int d = 16; d; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-    mx = fmaxf(mx, top);
-    const float old = top == -INFINITY ? 0.f : exp2_approx(top - mx);
-    const float f = ml.x == -INFINITY ? 0.f : exp2_approx(ml.x - mx);
-    float add = ml.x == -INFINITY ? 0.f : ml.y * f;
-    for (int d = 16; d; d >>= 1) add += __shfl_xor_sync(0xffffffffu, add, d);
-    if (top != -INFINITY) {
-      sum *= old;
-#pragma unroll
-      for (int k = 0; k < V; ++k) acc[k] *= old;
-    }
-    sum += add;
-    top = mx;
-    const int m = min(32, n - i0);
-#pragma unroll 4
-    for (int j = 0; j < m; ++j) {
-      const float fj = __shfl_sync(0xffffffffu, f, j);
-      const float* at = src(i0 + j);
-      float v[V];
-      if (V == 4) {
-        const float4 x = __ldcg(reinterpret_cast<const float4*>(at));
-        v[0] = x.x;
-        v[1] = x.y;
-        v[V - 2] = x.z;
-        v[V - 1] = x.w;
-      } else {
-        const float2 x = __ldcg(reinterpret_cast<const float2*>(at));
-        v[0] = x.x;
-        v[1] = x.y;
-      }
-      if (fj != 0.f) {   // (a partial that saw nothing holds anything)
-#pragma unroll
-        for (int k = 0; k < V; ++k) acc[k] += fj * v[k];
-      }
-    }
+// This lane's V columns of a row of D fp32 that another thread block wrote.
+template <int D, int V>
+__device__ __forceinline__ void load_row(const float* row, float (&v)[V]) {
+  const float* at = row + V * (threadIdx.x & 31);
+  if (V == 4) {
+    const float4 x = __ldcg(reinterpret_cast<const float4*>(at));
+    v[0] = x.x;
+    v[1] = x.y;
+    v[V - 2] = x.z;
+    v[V - 1] = x.w;
+  } else {
+    const float2 x = __ldcg(reinterpret_cast<const float2*>(at));
+    v[0] = x.x;
+    v[1] = x.y;
   }
 }
-// The partials by row that `part` left.
+// A row's sums (a whole warp, V columns a lane) as a part's result.
 template <int D, int V>
-__device__ __forceinline__ void join_rows(const AttendParams& p, int part, int64_t row, int n, float (&acc)[V], float& top, float& sum) {
-  const int64_t rows = (int64_t)p.b.n_tokens * p.q_heads;
+__device__ __forceinline__ void keep_row(const AttendParams& p, int part, int64_t row, const float (&acc)[V], float top, float sum) {
   const int lane = threadIdx.x & 31;
-  join_partials<V>(n, [&](int i) { return __ldcg(p.ml[part] + i * rows + row); },
-                   [&](int i) { return p.o[part] + (i * rows + row) * D + V * lane; }, acc, top, sum);
-}
-// Row r of a unit whose parts thread blocks first .. first + n - 1 of the
-// narrow kernel left: where it began, then continued.
-template <int D, int V>
-__device__ __forceinline__ void join_slots(const AttendParams& p, int r_block, int first, int n, int r, float (&acc)[V], float& top,
-                                           float& sum) {
-  const int lane = threadIdx.x & 31;
-#pragma unroll
-  for (int k = 0; k < V; ++k) acc[k] = 0.f;
-  top = -INFINITY;
-  sum = 0.f;
-  auto at = [&](int i) { return (2 * (int64_t)(first + i) + (i == 0 ? 1 : 0)) * r_block + r; };
-  join_partials<V>(n, [&](int i) { return __ldcg(p.block_ml + at(i)); }, [&](int i) { return p.block_o + at(i) * D + V * lane; }, acc, top, sum);
+  float* dst = p.o[part] + row * D + V * lane;
+  if (V == 4) *reinterpret_cast<float4*>(dst) = make_float4(acc[0], acc[1], acc[V - 2], acc[V - 1]);
+  else *reinterpret_cast<float2*>(dst) = make_float2(acc[0], acc[1]);
+  if (lane == 0) p.ml[part][row] = make_float2(sum == sum ? top : sum, sum);   // (NaN scores leave no maximum)
 }
 // A finished row: this lane's V columns.
 template <int D, int V>
@@ -136,13 +94,16 @@ __device__ __forceinline__ void write_row(const AttendParams& p, int64_t row, co
   if (p.lse && lane == 0) p.lse[row] = top == -INFINITY ? top : (top + log2_approx(sum)) * 0.69314718056f;
 }
 
-// The narrow kernel on `part`; late: behind this call's kernel on the prefix.
+// The narrow kernel on `part`; late: behind this call's kernel on the prefix,
+// beside which it may run.
 int narrow_groups(const sdq_batch* b, int group, int part);   // of 8 query rows
 int narrow_warps();                                           // per thread block
 cudaError_t launch_narrow(const sdq_cache_s* c, const AttendParams& p, int part, bool late, cudaStream_t st);
-// The wide kernel on `part`, and how many ways it splits the keys of a row
-// block (p.splits[part]).
+// The wide kernel on `part`, and how many thread blocks share the keys of a
+// row block (p.splits[part]).
 int wide_splits(const sdq_cache_s* c, const sdq_batch* b, int q_heads, int part, bool chained);
+double wide_time(const sdq_cache_s* c, const sdq_batch* b, int q_heads, int part, bool chained, int splits);   // us, estimated
+int64_t wide_grid(const sdq_cache_s* c, const AttendParams& p, int part);   // thread blocks
 cudaError_t launch_wide(const sdq_cache_s* c, const AttendParams& p, int part, cudaStream_t st);
 
 }  // namespace sdq

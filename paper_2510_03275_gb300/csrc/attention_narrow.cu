@@ -158,6 +158,32 @@ struct Walk {
   }
 };
 
+// How the line is cut: `early` thread blocks whose warps take `ahead` places
+// more than the others' (AttendParams), all of it if that is enough.
+struct Shares {
+  int64_t big, small, split;   // places a warp of the first `early` thread blocks, of the others; where the others begin
+  int early;
+  __device__ Shares(const AttendParams& p, int part, int64_t total, int blocks) {
+    early = part == kOwn ? min(p.early, blocks) : 0;
+    const int64_t first = (int64_t)early * kWarps, warps = (int64_t)blocks * kWarps, more = first * p.ahead;
+    if (early > 0 && total <= more) {
+      big = max((int64_t)1, (total + first - 1) / first);
+      small = 0;
+    } else {
+      small = max((int64_t)1, (total - (early > 0 ? more : 0) + warps - 1) / warps);
+      big = small + (early > 0 ? p.ahead : 0);
+    }
+    split = first * big;
+  }
+  __device__ int64_t begin(int block) const {
+    return block <= early ? (int64_t)block * kWarps * big : split + (int64_t)(block - early) * kWarps * small;
+  }
+  __device__ int64_t of(int block) const { return block < early ? big : small; }
+  __device__ int block_of(int64_t place) const {
+    return (int)(place < split || small == 0 ? place / (kWarps * big) : early + (place - split) / (kWarps * small));
+  }
+};
+
 // Where an output element of a piece stands: row r, column d of kRows x D fp32,
 // the 16-byte chunks of a row permuted so that the fragments' scattered
 // stores meet no bank twice.
@@ -217,9 +243,8 @@ __device__ __forceinline__ void add_pieces(int n, Ml ml_of, At at, int c, int fl
 }
 
 // Rows 8 n .. 8 n + 7 of unit u: the sum of a source's pieces, in the order of
-// the keys, then (slot < 0) joined with the prefix's partial results and
-// written to `out`, or kept as a partial result by row (the prefix, ahead of
-// the own part); or kept as part `slot` of the thread blocks' parts.  A warp: 4
+// the keys, written to `out`, or kept for the join with the call's other part;
+// or (slot >= 0) kept as part `slot` of the thread blocks' parts.  A warp: 4
 // lanes a row, lane c of them 16-byte chunks c, c + 4, ...; K of the D / 16
 // chunk groups from k0 on.  (Inlined: as a function of its own, calls cost 15000
 // cycles each.)
@@ -232,11 +257,7 @@ __device__ __forceinline__ void finish(const AttendParams& p, const Pieces<NT>& 
   if (r >= u.rows) return;
   const int tok = r / p.group;
   const int64_t row = (int64_t)(u.first + tok) * p.q_heads + u.h * p.group + r - tok * p.group;
-  const int64_t rows = (int64_t)p.b.n_tokens * p.q_heads;
-  const int nz = slot < 0 && part == kOwn && p.parts > 1 ? p.splits[kPrefix] : 0;
   const int x = 2 * ((r >> 1) & 3);   // (piece_at)
-  const float2* prefix_ml = p.ml[kPrefix] + row;
-  const float* prefix_o = p.o[kPrefix] + row * D;
   // pieces of this thread block: the odd ones in the warps' rings, then at most
   // one that ends its unit (even, in the workspace); or a whole unit's scratch
   const bool whole = src.e0 >= 2 * kWarps;
@@ -244,23 +265,20 @@ __device__ __forceinline__ void finish(const AttendParams& p, const Pieces<NT>& 
   const int far = !whole && src.e1 > 0 && (src.e1 & 1) ? src.e1 - 1 : -1;
   const float* near_o = whole ? reinterpret_cast<const float*>(smem + kWarps * S::kRing + (e0 - 2 * kWarps) * S::kScratch) + (r & 7) * D
                               : reinterpret_cast<const float*>(smem + (e0 >> 1) * S::kRing) + r * D;
-  const float* far_o = p.warp_o + (((int64_t)blockIdx.x * kWarps + (far >> 1)) * R + r) * D;
+  const float* far_o = p.warp_o[part] + (((int64_t)blockIdx.x * kWarps + (far >> 1)) * R + r) * D;
   // parts of thread blocks: where the unit began, then continued
-  const float2* block_ml = p.block_ml + 2 * (int64_t)src.first * R + r;
-  const float* block_o = p.block_o + (2 * (int64_t)src.first * R + r) * D;
+  const float2* block_ml = p.block_ml[part] + 2 * (int64_t)src.first * R + r;
+  const float* block_o = p.block_o[part] + (2 * (int64_t)src.first * R + r) * D;
   auto near_ml = [&](int i) { return make_float2(pc.m[e0 + step * i][r], pc.l[e0 + step * i][r]); };
   auto far_ml = [&](int) { return make_float2(pc.m[far][r], pc.l[far][r]); };
   auto block_of = [&](int i) { return (int64_t)(2 * i + (i == 0)) * R; };
   auto part_ml = [&](int i) { return __ldcg(block_ml + block_of(i)); };
-  auto row_ml = [&](int i) { return __ldcg(prefix_ml + i * rows); };
   float top = -INFINITY;
 #pragma unroll 4
   for (int i = 0; i < near; ++i) top = fmaxf(top, near_ml(i).x);
   if (far >= 0) top = fmaxf(top, far_ml(0).x);
 #pragma unroll 8
   for (int i = 0; i < src.n; ++i) top = fmaxf(top, part_ml(i).x);
-#pragma unroll 8
-  for (int i = 0; i < nz; ++i) top = fmaxf(top, row_ml(i).x);
   const float base = top == -INFINITY ? 0.f : top;
   float4 acc[K];
 #pragma unroll
@@ -269,14 +287,13 @@ __device__ __forceinline__ void finish(const AttendParams& p, const Pieces<NT>& 
   add_pieces<K, B, false>(near, near_ml, [&](int i) { return near_o + (step / 2) * i * (S::kRing / 4); }, c, x, base, acc, sum);
   if (far >= 0) add_pieces<K, 1, true>(1, far_ml, [&](int) { return far_o; }, c, x, base, acc, sum);
   add_pieces<K, B, true>(src.n, part_ml, [&](int i) { return block_o + block_of(i) * D; }, c, x, base, acc, sum);
-  add_pieces<K, B, true>(nz, row_ml, [&](int i) { return prefix_o + i * rows * D; }, c, 0, base, acc, sum);
   const bool first = (lane & 3) == 0 && k0 == 0;
-  if (slot >= 0 || (part == kPrefix && p.parts > 1)) {
-    float* dst = slot >= 0 ? p.block_o + (slot * R + r) * D : p.o[kPrefix] + row * D;
+  if (slot >= 0 || p.parts > 1) {
+    float* dst = slot >= 0 ? p.block_o[part] + (slot * R + r) * D : p.o[part] + row * D;
     const int flip = slot >= 0 ? x : 0;
 #pragma unroll
     for (int k = 0; k < K; ++k) *reinterpret_cast<float4*>(dst + 4 * ((c + 4 * k) ^ flip)) = acc[k];
-    if (first) *(slot >= 0 ? p.block_ml + slot * R + r : p.ml[kPrefix] + row) = make_float2(sum == sum ? top : sum, sum);
+    if (first) *(slot >= 0 ? p.block_ml[part] + slot * R + r : p.ml[part] + row) = make_float2(sum == sum ? top : sum, sum);
     return;
   }
   const float inv = sum > 0.f ? 1.f / sum : sum;   // (0 where nothing is seen; NaN stays)
@@ -311,18 +328,20 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (tid < (int)(sizeof(AttendParams) / 4)) reinterpret_cast<uint32_t*>(&sp)[tid] = reinterpret_cast<const uint32_t*>(&p)[tid];
   __syncthreads();
   // late: the kernel ahead is this call's own on the prefix, which started
-  // once everything before it was complete; it is waited for where its results
-  // are read
+  // once everything before it was complete and shares no memory with this one;
+  // it is waited for at the end, so that what follows this kernel follows both
   if (!late) pdl_wait();
   pdl_launch_dependents();
   call_record_start(p.rec, p.call, blockIdx.x == 0 && tid == 0);
   Walk walk(p, part);
-  const int64_t total = walk.total(), share = max((int64_t)1, (total + (int64_t)gridDim.x * kWarps - 1) / ((int64_t)gridDim.x * kWarps));
-  const int64_t t0 = ((int64_t)blockIdx.x * kWarps + warp) * share, t1 = min(total, t0 + share);
+  const int64_t total = walk.total();
+  const Shares shares(p, part, total, gridDim.x);
+  const int64_t share = shares.of(blockIdx.x), ct0 = shares.begin(blockIdx.x), ct1 = min(total, ct0 + kWarps * share);
+  const int64_t t0 = ct0 + warp * share, t1 = min(total, t0 + share);
   uint8_t* ring = smem + warp * S::kRing;
   const uint32_t ring_a = sbase + warp * S::kRing;
   float* scratch = reinterpret_cast<float*>(smem + kWarps * S::kRing + warp * S::kScratch);
-  bool ok = true, waited = !late;
+  bool ok = true;
   Unit head, tail;   // units whose pieces this warp joins: one that ends here, one that goes on behind this share
   bool head_set = false, tail_set = false;
   if (t0 < t1) {
@@ -478,10 +497,6 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int d = 4; d < 32; d <<= 1) l[n][j] += __shfl_xor_sync(0xffffffffu, l[n][j], d);
       const bool starts = lo == 0, ends = hi == u.tiles;
-      if (ends && !waited) {   // (results of the prefix; and the workspace's pieces may still be read)
-        pdl_wait();
-        waited = true;
-      }
       const bool whole = starts && ends;
       if (whole && p.parts == 1) {
         // a whole unit, nothing to join: O^T is turned by movmatrix as P was, a row's 4 lanes write 16 bytes at a time
@@ -515,7 +530,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       // last one into the ring, whose copies are all read
       const int e = whole ? 2 * kWarps + warp : 2 * warp + (ends ? 0 : 1);
       float* dst = whole  ? scratch
-                   : ends ? p.warp_o + ((int64_t)blockIdx.x * kWarps + warp) * (R * D)
+                   : ends ? p.warp_o[part] + ((int64_t)blockIdx.x * kWarps + warp) * (R * D)
                           : reinterpret_cast<float*>(ring);
       __syncwarp();
 #pragma unroll
@@ -556,9 +571,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   // ---- pieces of this thread block
   const bool all_ok = __syncthreads_and(ok);
-  if (!waited) pdl_wait();
-  const int64_t ct0 = (int64_t)blockIdx.x * kWarps * share, ct1 = min(total, ct0 + kWarps * share);
-  const int64_t block_share = kWarps * share;
   if (all_ok) {
     // the units with pieces here, each by one warp.  Those that lie in other
     // thread blocks too are kept as parts
@@ -585,7 +597,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         arrived[tid] = 0;
         if (pc.is_open[tid]) {
           const Unit& u = pc.open[tid];
-          const uint32_t n = (uint32_t)((u.a + u.tiles - 1) / block_share - u.a / block_share + 1);
+          const uint32_t n = (uint32_t)(shares.block_of(u.a + u.tiles - 1) - shares.block_of(u.a) + 1);
           uint64_t* tk = p.tickets[part] + (part == kPrefix ? u.h : (int64_t)u.s * p.kv_heads + u.h);
           const uint32_t got = ticket_take(tk, p.call, n);
           if (got == 0) call_record_fail(p.rec, p.call);
@@ -597,13 +609,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!arrived[i]) continue;
         // the last to arrive: all thread blocks' parts, a chunk group a warp
         const Unit& u = pc.open[i];
-        const int first = (int)(u.a / block_share), n = (int)((u.a + u.tiles - 1) / block_share) - first + 1;
+        const int first = shares.block_of(u.a), n = shares.block_of(u.a + u.tiles - 1) - first + 1;
         constexpr int kPer = kWarps / (D / 16);   // warps on a chunk group, each of its own rows
         for (int m = warp % kPer; m < NT; m += kPer)
           finish<D, NT, 1>(sp, pc, smem, part, u, m, Source{0, 0, first, n}, -1, warp / kPer);
       }
     }
-    // sequences without keys of their own: the prefix's result, or 0
+    // sequences without keys of their own: 0, or nothing to join
     if (part == kOwn)
       for (int s = blockIdx.x; s < p.b.n_seqs; s += gridDim.x) {
         const SeqSpan q = seq_span(p.b, s);
@@ -616,6 +628,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
   }
   if (!ok && lane == 0) call_record_fail(p.rec, p.call);
+  if (late) pdl_wait();
 }
 
 template <int D, int NT>

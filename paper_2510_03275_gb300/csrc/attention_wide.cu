@@ -27,6 +27,10 @@ namespace {
 //                   swizzle); warps 10 and 11 only complete its warpgroup
 // The MMAs of a thread block run in the order of their issue, so that S of the
 // next tile may overwrite P once the product that reads it is issued.
+// Few row blocks: a cluster of up to 8 thread blocks shares the line of one,
+// writes its sums to the workspace and meets at the cluster's barrier, after
+// which each thread block joins its part of the rows.  (Through the cluster's
+// shared memory the join took twice as long, 6 us of a 29 us kernel.)
 // Registers: 384 threads hold 168 each at launch; the first two warpgroups go
 // to 224 once the third has gone down to 56 (224 + 224 + 56 = 3 x 168).
 constexpr int kWideThreads = 384;
@@ -38,6 +42,7 @@ template <int D> struct WideShape {
   static constexpr int kMat = (D / 64) * kHalf;              // 128 rows of Q, K or V
   static constexpr int kRing = D == 128 ? 5 : 8;
   static constexpr int kSmem = 1024 + (2 + kRing) * kMat;
+  static_assert(256 * D * 4 <= (2 + kRing) * kMat, "256 fp32 rows fit over the operands");
 };
 
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
@@ -132,10 +137,13 @@ __device__ __forceinline__ bool wide_item(const AttendParams& p, int part, WideI
     // block `id` counted over the sequences' row blocks
     const int lane = threadIdx.x & 31;
     int base = 0, s = -1, rb = 0;
+    SeqSpan q{0, 0, 0};
     for (int s0 = 0; s0 < p.b.n_seqs && s < 0; s0 += 32) {
-      const int n = s0 + lane < p.b.n_seqs ? (seq_span(p.b, s0 + lane).count * p.group + 255) / 256 : 0;
+      SeqSpan x{0, 0, 0};
+      if (s0 + lane < p.b.n_seqs) x = seq_span(p.b, s0 + lane);
+      const int n = (x.count * p.group + 255) / 256;
       int end = n;
-      for (int d = 1; d < 32; d <<= 1) {
+      for (int d = 1; d < 32 && s0 + d < p.b.n_seqs; d <<= 1) {
         const int o = __shfl_up_sync(0xffffffffu, end, d);
         if (lane >= d) end += o;
       }
@@ -145,11 +153,11 @@ __device__ __forceinline__ bool wide_item(const AttendParams& p, int part, WideI
         s = s0 + l;
         rb = id - base - __shfl_sync(0xffffffffu, end - n, l);
         rb = __shfl_sync(0xffffffffu, n, l) - 1 - rb;   // the blocks that see the most keys first
+        q = SeqSpan{__shfl_sync(0xffffffffu, x.first, l), __shfl_sync(0xffffffffu, x.count, l), __shfl_sync(0xffffffffu, x.own, l)};
       }
       base += __shfl_sync(0xffffffffu, end, 31);
     }
     if (s < 0) return false;
-    const SeqSpan q = seq_span(p.b, s);
     w->s = s;
     w->first = q.first;
     w->count = q.count;
@@ -166,6 +174,54 @@ __device__ __forceinline__ bool wide_item(const AttendParams& p, int part, WideI
   return true;
 }
 
+// The cluster's rows (in the workspace, each thread block's sums over its own
+// keys): this thread block's share of them, two at a time per warp (8 warps),
+// summed in the order of the keys.
+template <int D>
+__device__ __forceinline__ void join_rows(const AttendParams& p, int part, const WideItem& w) {
+  constexpr int V = D / 32, kBatch = 2;
+  const int warp = threadIdx.x >> 5;
+  const int splits = p.splits[part], valid = min(256, w.rows - w.r0);
+  const int64_t rows = (int64_t)p.b.n_tokens * p.q_heads;
+  for (int r0 = warp * splits + w.split; r0 < valid; r0 += 8 * kBatch * splits) {
+    float2 ml[kBatch][kMaxWideSplits];
+    float v[kBatch][kMaxWideSplits][V];
+    int64_t out[kBatch];
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const int row = w.r0 + min(r0 + 8 * j * splits, valid - 1), tok = row / p.group;
+      out[j] = (int64_t)(w.first + tok) * p.q_heads + w.h * p.group + row - tok * p.group;
+#pragma unroll
+      for (int i = 0; i < kMaxWideSplits; ++i)
+        if (i < splits) {
+          ml[j][i] = __ldcg(p.split_ml[part] + i * rows + out[j]);
+          load_row<D, V>(p.split_o[part] + (i * rows + out[j]) * D, v[j][i]);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      if (r0 + 8 * j * splits >= valid) break;
+      float acc[V], sum = 0.f, top = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < V; ++k) acc[k] = 0.f;
+#pragma unroll
+      for (int i = 0; i < kMaxWideSplits; ++i)
+        if (i < splits) top = fmaxf(top, ml[j][i].x);
+      const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+      for (int i = 0; i < kMaxWideSplits; ++i)
+        if (i < splits) {
+          const float f = exp2_approx(ml[j][i].x - base);
+          sum += f == 0.f ? 0.f : ml[j][i].y * f;
+#pragma unroll
+          for (int k = 0; k < V; ++k) acc[k] += f * v[j][i][k];
+        }
+      if (p.parts > 1) keep_row<D, V>(p, part, out[j], acc, top, sum);
+      else write_row<D, V>(p, out[j], acc, top, sum);
+    }
+  }
+}
+
 template <int D>
 __global__ void __launch_bounds__(kWideThreads, 1)
     wide_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const AttendParams p,
@@ -178,18 +234,12 @@ __global__ void __launch_bounds__(kWideThreads, 1)
   const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t ring = sbase + 2 * S::kMat;
   uint8_t* ring_ptr = smem_raw + (ring - smem_u32(smem_raw));
-  pdl_wait();
-  pdl_launch_dependents();
-  call_record_start(p.rec, p.call, blockIdx.x == 0 && tid == 0);
-  WideItem w;
-  if (!wide_item(p, part, &w)) return;   // (all warps alike)
-  const int n = w.t1 - w.t0, halves = w.rows - w.r0 > 128 ? 2 : 1;
   if (tid == 0) {
     for (int i = 0; i < S::kRing; ++i) {
       mbar_init(&full[i], 1);
       mbar_init(&empty[i], 1);
     }
-    mbar_init(&q_full, 128 * halves);
+    mbar_init(&q_full, 256);
     for (int i = 0; i < 2; ++i) {
       mbar_init(&s_full[i], 1);
       for (int j = 0; j < 2; ++j) mbar_init(&p_full[i][j], 128);
@@ -205,6 +255,17 @@ __global__ void __launch_bounds__(kWideThreads, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  pdl_wait();
+  pdl_launch_dependents();
+  call_record_start(p.rec, p.call, blockIdx.x == 0 && tid == 0);
+  WideItem w;
+  if (!wide_item(p, part, &w)) {   // (all warps of the cluster alike)
+    if (warp == 8) tmem_dealloc(tmem_base, 512);
+    return;
+  }
+  const int n = w.t1 - w.t0, halves = w.rows - w.r0 > 128 ? 2 : 1;
+  // row by row at the end: a cluster's sums, or fp32 rows for the join with the other part
+  const bool joins = p.splits[part] > 1 || p.parts > 1;
   const uint32_t tmem = tmem_base;
   bool ok = true;
   if (warp >= 8) {
@@ -299,25 +360,31 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         if (!mbar_wait_warp(&mma_done, 0)) ok = false;
       }
     }
+    if (p.splits[part] > 1) cluster_sync();
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 224;\n");
     if ((warp >> 2) < halves) {
       // ---------------------------------------------------------- softmax
       const int half = warp >> 2, wtid = tid & 127;
       const uint32_t qb = sbase + half * S::kMat;
+      const int row = w.r0 + 128 * half + wtid, tok = row / p.group, g = row - tok * p.group;
+      const bool live = row < w.rows;
+      {
+        // a warp its 32 rows, a row's chunks by neighbouring lanes (rows past the last: zeros)
+        constexpr int kChunks = D / 8;
+        const uint16_t* mine = p.q + (live ? (int64_t)(w.first + tok) * p.ldq + (int64_t)(w.h * p.group + g) * D : 0);
+        const uint32_t bytes = live ? 16u : 0u;
 #pragma unroll
-      for (int i = wtid; i < 128 * (D / 8); i += 128) {
-        const int r = i / (D / 8), c = i % (D / 8), row = w.r0 + 128 * half + r;
-        const int tok = row / p.group, g = row - tok * p.group;
-        const bool in = row < w.rows;   // (rows past the last: zeros)
-        const uint16_t* src = p.q + (int64_t)(in ? w.first + tok : 0) * p.ldq + (int64_t)(w.h * p.group + (in ? g : 0)) * D + 8 * c;
-        cp_async16(smem_raw + (qb - smem_u32(smem_raw)) + (c >> 3) * kHalf + r * 128 + (((c & 7) ^ (r & 7)) << 4), src, in ? 16 : 0);
+        for (int i = 0; i < kChunks; ++i) {
+          const int l = (32 / kChunks) * i + lane / kChunks, r = 32 * (warp & 3) + l, c = lane % kChunks;
+          const uint16_t* src = reinterpret_cast<const uint16_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine), l));
+          cp_async16(smem_raw + (qb - smem_u32(smem_raw)) + (c >> 3) * kHalf + r * 128 + (((c & 7) ^ (r & 7)) << 4), src + 8 * c,
+                     __shfl_sync(0xffffffffu, bytes, l));
+        }
       }
       cp_async_wait_all();
       fence_proxy_async_smem();
       mbar_arrive(&q_full);
-      const int row = w.r0 + 128 * half + wtid, tok = row / p.group, g = row - tok * p.group;
-      const bool live = row < w.rows;
       // own keys that this row sees, and that every row of its half does
       const int lim = live ? w.own - w.count + tok + 1 : w.own;
       const int all = w.own - w.count + (w.r0 + 128 * half) / p.group + 1;
@@ -414,62 +481,85 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       // ------------------------------------------------------------- out
       if (n > 0 && ok) ok = mbar_wait_warp(&mma_done, 0);
       tc_fence_after();
-      if (ok) {
+      if (joins) {
+        // fp32 rows through shared memory, over operands that nothing reads any
+        // more (nor has still to arrive: the barrier is behind all copies of Q)
+        named_bar_sync(1, 128 * halves);
+        const int64_t at = (int64_t)(w.first + tok) * p.q_heads + w.h * p.group + g;
+        const bool split = p.splits[part] > 1;
+        const int64_t slot = (split ? (int64_t)w.split * p.b.n_tokens * p.q_heads : 0) + at;
+        const uint32_t stage = sbase + (uint32_t)((128 * half + 32 * (warp & 3)) * 4 * D), mine = stage + (uint32_t)(lane * 4 * D);
+        const uint32_t lives = __ballot_sync(0xffffffffu, live);
+        const unsigned long long dst = reinterpret_cast<unsigned long long>((split ? p.split_o[part] : p.o[part]) + slot * D);
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t o[32];
+          if (n > 0) {
+            tmem_ld32(to + 32 * c, o);
+            tmem_ld_wait();
+          } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) o[j] = 0;
+          }
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            st_shared16(mine + (((8 * c + j) ^ (lane & 7)) << 4), o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+        }
+        __syncwarp();
+        constexpr int kChunks = D / 4, kAt = 32 / kChunks;   // 16-byte pieces of a row, rows at once
+#pragma unroll 8
+        for (int i = 0; i < kChunks; ++i) {
+          const int r = kAt * i + lane / kChunks, c = lane % kChunks;
+          uint4* to_row = reinterpret_cast<uint4*>(__shfl_sync(0xffffffffu, dst, r)) + c;
+          const uint4 v = ld_shared16(stage + (uint32_t)(r * 4 * D) + ((c ^ (r & 7)) << 4));
+          if (lives >> r & 1) *to_row = v;
+        }
+        if (live) (split ? p.split_ml[part] : p.ml[part])[slot] = make_float2(l == l ? m : l, l);   // (NaN scores leave no maximum)
+      } else if (ok) {
         // rows to memory over the place of Q, which nothing reads any more: a
         // thread's row would go out in 16-byte pieces, 32 rows at a time
         const int64_t at = (int64_t)(w.first + tok) * p.q_heads + w.h * p.group + g;
-        const int64_t rows = (int64_t)p.b.n_tokens * p.q_heads, pr = w.split * rows + at;
-        const float k = p.direct ? (l > 0.f ? 1.f / l : l) : 1.f;   // (0 where nothing is seen; NaN stays)
-        constexpr int kChunks = D / 8;                             // 16-byte pieces of a row: D bf16, or half as many fp32
+        const float k = l > 0.f ? 1.f / l : l;       // (0 where nothing is seen; NaN stays)
+        constexpr int kChunks = D / 8;
         const uint32_t stage = qb + (uint32_t)(32 * (warp & 3) * 2 * D);
         const uint32_t mine = stage + (uint32_t)(lane * 2 * D);
         const uint32_t lives = __ballot_sync(0xffffffffu, live);
-        uint8_t* base = p.direct ? reinterpret_cast<uint8_t*>(p.out) : reinterpret_cast<uint8_t*>(p.o[part]);
-        const int64_t row_at = p.direct ? at * (2 * D) : pr * (4 * D);   // bytes
-        for (int pass = 0; pass < (p.direct ? 1 : 2); ++pass) {
-          if (!p.direct && n == 0) break;
+        unsigned long long dst = reinterpret_cast<unsigned long long>(p.out + at * D);
 #pragma unroll
-          for (int c = 0; c < D / 32; ++c) {
-            uint32_t o[32];
-            if (!p.direct && c >= D / 64) break;
-            const int col = p.direct ? 32 * c : pass * (D / 2) + 32 * c;
-            if (n > 0) {
-              tmem_ld32(to + col, o);
-              tmem_ld_wait();
-            } else {
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t o[32];
+          if (n > 0) {
+            tmem_ld32(to + 32 * c, o);
+            tmem_ld_wait();
+          } else {
 #pragma unroll
-              for (int j = 0; j < 32; ++j) o[j] = 0;
-            }
-            if (p.direct) {
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const uint32_t v0 = pack_bf16x2(__uint_as_float(o[8 * j]) * k, __uint_as_float(o[8 * j + 1]) * k);
-                const uint32_t v1 = pack_bf16x2(__uint_as_float(o[8 * j + 2]) * k, __uint_as_float(o[8 * j + 3]) * k);
-                const uint32_t v2 = pack_bf16x2(__uint_as_float(o[8 * j + 4]) * k, __uint_as_float(o[8 * j + 5]) * k);
-                const uint32_t v3 = pack_bf16x2(__uint_as_float(o[8 * j + 6]) * k, __uint_as_float(o[8 * j + 7]) * k);
-                st_shared16(mine + (((4 * c + j) ^ (lane & 7)) << 4), v0, v1, v2, v3);
-              }
-            } else {
-#pragma unroll
-              for (int j = 0; j < 8; ++j)
-                st_shared16(mine + (((8 * c + j) ^ (lane & 7)) << 4), o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
-            }
+            for (int j = 0; j < 32; ++j) o[j] = 0;
           }
-          __syncwarp();
 #pragma unroll
-          for (int i = 0; i < kChunks; ++i) {
-            const int r = (32 / kChunks) * i + lane / kChunks, c = lane % kChunks;
-            const int64_t off = __shfl_sync(0xffffffffu, row_at, r);
-            const uint4 v = ld_shared16(stage + (uint32_t)(r * 2 * D) + ((c ^ (r & 7)) << 4));
-            if (lives >> r & 1) *reinterpret_cast<uint4*>(base + off + pass * (2 * D) + 16 * c) = v;
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t v0 = pack_bf16x2(__uint_as_float(o[8 * j]) * k, __uint_as_float(o[8 * j + 1]) * k);
+            const uint32_t v1 = pack_bf16x2(__uint_as_float(o[8 * j + 2]) * k, __uint_as_float(o[8 * j + 3]) * k);
+            const uint32_t v2 = pack_bf16x2(__uint_as_float(o[8 * j + 4]) * k, __uint_as_float(o[8 * j + 5]) * k);
+            const uint32_t v3 = pack_bf16x2(__uint_as_float(o[8 * j + 6]) * k, __uint_as_float(o[8 * j + 7]) * k);
+            st_shared16(mine + (((4 * c + j) ^ (lane & 7)) << 4), v0, v1, v2, v3);
           }
-          __syncwarp();
         }
-        if (live) {
-          if (!p.direct) p.ml[part][pr] = make_float2(l == l ? m : l, l);   // (NaN scores leave no maximum)
-          else if (p.lse) p.lse[at] = m == -INFINITY ? m : (m + log2_approx(l)) * 0.69314718056f;
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) {
+          const int r = (32 / kChunks) * i + lane / kChunks, c = lane % kChunks;
+          uint4* to_row = reinterpret_cast<uint4*>(__shfl_sync(0xffffffffu, dst, r)) + c;
+          const uint4 v = ld_shared16(stage + (uint32_t)(r * 2 * D) + ((c ^ (r & 7)) << 4));
+          if (lives >> r & 1) *to_row = v;
         }
+        if (live && p.lse) p.lse[at] = m == -INFINITY ? m : (m + log2_approx(l)) * 0.69314718056f;
       }
+    }
+    else mbar_arrive(&q_full);
+    if (p.splits[part] > 1) {
+      __threadfence();
+      cluster_sync();   // all parts of the rows are in memory
+      join_rows<D>(p, part, w);
     }
   }
   if (!ok && lane == 0) call_record_fail(p.rec, p.call);
@@ -489,21 +579,73 @@ int64_t wide_blocks(const sdq_batch* b, int group, int part) {
 }
 
 template <int D>
-cudaError_t launch(const sdq_cache_s* c, const AttendParams& p, int part, cudaStream_t st) {
+void launch_config(cudaLaunchConfig_t* cfg, cudaLaunchAttribute* attr, int64_t grid, int splits, cudaStream_t st) {
+  *cfg = {};
+  cfg->gridDim = dim3((unsigned)grid);
+  cfg->blockDim = dim3(kWideThreads);
+  cfg->dynamicSmemBytes = WideShape<D>::kSmem;
+  cfg->stream = st;
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)splits;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg->attrs = attr;
+  cfg->numAttrs = 2;
+}
+
+template <int D>
+cudaError_t smem_limit(int device) {
   static std::atomic<int> smem_set[64];
-  const cudaError_t e = smem_limit_once(wide_kernel<D>, WideShape<D>::kSmem, c->device, smem_set);
+  return smem_limit_once(wide_kernel<D>, WideShape<D>::kSmem, device, smem_set);
+}
+
+template <int D>
+cudaError_t launch(const sdq_cache_s* c, const AttendParams& p, int part, cudaStream_t st) {
+  const cudaError_t e = smem_limit<D>(c->device);
   if (e != cudaSuccess) return e;
-  const int64_t grid = wide_blocks(&p.b, p.group, part) * p.kv_heads * p.splits[part];
-  return launch_pdl(wide_kernel<D>, dim3((unsigned)grid), dim3(kWideThreads), (size_t)WideShape<D>::kSmem, st, c->kmap, c->vmap, p, part);
+  cudaLaunchConfig_t cfg;
+  cudaLaunchAttribute attr[2];
+  launch_config<D>(&cfg, attr, wide_grid(c, p, part), p.splits[part], st);
+  return cudaLaunchKernelEx(&cfg, wide_kernel<D>, c->kmap, c->vmap, p, part);
+}
+
+template <int D>
+cudaError_t occupancy(sdq_cache_s* c) {
+  cudaError_t e = smem_limit<D>(c->device);
+  c->wide_clusters[1] = c->sm_count;
+  for (int s = 2; s <= kMaxWideSplits && e == cudaSuccess; ++s) {
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[2];
+    launch_config<D>(&cfg, attr, s, s, 0);
+    cfg.numAttrs = 1;   // the cluster alone
+    e = cudaOccupancyMaxActiveClusters(&c->wide_clusters[s], wide_kernel<D>, &cfg);
+  }
+  return e;
 }
 
 }  // namespace
 
-int wide_splits(const sdq_cache_s* c, const sdq_batch* b, int q_heads, int part, bool chained) {
-  const int64_t items = wide_blocks(b, q_heads / c->desc.kv_heads, part) * c->desc.kv_heads;
+cudaError_t wide_occupancy(sdq_cache_s* c) { return c->desc.head_dim == 128 ? occupancy<128>(c) : occupancy<64>(c); }
+
+int64_t wide_grid(const sdq_cache_s* c, const AttendParams& p, int part) {
+  return wide_blocks(&p.b, p.group, part) * c->desc.kv_heads * p.splits[part];
+}
+
+// us, over waves of clusters of s: a tile (256 rows) takes 1.3 us, a thread
+// block's two ends 5 us, the join of a cluster 5 us more.
+double wide_time(const sdq_cache_s* c, const sdq_batch* b, int q_heads, int part, bool chained, int s) {
+  const int64_t items = wide_blocks(b, q_heads / c->desc.kv_heads, part) * c->desc.kv_heads, held = std::max(1, c->wide_clusters[s]);
   const int64_t tiles = (part == kPrefix || chained ? ((int64_t)b->prefix_len + kKeys - 1) / kKeys : 0) +
                         (part == kOwn ? ((int64_t)b->max_own + kKeys - 1) / kKeys : 0);
-  return (int)std::max<int64_t>(1, std::min<int64_t>({c->sm_count / items, tiles, 64}));
+  return (double)((items + held - 1) / held) * (5.0 + (s > 1 ? 5.0 : 0.0) + 1.3 * (double)((tiles + s - 1) / s));
+}
+
+int wide_splits(const sdq_cache_s* c, const sdq_batch* b, int q_heads, int part, bool chained) {
+  int best = 1;
+  for (int s = 2; s <= kMaxWideSplits; ++s)
+    if (wide_time(c, b, q_heads, part, chained, s) < wide_time(c, b, q_heads, part, chained, best)) best = s;
+  return best;
 }
 
 cudaError_t launch_wide(const sdq_cache_s* c, const AttendParams& p, int part, cudaStream_t st) {
