@@ -512,7 +512,8 @@ int sdq_attention_status(const void* ws, void* stream);
  * <= 0 (or NaN): the first of the largest logits.  NaN logits count as -inf;
  * a row without a logit above -inf gives -1; with logits of +inf only those
  * have a weight.  temperature, top_k, top_p, min_p: one per row (device), or
- * NULL for 1, 0, 1, 0.  Weights are fp32 (exp, one quotient), masses whole
+ * NULL for 1, 0, 1, 0.  Weights are fp32 (exp of the
+ * difference times the rounded reciprocal of T), masses whole
  * multiples of 2^-44 of the largest weight, so that sums are exact and the
  * token depends on nothing but its inputs; weights below 2^-45 count as 0.
  * vocab up to 393216, rows up to 65535; no workspace; one kernel, launched
