@@ -3,7 +3,10 @@
 //
 // A cluster of up to 8 thread blocks keeps a row in its shared memory, so that
 // HBM is read once however often the row is looked at:
-//   1  load, largest logit
+//   1  load, largest logit.  For a top-k of k: the k / (blocks) largest of each
+//      block's threads' own largest are as many logits, so that the least of
+//      them over the blocks bounds the row's k-th from below.  Usually little
+//      more than k lie above the bound: they are gathered as in 3, without 2
 //   2  a histogram (count and mass) of the logits within 8 T of the largest, in
 //      steps of T / 16, and where top-p has no top-k ahead of it the mass of
 //      all; where a cut lies further down, of those within 8 to 12 T, and so
@@ -85,6 +88,9 @@ struct alignas(16) Shared {   // (the logits behind it are read 4 at a time)
       uint32_t rank[kCap];
     } all;
   };
+  // partial sums of a step that several threads share
+  uint32_t part_n[kThreads];
+  unsigned long long part_m[kThreads];
   // posted for the cluster: written before a cluster barrier, read after it,
   // not written again before the next one
   float post_max;
@@ -174,23 +180,30 @@ __device__ __forceinline__ void clear_histogram(Histogram& h) {
 
 // Cumulative counts and masses of the row's bins, from all blocks of the cluster.
 __device__ __forceinline__ void join_histogram(Shared& s, Cumulative& to, int cluster) {
+  static_assert(kThreads >= kMaxCluster * kBins, "a thread for each bin of each block");
+  {
+    const int q = threadIdx.x / kBins, b = threadIdx.x % kBins;
+    uint32_t cnt = 0;
+    unsigned long long mass = 0;
+    if (q < cluster) {
+      cnt = remote_u32(&s.own.cnt[b], q);
+      const uint32_t lo = remote_u32(&s.own.lo[b], q), hi = remote_u32(&s.own.hi[b], q);
+      mass = ((unsigned long long)hi << 32) + lo;
+    }
+    s.part_n[threadIdx.x] = cnt;
+    s.part_m[threadIdx.x] = mass;
+  }
+  __syncthreads();
   uint32_t c = 0;
   unsigned long long m = 0;
-  uint32_t v[3][kMaxCluster];
   const bool mine = threadIdx.x < kBins;
+  if (mine) {
 #pragma unroll
-  for (int r = 0; r < kMaxCluster; ++r)
-    if (mine && r < cluster) {   // (all under way at once)
-      v[0][r] = remote_u32(&s.own.cnt[threadIdx.x], r);
-      v[1][r] = remote_u32(&s.own.lo[threadIdx.x], r);
-      v[2][r] = remote_u32(&s.own.hi[threadIdx.x], r);
+    for (int q = 0; q < kMaxCluster; ++q) {
+      c += s.part_n[q * kBins + threadIdx.x];
+      m += s.part_m[q * kBins + threadIdx.x];
     }
-#pragma unroll
-  for (int r = 0; r < kMaxCluster; ++r)
-    if (mine && r < cluster) {
-      c += v[0][r];
-      m += ((unsigned long long)v[2][r] << 32) + v[1][r];
-    }
+  }
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   for (int d = 1; d < 32; d <<= 1) {
     const uint32_t a = __shfl_up_sync(0xffffffffu, c, d);
@@ -352,19 +365,36 @@ __device__ __forceinline__ Place locate(Shared& s, const Row& r, const Goal& g, 
 __device__ __forceinline__ unsigned long long order_of(uint32_t key, uint32_t idx) { return ((unsigned long long)key << 32) | (uint32_t)~idx; }
 __device__ __forceinline__ uint32_t key_in(unsigned long long order) { return (uint32_t)(order >> 32); }
 __device__ __forceinline__ int idx_in(unsigned long long order) { return (int)~(uint32_t)order; }
-// Rank of the gathered logit `order`, and the mass before it.
-__device__ __forceinline__ void rank_in(const Shared& s, uint32_t have, unsigned long long order, uint32_t* rank, unsigned long long* before) {
+// Rank of the gathered logit that is this thread's (order; thread c has logit
+// c), and the mass before it: all threads of the block, as many to a logit as
+// there are.
+__device__ __forceinline__ void rank_in(Shared& s, uint32_t have, uint32_t* rank, unsigned long long* before) {
+  const uint32_t width = (have + 31) & ~31u, parts = kThreads / width;   // (have >= 1)
+  const uint32_t c = threadIdx.x % width, part = threadIdx.x / width;
   uint32_t n = 0;
   unsigned long long m = 0;
+  if (part < parts && c < have) {
+    const unsigned long long order = s.all.order[c];
+    const uint32_t j1 = (part + 1) * have / parts;
 #pragma unroll 8
-  for (uint32_t j = 0; j < have; ++j) {
-    const bool better = s.all.order[j] > order;
-    const unsigned long long w = s.all.w[j];
-    n += better;
-    m += better ? w : 0ull;
+    for (uint32_t j = part * have / parts; j < j1; ++j) {
+      const bool better = s.all.order[j] > order;
+      const unsigned long long w = s.all.w[j];
+      n += better;
+      m += better ? w : 0ull;
+    }
   }
-  *rank = n;
-  *before = m;
+  s.part_n[threadIdx.x] = n;
+  s.part_m[threadIdx.x] = m;
+  __syncthreads();
+  *rank = 0;
+  *before = 0;
+  if (threadIdx.x < have)
+    for (uint32_t q = 0; q < parts; ++q) {
+      *rank += s.part_n[q * width + threadIdx.x];
+      *before += s.part_m[q * width + threadIdx.x];
+    }
+  __syncthreads();
 }
 
 // This block's share of a gathered list: those of the logits between two
@@ -384,7 +414,6 @@ __device__ __forceinline__ void gather(Shared& s, const Row& r, float from, floa
 }
 // The cluster's lists into s.all (after a cluster barrier); their number.
 __device__ __forceinline__ uint32_t collect(Shared& s, const Row& r) {
-  // block q's by warp q
   const uint32_t mine = posted(&s.list_n, r.cluster, 0u);
   uint32_t upto = mine;
   for (int d = 1; d < kMaxCluster; d <<= 1) {
@@ -392,15 +421,14 @@ __device__ __forceinline__ uint32_t collect(Shared& s, const Row& r) {
     if ((int)(threadIdx.x & 31) >= d) upto += o;
   }
   const uint32_t have = min((uint32_t)kCap, __shfl_sync(0xffffffffu, upto, kMaxCluster - 1));
-  const int q = threadIdx.x >> 5;
-  if (q < r.cluster) {
-    const uint32_t m = __shfl_sync(0xffffffffu, mine, q), at = __shfl_sync(0xffffffffu, upto, q) - m;
-    for (uint32_t j = threadIdx.x & 31; j < m && at + j < have; j += 32) {
+  const int warp = threadIdx.x >> 5, q = warp % r.cluster, per = kWarps / r.cluster;   // warps to a block's list
+  const uint32_t m = __shfl_sync(0xffffffffu, mine, q), at = __shfl_sync(0xffffffffu, upto, q) - m;
+  if (warp < per * r.cluster)
+    for (uint32_t j = 32 * (warp / r.cluster) + (threadIdx.x & 31); j < m && at + j < have; j += 32 * per) {
       const uint32_t k = remote_u32(&s.list_key[j], q);
       s.all.order[at + j] = order_of(k, remote_u32(&s.list_idx[j], q));
       s.all.w[at + j] = weight(scaled(logit_of(k), r.top, r.inv_t));
     }
-  }
   __syncthreads();
   return have;
 }
@@ -512,10 +540,10 @@ __device__ __forceinline__ void resolve(Shared& s, const Row& r, const Goal& g, 
   cluster_sync();
   const uint32_t have = collect(s, r);
   const uint32_t c = threadIdx.x;   // (have <= kCap, a thread each)
+  uint32_t rank;
+  unsigned long long before;
+  rank_in(s, max(have, 1u), &rank, &before);
   if (c < have) {
-    uint32_t rank;
-    unsigned long long before;
-    rank_in(s, have, s.all.order[c], &rank, &before);
     s.all.rank[c] = rank;
     if (g.by_count ? above_cnt + rank < g.count : above_mass + before < g.mass) {
       atomicMax(&s.nkeep, rank + 1);
@@ -525,6 +553,41 @@ __device__ __forceinline__ void resolve(Shared& s, const Row& r, const Goal& g, 
   __syncthreads();
   if (c < have && s.all.rank[c] + 1 == s.nkeep) s.cut = {key_in(s.all.order[c]), idx_in(s.all.order[c])};
   __syncthreads();
+}
+
+// The n-th largest of the threads' keys (n <= kThreads), 8 bits at a time.
+__device__ __forceinline__ uint32_t nth_largest(Shared& s, uint32_t key, uint32_t n) {
+  uint32_t prefix = 0;
+#pragma unroll 1
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    __syncthreads();
+    if (threadIdx.x < 256) s.part_n[threadIdx.x] = 0;
+    __syncthreads();
+    if (shift == 24 || key >> (shift + 8) == prefix) atomicAdd(&s.part_n[key >> shift & 255u], 1u);
+    __syncthreads();
+    if (threadIdx.x < 32) {
+      // lane l: bins 255 - 8 l and the 7 below
+      const int lane = threadIdx.x, first = 255 - 8 * lane;
+      uint32_t own = 0;
+      for (int b = 0; b < 8; ++b) own += s.part_n[first - b];
+      uint32_t upto = own;
+      for (int d = 1; d < 32; d <<= 1) {
+        const uint32_t o = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += o;
+      }
+      if (upto >= n && upto - own < n) {   // (one lane)
+        uint32_t left = n - (upto - own);
+        int b = first;
+        while (s.part_n[b] < left) left -= s.part_n[b--];
+        s.found = b;
+        s.found_cnt = left;
+      }
+    }
+    __syncthreads();
+    prefix = prefix << 8 | (uint32_t)s.found;
+    n = s.found_cnt;
+  }
+  return prefix;
 }
 
 // f times a mass, f in [0, 1), rounded down, and whether that left a rest.
@@ -565,7 +628,7 @@ __device__ __forceinline__ int choose(Shared& s, const Row& r, uint32_t have, in
   const unsigned long long order = c < have ? s.all.order[c] : 0;
   unsigned long long w = c < have ? s.all.w[c] : 0, before = 0;
   uint32_t rank = 0;
-  if (c < have && (top_k > 0 || cut_p)) rank_in(s, have, order, &rank, &before);
+  rank_in(s, max(have, 1u), &rank, &before);
   if (top_k > 0) {
     if (rank >= (uint32_t)top_k) w = 0;
     mass = block_sum(s, w);
@@ -637,6 +700,13 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleParams 
       top = fmaxf(top, fmaxf(max3(v[j].x, v[j].y, v[j].z), v[j].w));
     }
   }
+  const bool cut_k = top_k > 0 && top_k < p.vocab, cut_p = top_p < 1.f;
+  const uint32_t each = ((uint32_t)top_k + p.cluster - 1) / p.cluster;   // of a block's threads' largest
+  const bool bound = cut_k && top_k <= kCap / 2;
+  if (bound) {
+    const uint32_t key = nth_largest(s, key_of(top), each);
+    if (tid == 0) s.post_lo = key;
+  }
   for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
   if (lane == 0) s.red_f[warp] = top;
   clear_histogram(s.own);
@@ -670,8 +740,39 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleParams 
     cluster_sync();   // no block ends while its memory is being read
     return;
   }
+  if (bound) {
+    const float least_z = logit_of(__reduce_min_sync(0xffffffffu, posted(&s.post_lo, r.cluster, 0xFFFFFFFFu)));
+    if (least_z > -INFINITY) {
+      if (tid == 0) s.list_n = 0;
+      __syncthreads();
+      for (int q = tid; q < r.groups; q += kThreads) {
+        const float4 z4 = quads[q];
+        if (fmaxf(max3(z4.x, z4.y, z4.z), z4.w) < least_z) continue;
+        const float z[4] = {z4.x, z4.y, z4.z, z4.w};
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if (z[c] >= least_z) {
+            const uint32_t at = atomicAdd(&s.list_n, 1u);
+            if (at < kCap) {
+              s.list_key[at] = key_of(z[c]);
+              s.list_idx[at] = r.lo + 4 * q + c - r.pad;
+            }
+          }
+      }
+      cluster_sync();
+      if (warp_sum(posted(&s.list_n, r.cluster, 0u)) <= kCap) {
+        uint32_t have = 0;
+        if (r.rank == 0) have = collect(s, r);
+        cluster_sync();   // no block ends while its memory is being read
+        if (r.rank != 0) return;
+        const int token = choose(s, r, have, top_k, cut_p, top_p, least, u, 0);
+        if (tid == 0) p.tokens[row] = token;
+        return;
+      }
+      cluster_sync();   // nobody reads the list any more
+    }
+  }
   // 2: the histogram; the mass of all
-  const bool cut_k = top_k > 0 && top_k < p.vocab, cut_p = top_p < 1.f;
   s.cut = {0, 0x7FFFFFFF};   // everything
   if (cut_k || cut_p) {
     unsigned long long mass = 0;
