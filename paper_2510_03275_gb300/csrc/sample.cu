@@ -7,18 +7,18 @@
 //      block's threads' own largest are as many logits, so that the least of
 //      them over the blocks bounds the row's k-th from below.  Usually little
 //      more than k lie above the bound: they are gathered as in 3, without 2
-//   2  a histogram (count and mass) of the logits within 8 T of the largest, in
-//      steps of T / 16, and where top-p has no top-k ahead of it the mass of
-//      all; where a cut lies further down, of those within 8 to 12 T, and so
-//      on: each pass adds few logits to its histogram
+//   2  a histogram (count and mass) of the logits within 12 T of the largest,
+//      and where top-p has no top-k ahead of it the mass of all; where a cut
+//      lies further down, a histogram of the rest
 //   3  top-k's bucket (top-p's where there is no top-k) from the joined
 //      histogram.  Where no more than kCap logits lie in it and above, they are
 //      gathered in one thread block, a thread each, which counts every one's
 //      rank and the mass before it, cuts, and finds the token among what is
-//      left.  Otherwise
-//   4  top-k, then top-p: the bucket's members are gathered (narrowed by their
-//      logits' bits first where they are too many) and every one's rank and
-//      mass before it counted, which gives the cut as a (logit, index) pair
+//      left (sorting 512 of them took 12000 cycles).  Otherwise
+//   4  top-k, then top-p: the bucket is narrowed (by histograms of its parts,
+//      at last by the logits' bits) until kCap or fewer are left, they are
+//      gathered, and every one's rank and mass before it counted, which gives
+//      the cut as a (logit, index) pair
 //   5  mass of what is left in index order, and the token at u times it
 // A pass looks at the largest of 4 neighbours first: few logits are near enough
 // to the row's largest to need a weight.
@@ -55,7 +55,7 @@ struct SampleParams {
   int vocab, chunk, cluster;
 };
 
-constexpr int kLevels = 5;
+constexpr int kLevels = 2;
 
 // A cut: kept are the logits above (key), and those equal to it up to index idx.
 struct Cut {
@@ -146,18 +146,17 @@ __device__ __forceinline__ unsigned long long weight(float x) {
   // (from 9 on below 2^32: a cheaper conversion to the same number)
   return x > -9.f ? __float2ull_rn(weight_f(x) * kUnit) : x > kLeast ? (unsigned long long)__float2uint_rn(weight_f(x) * kUnit) : 0ull;
 }
-// Bucket of a logit of weight above 0: level l (distances of 0 to 8 T, 12 T, 16
-// T, 20 T, beyond), bin b of kBins: l kBins + b.
-__device__ __forceinline__ float level_from(int l) { return l == 0 ? 0.f : 4.f + 4.f * l; }
-__device__ __forceinline__ float level_width(int l) { return l == 0 ? 8.f : l < kLevels - 1 ? 4.f : 12.f; }
-__device__ __forceinline__ int level_of(float x) { return x > -8.f ? 0 : min(kLevels - 1, (int)(x * -0.25f) - 1); }
-__device__ __forceinline__ int bin_of(float x, int l) {
-  return min(kBins - 1, (int)((-x - level_from(l)) * (kBins / level_width(l))));
+// Where a logit of weight above 0 stands: its level (distances of 0 to 12 T,
+// beyond), and its place there, 0 .. kBins 2^14 - 1 from the level's nearest on:
+// the place's upper 7 bits are its bin, the next 7 its bin in a bin, and again.
+constexpr int kPlaceBits = 14;
+__device__ __forceinline__ float level_from(int l) { return l == 0 ? 0.f : 12.f; }
+__device__ __forceinline__ float level_width(int l) { return l == 0 ? 12.f : 20.f; }
+__device__ __forceinline__ int level_of(float x) { return x > -12.f ? 0 : 1; }
+__device__ __forceinline__ uint32_t place_of(float x, int l) {
+  return min((uint32_t)(kBins << kPlaceBits) - 1, (uint32_t)((-x - level_from(l)) * ((kBins << kPlaceBits) / level_width(l))));
 }
-__device__ __forceinline__ int bucket_of(float x) {
-  const int l = level_of(x);
-  return l * kBins + bin_of(x, l);
-}
+__device__ __forceinline__ int bin_of(float x, int l) { return (int)(place_of(x, l) >> kPlaceBits); }
 __device__ __forceinline__ void add_to(Histogram& h, int b, unsigned long long w) {
   atomicAdd(&h.cnt[b], 1u);
   const uint32_t lo = (uint32_t)w, old = atomicAdd(&h.lo[b], lo);
@@ -326,7 +325,8 @@ __device__ __forceinline__ void look_at(Shared& s, const Row& r, int l, Cumulati
 
 // Where a goal's cut falls.
 struct Place {
-  int bucket;                    // -1: nothing is cut off (then all levels were looked at)
+  int level;                     // -1: nothing is cut off (then all levels were looked at)
+  int bin;
   uint32_t above_cnt, n;         // logits above the bucket, in it
   unsigned long long above_mass;
   float from, to;                // its range of distances, in T
@@ -345,7 +345,7 @@ __device__ __forceinline__ Place locate(Shared& s, const Row& r, const Goal& g, 
     cnt += s.level_cnt[level];
     mass += s.level_mass[level];
     if (++level == kLevels) {
-      at.bucket = -1;
+      at.level = -1;
       return at;
     }
     if (*held != level) look_at(s, r, level, s.row[1]);
@@ -353,7 +353,8 @@ __device__ __forceinline__ Place locate(Shared& s, const Row& r, const Goal& g, 
     __syncthreads();
     pick(s, s.row[1], g, cnt, mass);
   }
-  at.bucket = level * kBins + s.found;
+  at.level = level;
+  at.bin = s.found;
   at.above_cnt = s.found_above_cnt;
   at.above_mass = s.found_above_mass;
   at.n = s.found_cnt;
@@ -437,17 +438,38 @@ __device__ __forceinline__ uint32_t collect(Shared& s, const Row& r) {
 // s.keep_mass.  Every block of the cluster finds the same.  use: 0 for a
 // kernel's first call, 1 for its second.
 __device__ __forceinline__ void resolve(Shared& s, const Row& r, const Goal& g, const Place& at0, int use) {
-  const int bucket = at0.bucket;
+  const int level = at0.level;
   uint32_t above_cnt = at0.above_cnt, n = at0.n;
   unsigned long long above_mass = at0.above_mass;
   const float from = at0.from, to = at0.to;
+  uint32_t prefix = (uint32_t)at0.bin;
+  int shift = kPlaceBits;   // the bucket: places of this prefix above `shift` bits
+  auto inside = [&](float x) { return level_of(x) == level && place_of(x, level) >> shift == prefix; };
+#pragma unroll 1
+  while (n > kCap && shift > 0) {
+    cluster_sync();   // nobody reads the last histogram any more
+    clear_histogram(s.own);
+    __syncthreads();
+    each_between(r, from, to, [&](int, float, float x, unsigned long long w) {
+      if (inside(x)) add_to(s.own, place_of(x, level) >> (shift - 7) & (kBins - 1), w);
+    });
+    cluster_sync();
+    join_histogram(s, s.sub, r.cluster);
+    pick(s, s.sub, g, above_cnt, above_mass);
+    n = s.found_cnt;
+    above_cnt = s.found_above_cnt;
+    above_mass = s.found_above_mass;
+    prefix = prefix << 7 | (uint32_t)s.found;
+    shift -= 7;
+    __syncthreads();
+  }
   uint32_t klo = 0, khi = 0xFFFFFFFFu;
   const bool by_key = n > kCap;
   if (by_key) {
     // the bucket's range of keys, then bins of that range until few are left or one value
     uint32_t lo = 0xFFFFFFFFu, hi = 0;
     each_between(r, from, to, [&](int, float z, float x, unsigned long long) {
-      if (bucket_of(x) != bucket) return;
+      if (!inside(x)) return;
       lo = min(lo, key_of(z));
       hi = max(hi, key_of(z));
     });
@@ -467,13 +489,13 @@ __device__ __forceinline__ void resolve(Shared& s, const Row& r, const Goal& g, 
     khi = __reduce_max_sync(0xffffffffu, posted(&s.post_hi, r.cluster, 0u));
     while (n > kCap && klo < khi) {
       static_assert(kBins == 128, "7 bits of the range");
-      const int shift = max(0, 32 - __clz(khi - klo) - 7);
+      const int bits = max(0, 32 - __clz(khi - klo) - 7);
       cluster_sync();   // nobody reads the last histogram any more
       clear_histogram(s.own);
       __syncthreads();
       each_between(r, from, to, [&](int, float z, float, unsigned long long w) {
         const uint32_t k = key_of(z);
-        if (k >= klo && k <= khi) add_to(s.own, (khi - k) >> shift, w);
+        if (k >= klo && k <= khi) add_to(s.own, (khi - k) >> bits, w);
       });
       cluster_sync();
       join_histogram(s, s.sub, r.cluster);
@@ -482,8 +504,8 @@ __device__ __forceinline__ void resolve(Shared& s, const Row& r, const Goal& g, 
       n = s.found_cnt;
       above_cnt = s.found_above_cnt;
       above_mass = s.found_above_mass;
-      khi -= (uint32_t)s.found << shift;
-      klo = max(klo, khi - ((1u << shift) - 1));   // (keys of finite logits are at least 2^23)
+      khi -= (uint32_t)s.found << bits;
+      klo = max(klo, khi - ((1u << bits) - 1));   // (keys of finite logits are at least 2^23)
     }
     cluster_sync();   // the same, ahead of the next call's; and of the posted range
   }
@@ -535,7 +557,7 @@ __device__ __forceinline__ void resolve(Shared& s, const Row& r, const Goal& g, 
   }
   gather(s, r, from, to, [&](float z, float x) {
     const uint32_t k = key_of(z);
-    return by_key ? k >= klo && k <= khi : bucket_of(x) == bucket;
+    return by_key ? k >= klo && k <= khi : inside(x);
   });
   cluster_sync();
   const uint32_t have = collect(s, r);
@@ -701,10 +723,9 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleParams 
     }
   }
   const bool cut_k = top_k > 0 && top_k < p.vocab, cut_p = top_p < 1.f;
-  const uint32_t each = ((uint32_t)top_k + p.cluster - 1) / p.cluster;   // of a block's threads' largest
   const bool bound = cut_k && top_k <= kCap / 2;
   if (bound) {
-    const uint32_t key = nth_largest(s, key_of(top), each);
+    const uint32_t key = nth_largest(s, key_of(top), ((uint32_t)top_k + p.cluster - 1) / p.cluster);   // of a block's threads' largest
     if (tid == 0) s.post_lo = key;
   }
   for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
@@ -741,48 +762,47 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleParams 
     return;
   }
   if (bound) {
+    // (-inf: too few logits for a bound; all are listed then, if they are few enough)
     const float least_z = logit_of(__reduce_min_sync(0xffffffffu, posted(&s.post_lo, r.cluster, 0xFFFFFFFFu)));
-    if (least_z > -INFINITY) {
-      if (tid == 0) s.list_n = 0;
-      __syncthreads();
-      for (int q = tid; q < r.groups; q += kThreads) {
-        const float4 z4 = quads[q];
-        if (fmaxf(max3(z4.x, z4.y, z4.z), z4.w) < least_z) continue;
-        const float z[4] = {z4.x, z4.y, z4.z, z4.w};
+    if (tid == 0) s.list_n = 0;
+    __syncthreads();
+    for (int q = tid; q < r.groups; q += kThreads) {
+      const float4 z4 = quads[q];
+      const float z[4] = {z4.x, z4.y, z4.z, z4.w};
+      if (!(fmaxf(max3(z4.x, z4.y, z4.z), z4.w) >= least_z)) continue;
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-          if (z[c] >= least_z) {
-            const uint32_t at = atomicAdd(&s.list_n, 1u);
-            if (at < kCap) {
-              s.list_key[at] = key_of(z[c]);
-              s.list_idx[at] = r.lo + 4 * q + c - r.pad;
-            }
+      for (int c = 0; c < 4; ++c)
+        if (z[c] >= least_z && z[c] > -INFINITY) {
+          const uint32_t at = atomicAdd(&s.list_n, 1u);
+          if (at < kCap) {
+            s.list_key[at] = key_of(z[c]);
+            s.list_idx[at] = r.lo + 4 * q + c - r.pad;
           }
-      }
-      cluster_sync();
-      if (warp_sum(posted(&s.list_n, r.cluster, 0u)) <= kCap) {
-        uint32_t have = 0;
-        if (r.rank == 0) have = collect(s, r);
-        cluster_sync();   // no block ends while its memory is being read
-        if (r.rank != 0) return;
-        const int token = choose(s, r, have, top_k, cut_p, top_p, least, u, 0);
-        if (tid == 0) p.tokens[row] = token;
-        return;
-      }
-      cluster_sync();   // nobody reads the list any more
+        }
     }
+    cluster_sync();
+    if (warp_sum(posted(&s.list_n, r.cluster, 0u)) <= kCap) {
+      uint32_t have = 0;
+      if (r.rank == 0) have = collect(s, r);
+      cluster_sync();   // no block ends while its memory is being read
+      if (r.rank != 0) return;
+      const int token = choose(s, r, have, top_k, cut_p, top_p, least, u, 0);
+      if (tid == 0) p.tokens[row] = token;
+      return;
+    }
+    cluster_sync();   // nobody reads what was posted any more
   }
-  // 2: the histogram; the mass of all
+  // 2: the histogram; where top-p has no top-k ahead of it, the mass of all
   s.cut = {0, 0x7FFFFFFF};   // everything
   if (cut_k || cut_p) {
     unsigned long long mass = 0;
     if (cut_k) {
-      each_between(r, 0.f, 8.f, [&](int, float, float x, unsigned long long w) {
+      each_between(r, 0.f, level_width(0), [&](int, float, float x, unsigned long long w) {
         if (level_of(x) == 0) add_to(s.own, bin_of(x, 0), w);
       });
     } else {
-      // (as each_between; groups beyond 9 T have weights below 2^32 units and take no part in the histogram)
-      const float far = r.t * 9.f * 1.0001f;
+      // (as each_between; groups beyond the level have weights below 2^32 units and take no part in the histogram)
+      const float far = r.t * level_width(0) * 1.0001f;
 #pragma unroll 2
       for (int q = tid; q < r.groups; q += kThreads) {
         const float4 z4 = quads[q];
@@ -820,14 +840,17 @@ __global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleParams 
       if (step == 1 && !cut_p) break;
       const Goal g = step == 0 ? Goal{true, (uint32_t)top_k, 0} : Goal{false, 0, mass_goal(top_p, mass)};
       const Place at = locate(s, r, g, &held);
-      if (at.bucket < 0) {   // (fewer than top_k)
+      if (at.level < 0) {   // (fewer than top_k)
         by_k = false;
         mass = 0;
         for (int l = 0; l < kLevels; ++l) mass += s.level_mass[l];
         continue;
       }
       if ((step == 0 || !by_k) && at.above_cnt + at.n <= kCap) {
-        gather(s, r, 0.f, at.to, [&](float, float x) { return bucket_of(x) <= at.bucket; });
+        gather(s, r, 0.f, at.to, [&](float, float x) {
+          const int l = level_of(x);
+          return l < at.level || (l == at.level && bin_of(x, l) <= at.bin);
+        });
         cluster_sync();
         uint32_t have = 0;
         if (r.rank == 0) have = collect(s, r);
