@@ -408,9 +408,9 @@ def sdq_cache_append(cache, batch, q_heads, q, k, v, rope, q_out, stream=None):
     """q, k, v: one row per token, of one type; their row strides are the tensors'."""
     kind = _dtype(q) if k.dtype == v.dtype == q.dtype else -1
     # (a single row has no stride of its own)
-    ldq, ldk, ldv = (t.stride(0) if t.shape[0] > 1 else t.shape[1] for t in (q, k, v))
+    ldq, ldk, ldv = (q.shape[1], k.shape[1], v.shape[1]) if q.shape[0] == 1 else (q.stride()[0], k.stride()[0], v.stride()[0])
     _check(lib().sdq_cache_append(cache, batch.ref, q_heads, q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
-                                  kind, rope.ref, _ptr(q_out), _stream(stream)), "sdq_cache_append")
+                                  kind, rope.ref, q_out.data_ptr(), _stream(stream)), "sdq_cache_append")
 
 
 def sdq_attention_workspace_bytes(cache, batch, q_heads) -> int:
@@ -527,13 +527,17 @@ class Batch:
                          token_start.data_ptr(), own_len.data_ptr(), pages.data_ptr() or None,
                          None if prefix_pages is None else prefix_pages.data_ptr() or None)
         self.ref = ctypes.addressof(self._c)
+        self._checked = None
 
     def check(self, page_tokens: int):
         """Raise where the page tables are too short for max_own or prefix_len."""
+        if self._checked == page_tokens:   # (neither changes)
+            return
         if self.max_own > self.page_columns * page_tokens:
             raise ValueError("Batch: pages has too few columns for max_own")
         if self.prefix_len > (0 if self.tensors[3] is None else self.tensors[3].shape[0]) * page_tokens:
             raise ValueError("Batch: prefix_pages is too short for prefix_len")
+        self._checked = page_tokens
 
 
 class Rope:
@@ -592,15 +596,15 @@ class KVCache:
         the rotated queries (tokens x q_heads x head_dim, bf16); keys and
         values go to the cache."""
         import torch
-        d = self.desc
-        for t, width in ((q, q.shape[-1]), (k, d.kv_heads * d.head_dim), (v, d.kv_heads * d.head_dim)):
-            if t.dim() != 2 or t.shape[0] != batch.n_tokens or t.shape[1] != width or t.stride(1) != 1 or not t.is_cuda:
-                raise ValueError("KVCache.append: q, k and v need one row of heads x head_dim elements per token")
-        q_heads, rest = divmod(q.shape[1], d.head_dim)
+        d, tokens, shape = self.desc, batch.n_tokens, q.shape
+        if (len(shape) != 2 or shape[0] != tokens or not k.shape == v.shape == (tokens, d.kv_heads * d.head_dim)
+                or not q.stride()[1] == k.stride()[1] == v.stride()[1] == 1 or not (q.is_cuda and k.is_cuda and v.is_cuda)):
+            raise ValueError("KVCache.append: q, k and v need one row of heads x head_dim elements per token")
+        q_heads, rest = divmod(shape[1], d.head_dim)
         if rest:
             raise ValueError("KVCache.append: q's rows are not whole heads")
         batch.check(d.page_tokens)
-        out = torch.empty((batch.n_tokens, q_heads, d.head_dim), dtype=torch.bfloat16, device=q.device)
+        out = torch.empty((tokens, q_heads, d.head_dim), dtype=torch.bfloat16, device=q.device)
         sdq_cache_append(self.handle, batch, q_heads, q, k, v, rope, out, stream)
         return out
 
@@ -617,21 +621,21 @@ class KVCache:
         outputs of the same shape in bf16.  scale: 1 / sqrt(head_dim) unless
         given; lse: fp32 (tokens x q_heads), written if given."""
         import torch
-        d = self.desc
-        if q.dim() != 3 or q.shape[0] != batch.n_tokens or q.shape[2] != d.head_dim or q.dtype != torch.bfloat16 or not q.is_cuda:
+        d, tokens, dim, shape = self.desc, batch.n_tokens, self.desc.head_dim, q.shape
+        if len(shape) != 3 or shape[0] != tokens or shape[2] != dim or q.dtype != torch.bfloat16 or not q.is_cuda:
             raise ValueError("KVCache.attend: q must be a bfloat16 CUDA tensor (tokens, q_heads, head_dim)")
-        heads = q.shape[1]
-        if q.stride(2) != 1 or (heads > 1 and q.stride(1) != d.head_dim):
+        heads, stride = shape[1], q.stride()
+        if stride[2] != 1 or (heads > 1 and stride[1] != dim):
             raise ValueError("KVCache.attend: the heads of a token of q must be adjacent")
-        if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (batch.n_tokens, heads)
+        if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (tokens, heads)
                                 or not lse.is_contiguous() or not lse.is_cuda):
             raise ValueError("KVCache.attend: lse must be a contiguous float32 CUDA tensor (tokens, q_heads)")
         batch.check(d.page_tokens)
         if ws is None:
             ws = self.alloc_workspace(batch, heads)
-        out = torch.empty((batch.n_tokens, heads, d.head_dim), dtype=torch.bfloat16, device=q.device)
-        sdq_attention(self.handle, batch, heads, q, q.stride(0) if batch.n_tokens > 1 else heads * d.head_dim,
-                      d.head_dim ** -0.5 if scale is None else scale, out, lse, ws, stream)
+        out = torch.empty((tokens, heads, dim), dtype=torch.bfloat16, device=q.device)
+        sdq_attention(self.handle, batch, heads, q, stride[0] if tokens > 1 else heads * dim,
+                      dim ** -0.5 if scale is None else scale, out, lse, ws, stream)
         return out
 
 
@@ -640,12 +644,13 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, stre
     strided) from one random number per row -> int32 tokens.  The settings:
     one per row (float32, top_k int32), or None for none."""
     import torch
-    if logits.dim() != 2 or logits.stride(1) != 1 or not logits.is_cuda:
+    shape = logits.shape
+    if len(shape) != 2 or logits.stride()[1] != 1 or not logits.is_cuda:
         raise ValueError("sample: logits must be a CUDA tensor (rows, vocab) with adjacent elements in a row")
-    for t, dtype in ((u, torch.float32), (temperature, torch.float32), (top_k, torch.int32), (top_p, torch.float32),
-                     (min_p, torch.float32)):
-        if t is not None and (t.dtype != dtype or t.shape != logits.shape[:1] or not t.is_contiguous() or not t.is_cuda):
+    rows, f32 = shape[:1], torch.float32
+    for t, dtype in ((u, f32), (temperature, f32), (top_k, torch.int32), (top_p, f32), (min_p, f32)):
+        if t is not None and (t.dtype is not dtype or t.shape != rows or not t.is_contiguous() or not t.is_cuda):
             raise ValueError("sample: u, temperature, top_p and min_p are float32, top_k int32, one per row, on the GPU")
-    tokens = torch.empty(logits.shape[0], dtype=torch.int32, device=logits.device)
+    tokens = torch.empty(rows, dtype=torch.int32, device=logits.device)
     sdq_sample(logits, u, temperature, top_k, top_p, min_p, tokens, stream)
     return tokens
