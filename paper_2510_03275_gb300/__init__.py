@@ -205,6 +205,18 @@ def _stream(stream):
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _empty(shape, dtype, device, stream):
+    """Device memory that belongs to the stream a call runs on (a block that the current stream still uses is not
+    handed out to another)."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(getattr(stream, "cuda_stream", stream), device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 # ------------------------------------------------------------- C-ABI names
 def sdq_plan_create(desc: LayerDesc, had_signs=None) -> int:
     import numpy as np
@@ -604,17 +616,17 @@ class KVCache:
         if rest:
             raise ValueError("KVCache.append: q's rows are not whole heads")
         batch.check(d.page_tokens)
-        out = torch.empty((tokens, q_heads, d.head_dim), dtype=torch.bfloat16, device=q.device)
+        out = _empty((tokens, q_heads, d.head_dim), torch.bfloat16, q.device, stream)
         sdq_cache_append(self.handle, batch, q_heads, q, k, v, rope, out, stream)
         return out
 
-    def alloc_workspace(self, batch: Batch, q_heads: int):
+    def alloc_workspace(self, batch: Batch, q_heads: int, stream=None):
         """For ``attend`` on this batch (or one of the same integers)."""
         import torch
         n = sdq_attention_workspace_bytes(self.handle, batch, q_heads)
         if n == 0:
             raise SdqError(-1, "sdq_attention_workspace_bytes")
-        return torch.empty(n, dtype=torch.uint8, device=self.k_pages.device)
+        return _empty(n, torch.uint8, self.k_pages.device, stream)
 
     def attend(self, batch: Batch, q, scale=None, ws=None, lse=None, stream=None):
         """q (tokens x q_heads x head_dim, bf16; tokens may be strided) ->
@@ -632,8 +644,8 @@ class KVCache:
             raise ValueError("KVCache.attend: lse must be a contiguous float32 CUDA tensor (tokens, q_heads)")
         batch.check(d.page_tokens)
         if ws is None:
-            ws = self.alloc_workspace(batch, heads)
-        out = torch.empty((tokens, heads, dim), dtype=torch.bfloat16, device=q.device)
+            ws = self.alloc_workspace(batch, heads, stream)
+        out = _empty((tokens, heads, dim), torch.bfloat16, q.device, stream)
         sdq_attention(self.handle, batch, heads, q, stride[0] if tokens > 1 else heads * dim,
                       dim ** -0.5 if scale is None else scale, out, lse, ws, stream)
         return out
@@ -651,6 +663,6 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, stre
     for t, dtype in ((u, f32), (temperature, f32), (top_k, torch.int32), (top_p, f32), (min_p, f32)):
         if t is not None and (t.dtype is not dtype or t.shape != rows or not t.is_contiguous() or not t.is_cuda):
             raise ValueError("sample: u, temperature, top_p and min_p are float32, top_k int32, one per row, on the GPU")
-    tokens = torch.empty(rows, dtype=torch.int32, device=logits.device)
+    tokens = _empty(rows, torch.int32, logits.device, stream)
     sdq_sample(logits, u, temperature, top_k, top_p, min_p, tokens, stream)
     return tokens
