@@ -9,35 +9,52 @@ namespace sdq {
 
 namespace {
 
-// One warp per row: the prefix's result and the own part's.
+// One warp per row: the prefix's results, then the own part's, one for each
+// thread block that shared a row block's keys; kBatch rows' pieces under way at once.
 template <int D>
 __global__ void __launch_bounds__(256) join_kernel(const AttendParams p) {
   pdl_wait();
   pdl_launch_dependents();
-  constexpr int V = D / 32;
-  const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (row >= (int64_t)p.b.n_tokens * p.q_heads) return;
+  constexpr int V = D / 32, kBatch = 4;
+  const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), rows = (int64_t)p.b.n_tokens * p.q_heads;
+  if (row >= rows) return;
   // (a token that no sequence counts as its own has no own result: seq_span)
   const int tok = (int)(row / p.q_heads);
   const SeqSpan q = seq_span(p.b, seq_of_token(p.b.token_start, p.b.n_seqs, tok));
-  float2 ml[2];
-  float v[2][V], acc[V], sum = 0.f;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    ml[i] = __ldcg(p.ml[i] + row);
-    load_row<D, V>(p.o[i] + row * D, v[i]);
-  }
-  if (tok >= q.first + q.count) ml[kOwn] = make_float2(-INFINITY, 0.f);
-  const float top = fmaxf(ml[0].x, ml[1].x), base = top == -INFINITY ? 0.f : top;
+  const bool own = tok < q.first + q.count;
+  const int np = p.narrow[kPrefix] + max(p.wide[kPrefix], p.splits[kPrefix]);
+  const int n = np + (own ? p.narrow[kOwn] + max(p.wide[kOwn], p.splits[kOwn]) : 0);
+  float acc[V], sum = 0.f, top = -INFINITY;
 #pragma unroll
   for (int k = 0; k < V; ++k) acc[k] = 0.f;
+#pragma unroll 1
+  for (int i0 = 0; i0 < n; i0 += kBatch) {
+    float2 ml[kBatch];
+    float v[kBatch][V];
 #pragma unroll
-  for (int i = kPrefix; i >= kOwn; --i) {
-    const float f = exp2_approx(ml[i].x - base);
-    if (f == 0.f) continue;   // (a part that saw nothing holds anything)
-    sum += ml[i].y * f;
+    for (int j = 0; j < kBatch; ++j) {
+      const int i = min(i0 + j, n - 1), part = i < np ? kPrefix : kOwn, at = i < np ? i : i - np;
+      const bool split = p.splits[part] > 1;
+      const int64_t place = (split ? at * rows : 0) + row;
+      ml[j] = __ldcg((split ? p.split_ml[part] : p.ml[part]) + place);
+      load_row<D, V>((split ? p.split_o[part] : p.o[part]) + place * D, v[j]);
+    }
+    float now = top;
 #pragma unroll
-    for (int k = 0; k < V; ++k) acc[k] += f * v[i][k];
+    for (int j = 0; j < kBatch; ++j) now = fmaxf(now, ml[j].x);
+    const float base = now == -INFINITY ? 0.f : now, old = exp2_approx(top - base);   // (0 before the first)
+    top = now;
+    sum *= old;
+#pragma unroll
+    for (int k = 0; k < V; ++k) acc[k] *= old;
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const float f = i0 + j < n ? exp2_approx(ml[j].x - base) : 0.f;
+      if (f == 0.f) continue;   // (a part that saw nothing holds anything)
+      sum += ml[j].y * f;
+#pragma unroll
+      for (int k = 0; k < V; ++k) acc[k] += f * v[j][k];
+    }
   }
   write_row<D, V>(p, row, acc, top, sum);
 }
@@ -67,7 +84,7 @@ void set_route(const sdq_cache_s* c, const sdq_batch* b, int q_heads, AttendPara
   p->narrow[kPrefix] = prefix_rows > 0 && prefix_rows <= kPrefixNarrowRows;
   p->parts = p->wide[kOwn] + p->narrow[kOwn] + p->wide[kPrefix] + p->narrow[kPrefix];
   for (int part = 0; part < 2; ++part) {
-    p->splits[part] = p->wide[part] ? wide_splits(c, b, q_heads, part, p->chained) : 0;
+    p->splits[part] = p->wide[part] ? wide_splits(c, b, q_heads, part, p->chained, part == kPrefix && p->narrow[kOwn]) : 0;
   }
   p->ctas = c->sm_count;
   // Beside a wide kernel that leaves SMs free, the narrow one's first thread
@@ -75,7 +92,7 @@ void set_route(const sdq_cache_s* c, const sdq_batch* b, int q_heads, AttendPara
   // take ahead what they can read until then (40 bytes a ns and SM).
   if (p->wide[kPrefix] && p->narrow[kOwn]) {
     p->early = c->sm_count - (int)std::min<int64_t>(wide_grid(c, *p, kPrefix), c->sm_count);
-    p->ahead = (int)(wide_time(c, b, q_heads, kPrefix, false, p->splits[kPrefix]) * 40e3 / (64.0 * c->desc.head_dim * narrow_warps()));
+    p->ahead = (int)((wide_time(c, b, q_heads, kPrefix, false, p->splits[kPrefix]) + kNarrowStart) * 40e3 / (64.0 * c->desc.head_dim * narrow_warps()));
   }
 }
 
@@ -92,8 +109,8 @@ AttendWs attend_workspace(const sdq_cache_s* c, const sdq_batch* b, int q_heads,
   L.tickets[kOwn] = take(p.narrow[kOwn] ? sizeof(uint64_t) * b->n_seqs * c->desc.kv_heads : 0);
   L.tickets[kPrefix] = take(p.narrow[kPrefix] ? sizeof(uint64_t) * c->desc.kv_heads : 0);
   for (int part = 0; part < 2; ++part) {
-    L.ml[part] = take(p.parts > 1 ? sizeof(float2) * rows : 0);
-    L.o[part] = take(p.parts > 1 ? sizeof(float) * rows * d : 0);
+    L.ml[part] = take(p.parts > 1 && p.splits[part] <= 1 ? sizeof(float2) * rows : 0);
+    L.o[part] = take(p.parts > 1 && p.splits[part] <= 1 ? sizeof(float) * rows * d : 0);
     L.split_ml[part] = take(p.splits[part] > 1 ? sizeof(float2) * p.splits[part] * rows : 0);
     L.split_o[part] = take(p.splits[part] > 1 ? sizeof(float) * p.splits[part] * rows * d : 0);
     const size_t slots = p.narrow[part] ? (size_t)p.ctas * 8 * narrow_groups(b, p.group, part) : 0;
@@ -117,7 +134,7 @@ cudaError_t launch_parts(const sdq_cache_s* c, const AttendParams& p, cudaStream
     if (p.wide[part]) e = launch_wide(c, p, part, st);
     else if (p.narrow[part]) e = launch_narrow(c, p, part, part == kOwn && p.parts > 1, st);
   }
-  if (e != cudaSuccess || p.parts == 1) return e;
+  if (e != cudaSuccess || (p.parts == 1 && p.splits[kOwn] <= 1 && p.splits[kPrefix] <= 1)) return e;
   return c->desc.head_dim == 128 ? launch_join<128>(p, st) : launch_join<64>(p, st);
 }
 

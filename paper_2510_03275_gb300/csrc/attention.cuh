@@ -20,7 +20,7 @@ struct AttendWs {
   size_t rec;                // call record
   size_t tickets[2];         // of (sequence, key head) and of the prefix's key heads
   size_t o[2], ml[2];        // two parts' results by row, for their join
-  size_t split_o[2], split_ml[2];   // wide kernel: [thread block of the cluster][row]
+  size_t split_o[2], split_ml[2];   // wide kernel: [thread block of a row block's][row]
   size_t warp_o[2];          // narrow kernel: a piece per warp
   size_t block_o[2], block_ml[2];   // and two parts per thread block
   size_t total;
@@ -74,15 +74,6 @@ __device__ __forceinline__ void load_row(const float* row, float (&v)[V]) {
     v[1] = x.y;
   }
 }
-// A row's sums (a whole warp, V columns a lane) as a part's result.
-template <int D, int V>
-__device__ __forceinline__ void keep_row(const AttendParams& p, int part, int64_t row, const float (&acc)[V], float top, float sum) {
-  const int lane = threadIdx.x & 31;
-  float* dst = p.o[part] + row * D + V * lane;
-  if (V == 4) *reinterpret_cast<float4*>(dst) = make_float4(acc[0], acc[1], acc[V - 2], acc[V - 1]);
-  else *reinterpret_cast<float2*>(dst) = make_float2(acc[0], acc[1]);
-  if (lane == 0) p.ml[part][row] = make_float2(sum == sum ? top : sum, sum);   // (NaN scores leave no maximum)
-}
 // A finished row: this lane's V columns.
 template <int D, int V>
 __device__ __forceinline__ void write_row(const AttendParams& p, int64_t row, const float (&acc)[V], float top, float sum) {
@@ -100,8 +91,10 @@ int narrow_groups(const sdq_batch* b, int group, int part);   // of 8 query rows
 int narrow_warps();                                           // per thread block
 cudaError_t launch_narrow(const sdq_cache_s* c, const AttendParams& p, int part, bool late, cudaStream_t st);
 // The wide kernel on `part`, and how many thread blocks share the keys of a
-// row block (p.splits[part]).
-int wide_splits(const sdq_cache_s* c, const sdq_batch* b, int q_heads, int part, bool chained);
+// row block (p.splits[part]); narrow: the narrow kernel runs beside it.
+constexpr int kMaxWideSplits = 16;
+constexpr double kNarrowStart = 4.0;   // us that the narrow kernel takes beyond its reading
+int wide_splits(const sdq_cache_s* c, const sdq_batch* b, int q_heads, int part, bool chained, bool narrow);
 double wide_time(const sdq_cache_s* c, const sdq_batch* b, int q_heads, int part, bool chained, int splits);   // us, estimated
 int64_t wide_grid(const sdq_cache_s* c, const AttendParams& p, int part);   // thread blocks
 cudaError_t launch_wide(const sdq_cache_s* c, const AttendParams& p, int part, cudaStream_t st);

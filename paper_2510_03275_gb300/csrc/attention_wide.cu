@@ -27,10 +27,10 @@ namespace {
 //                   swizzle); warps 10 and 11 only complete its warpgroup
 // The MMAs of a thread block run in the order of their issue, so that S of the
 // next tile may overwrite P once the product that reads it is issued.
-// Few row blocks: a cluster of up to 8 thread blocks shares the line of one,
-// writes its sums to the workspace and meets at the cluster's barrier, after
-// which each thread block joins its part of the rows.  (Through the cluster's
-// shared memory the join took twice as long, 6 us of a 29 us kernel.)
+// Few row blocks: several thread blocks share the line of one, write their sums
+// to the workspace, and the kernel that joins a call's parts takes them all.  (As
+// clusters that joined at the end of this kernel, in the workspace or in their
+// shared memory, they took 4 to 10 us longer, and the device holds fewer.)
 // Registers: 384 threads hold 168 each at launch; the first two warpgroups go
 // to 224 once the third has gone down to 56 (224 + 224 + 56 = 3 x 168).
 constexpr int kWideThreads = 384;
@@ -174,54 +174,6 @@ __device__ __forceinline__ bool wide_item(const AttendParams& p, int part, WideI
   return true;
 }
 
-// The cluster's rows (in the workspace, each thread block's sums over its own
-// keys): this thread block's share of them, two at a time per warp (8 warps),
-// summed in the order of the keys.
-template <int D>
-__device__ __forceinline__ void join_rows(const AttendParams& p, int part, const WideItem& w) {
-  constexpr int V = D / 32, kBatch = 2;
-  const int warp = threadIdx.x >> 5;
-  const int splits = p.splits[part], valid = min(256, w.rows - w.r0);
-  const int64_t rows = (int64_t)p.b.n_tokens * p.q_heads;
-  for (int r0 = warp * splits + w.split; r0 < valid; r0 += 8 * kBatch * splits) {
-    float2 ml[kBatch][kMaxWideSplits];
-    float v[kBatch][kMaxWideSplits][V];
-    int64_t out[kBatch];
-#pragma unroll
-    for (int j = 0; j < kBatch; ++j) {
-      const int row = w.r0 + min(r0 + 8 * j * splits, valid - 1), tok = row / p.group;
-      out[j] = (int64_t)(w.first + tok) * p.q_heads + w.h * p.group + row - tok * p.group;
-#pragma unroll
-      for (int i = 0; i < kMaxWideSplits; ++i)
-        if (i < splits) {
-          ml[j][i] = __ldcg(p.split_ml[part] + i * rows + out[j]);
-          load_row<D, V>(p.split_o[part] + (i * rows + out[j]) * D, v[j][i]);
-        }
-    }
-#pragma unroll
-    for (int j = 0; j < kBatch; ++j) {
-      if (r0 + 8 * j * splits >= valid) break;
-      float acc[V], sum = 0.f, top = -INFINITY;
-#pragma unroll
-      for (int k = 0; k < V; ++k) acc[k] = 0.f;
-#pragma unroll
-      for (int i = 0; i < kMaxWideSplits; ++i)
-        if (i < splits) top = fmaxf(top, ml[j][i].x);
-      const float base = top == -INFINITY ? 0.f : top;
-#pragma unroll
-      for (int i = 0; i < kMaxWideSplits; ++i)
-        if (i < splits) {
-          const float f = exp2_approx(ml[j][i].x - base);
-          sum += f == 0.f ? 0.f : ml[j][i].y * f;
-#pragma unroll
-          for (int k = 0; k < V; ++k) acc[k] += f * v[j][i][k];
-        }
-      if (p.parts > 1) keep_row<D, V>(p, part, out[j], acc, top, sum);
-      else write_row<D, V>(p, out[j], acc, top, sum);
-    }
-  }
-}
-
 template <int D>
 __global__ void __launch_bounds__(kWideThreads, 1)
     wide_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const AttendParams p,
@@ -259,12 +211,12 @@ __global__ void __launch_bounds__(kWideThreads, 1)
   pdl_launch_dependents();
   call_record_start(p.rec, p.call, blockIdx.x == 0 && tid == 0);
   WideItem w;
-  if (!wide_item(p, part, &w)) {   // (all warps of the cluster alike)
+  if (!wide_item(p, part, &w)) {   // (all warps alike)
     if (warp == 8) tmem_dealloc(tmem_base, 512);
     return;
   }
   const int n = w.t1 - w.t0, halves = w.rows - w.r0 > 128 ? 2 : 1;
-  // row by row at the end: a cluster's sums, or fp32 rows for the join with the other part
+  // at the end: fp32 sums for the join, or rows of the output
   const bool joins = p.splits[part] > 1 || p.parts > 1;
   const uint32_t tmem = tmem_base;
   bool ok = true;
@@ -360,7 +312,6 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         if (!mbar_wait_warp(&mma_done, 0)) ok = false;
       }
     }
-    if (p.splits[part] > 1) cluster_sync();
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 224;\n");
     if ((warp >> 2) < halves) {
@@ -556,11 +507,6 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       }
     }
     else mbar_arrive(&q_full);
-    if (p.splits[part] > 1) {
-      __threadfence();
-      cluster_sync();   // all parts of the rows are in memory
-      join_rows<D>(p, part, w);
-    }
   }
   if (!ok && lane == 0) call_record_fail(p.rec, p.call);
   tc_fence_before();
@@ -579,72 +525,49 @@ int64_t wide_blocks(const sdq_batch* b, int group, int part) {
 }
 
 template <int D>
-void launch_config(cudaLaunchConfig_t* cfg, cudaLaunchAttribute* attr, int64_t grid, int splits, cudaStream_t st) {
-  *cfg = {};
-  cfg->gridDim = dim3((unsigned)grid);
-  cfg->blockDim = dim3(kWideThreads);
-  cfg->dynamicSmemBytes = WideShape<D>::kSmem;
-  cfg->stream = st;
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = (unsigned)splits;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[1].val.programmaticStreamSerializationAllowed = 1;
-  cfg->attrs = attr;
-  cfg->numAttrs = 2;
-}
-
-template <int D>
-cudaError_t smem_limit(int device) {
-  static std::atomic<int> smem_set[64];
-  return smem_limit_once(wide_kernel<D>, WideShape<D>::kSmem, device, smem_set);
-}
-
-template <int D>
 cudaError_t launch(const sdq_cache_s* c, const AttendParams& p, int part, cudaStream_t st) {
-  const cudaError_t e = smem_limit<D>(c->device);
+  static std::atomic<int> smem_set[64];
+  const cudaError_t e = smem_limit_once(wide_kernel<D>, WideShape<D>::kSmem, c->device, smem_set);
   if (e != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg;
-  cudaLaunchAttribute attr[2];
-  launch_config<D>(&cfg, attr, wide_grid(c, p, part), p.splits[part], st);
-  return cudaLaunchKernelEx(&cfg, wide_kernel<D>, c->kmap, c->vmap, p, part);
-}
-
-template <int D>
-cudaError_t occupancy(sdq_cache_s* c) {
-  cudaError_t e = smem_limit<D>(c->device);
-  c->wide_clusters[1] = c->sm_count;
-  for (int s = 2; s <= kMaxWideSplits && e == cudaSuccess; ++s) {
-    cudaLaunchConfig_t cfg;
-    cudaLaunchAttribute attr[2];
-    launch_config<D>(&cfg, attr, s, s, 0);
-    cfg.numAttrs = 1;   // the cluster alone
-    e = cudaOccupancyMaxActiveClusters(&c->wide_clusters[s], wide_kernel<D>, &cfg);
-  }
-  return e;
+  return launch_pdl(wide_kernel<D>, dim3((unsigned)wide_grid(c, p, part)), dim3(kWideThreads), (size_t)WideShape<D>::kSmem, st, c->kmap,
+                    c->vmap, p, part);
 }
 
 }  // namespace
-
-cudaError_t wide_occupancy(sdq_cache_s* c) { return c->desc.head_dim == 128 ? occupancy<128>(c) : occupancy<64>(c); }
 
 int64_t wide_grid(const sdq_cache_s* c, const AttendParams& p, int part) {
   return wide_blocks(&p.b, p.group, part) * c->desc.kv_heads * p.splits[part];
 }
 
-// us, over waves of clusters of s: a tile (256 rows) takes 1.3 us, a thread
-// block's two ends 5 us, the join of a cluster 5 us more.
+// us, over waves of thread blocks: a tile (256 rows) takes 1.3 us, a thread
+// block's two ends 5 us.
 double wide_time(const sdq_cache_s* c, const sdq_batch* b, int q_heads, int part, bool chained, int s) {
-  const int64_t items = wide_blocks(b, q_heads / c->desc.kv_heads, part) * c->desc.kv_heads, held = std::max(1, c->wide_clusters[s]);
+  const int64_t blocks = wide_blocks(b, q_heads / c->desc.kv_heads, part) * c->desc.kv_heads * s;
   const int64_t tiles = (part == kPrefix || chained ? ((int64_t)b->prefix_len + kKeys - 1) / kKeys : 0) +
                         (part == kOwn ? ((int64_t)b->max_own + kKeys - 1) / kKeys : 0);
-  return (double)((items + held - 1) / held) * (5.0 + (s > 1 ? 5.0 : 0.0) + 1.3 * (double)((tiles + s - 1) / s));
+  return (double)((blocks + c->sm_count - 1) / c->sm_count) * (5.0 + 1.3 * (double)((tiles + s - 1) / s));
 }
 
-int wide_splits(const sdq_cache_s* c, const sdq_batch* b, int q_heads, int part, bool chained) {
+// The least of: its time; the join of the parts' sums, a launch (3 us) and 4
+// TB/s; and what the narrow kernel beside it, where that takes the other part,
+// needs longer: kNarrowStart and its reading (40 bytes a ns and SM) on the SMs
+// left free, or on all of them afterwards.  (The lengths are not known here: a
+// sixth of their bound, as for lengths spread over their logarithm.)  64 rows of 8 heads a key
+// head against 8199 keys, and 1 to 512 of each sequence: 7 parts take 32 us, 6
+// 34, 8 42; 16 of 32 against 2051 and 1 to 300: 3 take 20 us, 4 28.
+int wide_splits(const sdq_cache_s* c, const sdq_batch* b, int q_heads, int part, bool chained, bool narrow) {
+  const double own = narrow ? (double)b->n_seqs * c->desc.kv_heads * b->max_own / 6 * c->desc.head_dim * 4 : 0.0;   // bytes
+  auto time = [&](int s) {
+    const double t = wide_time(c, b, q_heads, part, chained, s);
+    const int64_t grid = wide_blocks(b, q_heads / c->desc.kv_heads, part) * c->desc.kv_heads * s;
+    const double free = 40e3 * (double)std::max<int64_t>(0, c->sm_count - grid);   // bytes a us
+    const double both = own <= free * t ? std::max(t, kNarrowStart + own / std::max(1.0, free))
+                                        : t + kNarrowStart + (own - free * t) / (40e3 * c->sm_count);
+    return both + (s > 1 ? 3.0 + (double)b->n_tokens * q_heads * c->desc.head_dim * 4.0 * s / 4e6 : 0.0);
+  };
   int best = 1;
   for (int s = 2; s <= kMaxWideSplits; ++s)
-    if (wide_time(c, b, q_heads, part, chained, s) < wide_time(c, b, q_heads, part, chained, best)) best = s;
+    if (time(s) < time(best)) best = s;
   return best;
 }
 

@@ -166,10 +166,6 @@ extern "C" int sdq_cache_create(const sdq_cache_desc* desc, uint16_t* k_pages, u
       return SDQ_ERR_CUDA;
     }
   }
-  if (wide_occupancy(c) != cudaSuccess) {
-    delete c;
-    return SDQ_ERR_CUDA;
-  }
   *out = c;
   return SDQ_OK;
 }

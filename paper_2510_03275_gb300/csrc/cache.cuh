@@ -3,17 +3,12 @@
 
 #include "common.cuh"
 
-namespace sdq {
-constexpr int kMaxWideSplits = 8;   // thread blocks of a cluster that share a row block's keys
-}
-
 struct sdq_cache_s {
   sdq_cache_desc desc;
   int device, sm_count;
   uint16_t *k, *v;
   int64_t rows;          // token rows of each array: n_pages * kv_heads * page_tokens
   CUtensorMap kmap, vmap;     // rows x head_dim in boxes of min(page_tokens, 64) rows x 64 elements, 128-byte swizzle
-  int wide_clusters[sdq::kMaxWideSplits + 1];   // clusters of s thread blocks that the device holds at once (wide kernel)
   CUtensorMap ktile, vtile;   // 64 elements x rows x halves of a row in boxes of 16 rows, all of their elements
 };
 
@@ -23,8 +18,6 @@ namespace sdq {
 inline int cache_box_rows(const sdq_cache_desc& d) { return d.page_tokens < 64 ? d.page_tokens : 64; }
 // SDQ_OK, or why `b` cannot be run on `c` (host values only).
 int check_batch(const sdq_cache_s* c, const sdq_batch* b, int32_t q_heads);
-// Fills the cache's wide_clusters.
-cudaError_t wide_occupancy(sdq_cache_s* c);
 // SDQ_OK when the current device is the cache's.
 int check_cache_device(const sdq_cache_s* c);
 
