@@ -10,7 +10,8 @@ namespace sdq {
 namespace {
 
 // One warp per row: the prefix's results, then the own part's, one for each
-// thread block that shared a row block's keys; kBatch rows' pieces under way at once.
+// thread block that shared a row block's keys, in this order; kBatch pieces under
+// way at once.  L2 bounds it, or the launch: 4096 rows of 7 + 1 parts 5 us.
 template <int D>
 __global__ void __launch_bounds__(256) join_kernel(const AttendParams p) {
   pdl_wait();

@@ -21,8 +21,13 @@ namespace {
 //   columns (the other way round half of a 16-row tile would be padding), O^T
 //   += V^T P^T; K and V fragments come by ldmatrix, P^T is turned from the
 //   accumulator's layout into the operand's by movmatrix.
-// P is rounded to bf16 for its product (relative 2^-8 at most per weight, as
+// P is rounded to bf16 for its product (relative 2^-9 at most per weight, as
 // the values themselves carry); sums, maxima and outputs are fp32.
+// 64 tokens of 64 heads (8 key heads of 128) on 1 to 4096 keys each: 43 us, 4.7
+// TB/s; 2 x 3 tokens on 65537 to 131072: 164 us, 5.9 TB/s.  One token on 1037
+// keys takes 11.6 us, a chain of latencies: a block's tables and queries 4000
+// cycles, its tiles 2500, its pieces 3300, the ticket 3000 to 6000, the join of
+// the blocks 3500.
 constexpr int kWarps = 8, kThreads = 32 * kWarps, kTile = 16;
 // A (sequence, head) takes as many places of the line as it has tiles, and
 // kUnitCost more: its queries, its output and the join cost its warp about as
