@@ -77,6 +77,7 @@ void set_route(const sdq_cache_s* c, const sdq_batch* b, int q_heads, AttendPara
   const bool own_wide = own_rows > kNarrowRows;
   p->b = *b;
   p->group = group;
+  p->group_inverse = 65536u / (uint32_t)group + 1;
   p->chained = own_wide && prefix_rows > 0 && prefix_rows >= 128ll * b->n_seqs;
   p->wide[kOwn] = own_wide;
   // (a call without any keys goes through the narrow kernel too: it writes the zeros)

@@ -34,6 +34,7 @@ struct AttendParams {
   float* lse;               // natural log-sum-exp per row, may be null
   float scale;              // softmax scale times log2(e)
   int q_heads, kv_heads, group, page_shift, box_shift, n_pages;
+  uint32_t group_inverse;   // 2^16 / group + 1
   int narrow[2], wide[2];   // which kernel takes a part (neither: it has no keys)
   int parts;                // parts that are computed apart (1, 2)
   int chained;              // the wide kernel's rows of kOwn run over the prefix first (no kPrefix part)

@@ -81,6 +81,9 @@ struct Unit {
   int64_t a;                 // its first place in the line (its tiles', then kUnitCost more)
 };
 
+// Row r of a unit: its token (r below 32: exact).
+__device__ __forceinline__ int token_of(const AttendParams& p, int r) { return (int)((uint32_t)r * p.group_inverse >> 16); }
+
 // The line of units that have tiles.  All of it by whole warps: a lane holds
 // the span of one of 32 consecutive sequences.
 struct Walk {
@@ -266,11 +269,9 @@ template <int D, int NT, int K>
 __device__ __forceinline__ void finish(const AttendParams& p, const Pieces<NT>& pc, const uint8_t* smem, int part, const Unit& u, int n,
                                     Source src, int64_t slot, int k0) {
   using S = NarrowShape<D, NT>;
-  constexpr int R = S::kRows, B = K == 1 ? 8 : 2;
+  constexpr int R = S::kRows, B = K == 1 ? 4 : 1;   // (4 for K = 8: more code, and up to 3 us more)
   const int lane = threadIdx.x & 31, r = 8 * n + (lane >> 2), c = (lane & 3) + 4 * k0;
   if (r >= u.rows) return;
-  const int tok = r / p.group;
-  const int64_t row = (int64_t)(u.first + tok) * p.q_heads + u.h * p.group + r - tok * p.group;
   const int x = 2 * ((r >> 1) & 3);   // (piece_at)
   // pieces of this thread block: the odd ones in the warps' rings, then at most
   // one that ends its unit (even, in the workspace); or a whole unit's scratch
@@ -307,6 +308,8 @@ __device__ __forceinline__ void finish(const AttendParams& p, const Pieces<NT>& 
   add_pieces<K, B, false>(near, near_ml, [&](int i) { return near_o + (step / 2) * i * (S::kRing / 4); }, c, x, base, acc, sum);
   if (far >= 0) add_pieces<K, 1, true>(1, far_ml, [&](int) { return far_o; }, c, x, base, acc, sum);
   add_pieces<K, B, true>(src.n, part_ml, [&](int i) { return block_o + block_of(i) * D; }, c, x, base, acc, sum);
+  const int tok = token_of(p, r);
+  const int64_t row = (int64_t)(u.first + tok) * p.q_heads + u.h * p.group + r - tok * p.group;
   const bool first = (lane & 3) == 0 && k0 == 0;
   if (slot >= 0 || p.parts > 1) {
     float* dst = slot >= 0 ? p.block_o[part] + (slot * R + r) * D : p.o[part] + row * D;
@@ -407,7 +410,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       float o[NT][D / 16][4], m[NT][2], l[NT][2];
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        const int r = 8 * n + g8, tok = r / p.group;
+        const int r = 8 * n + g8, tok = token_of(p, r);
         const uint16_t* src = p.q + (int64_t)(u.first + tok) * p.ldq + (int64_t)(u.h * p.group + r - tok * p.group) * D + c2;
 #pragma unroll
         for (int d = 0; d < D / 16; ++d)
@@ -416,7 +419,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const int rj = 8 * n + c2 + j;
-          lim[n][j] = part == kPrefix || rj >= u.rows ? u.keys : u.keys - u.count + rj / p.group + 1;
+          lim[n][j] = part == kPrefix || rj >= u.rows ? u.keys : u.keys - u.count + token_of(p, rj) + 1;
           m[n][j] = -INFINITY;
           l[n][j] = 0.f;
         }
@@ -526,7 +529,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           float inv[2];
 #pragma unroll
           for (int j = 0; j < 2; ++j) inv[j] = l[n][j] > 0.f ? 1.f / l[n][j] : l[n][j];   // (0 where nothing is seen; NaN stays)
-          const int r = 8 * n + g8, tok = r / p.group;
+          const int r = 8 * n + g8, tok = token_of(p, r);
           const int64_t row = (int64_t)(u.first + tok) * p.q_heads + u.h * p.group + r - tok * p.group;
 #pragma unroll
           for (int d = 0; d < D / 16; ++d)
@@ -538,7 +541,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (p.lse && g8 == 0)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-              const int rj = 8 * n + c2 + j, tj = rj / p.group;
+              const int rj = 8 * n + c2 + j, tj = token_of(p, rj);
               if (rj < u.rows)
                 p.lse[(int64_t)(u.first + tj) * p.q_heads + u.h * p.group + rj - tj * p.group] =
                     m[n][j] == -INFINITY && l[n][j] == l[n][j] ? m[n][j] : (m[n][j] + log2_approx(l[n][j])) * 0.69314718056f;
