@@ -482,9 +482,8 @@ int sdq_cache_append(sdq_cache cache, const sdq_batch* batch, int32_t q_heads, c
  * joined in a fixed order.  scale: positive and finite.  q, out 16-byte
  * aligned, ldq a multiple of 8, ws 256-byte aligned.  Kernels are launched
  * with programmatic dependent launch.  A value that is not finite at a place
- * that a token sees reaches that token; at the places of its sequence's later
- * tokens of the same call it may too (their weight is 0, and 0 times it is
- * not); free places of a page may hold anything.
+ * that a token sees reaches that token, and no other; free places of a page may
+ * hold anything.
  * sdq_attention_workspace_bytes: for a batch of these integers (the device
  * arrays are not read; a smaller batch may need more, as it splits the keys
  * further); 0 on invalid input.  The

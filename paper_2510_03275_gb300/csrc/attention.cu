@@ -174,7 +174,7 @@ extern "C" int sdq_attention(sdq_cache c, const sdq_batch* b, int32_t q_heads, c
   const AttendWs L = attend_workspace(c, b, q_heads, p);
   if (ws_bytes < L.total) return SDQ_ERR_WORKSPACE;
   uint8_t* w = static_cast<uint8_t*>(ws);
-  p.q = q; p.ldq = ldq; p.out = out; p.lse = lse;
+  p.q = q; p.v = c->v; p.ldq = ldq; p.out = out; p.lse = lse;
   p.scale = scale * 1.44269504089f;
   p.q_heads = q_heads; p.kv_heads = c->desc.kv_heads;
   p.page_shift = log2_of(c->desc.page_tokens);

@@ -28,7 +28,7 @@ struct AttendWs {
 
 struct AttendParams {
   sdq_batch b;
-  const uint16_t* q;
+  const uint16_t *q, *v;    // v: the cache's values
   int64_t ldq;              // elements between tokens
   uint16_t* out;
   float* lse;               // natural log-sum-exp per row, may be null
@@ -57,6 +57,24 @@ __device__ __forceinline__ float log2_approx(float x) {
   float r;
   asm("lg2.approx.f32 %0, %1;\n" : "=f"(r) : "f"(x));
   return r;
+}
+
+// Of two bf16: which are infinite or NaN, as their 16 bits each.
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) {
+  return ((w & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((w & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
+}
+// Is one of 8 bf16 infinite or NaN?  (An exponent of ones and 1 more carries into the sign's place.)
+__device__ __forceinline__ bool some_not_finite(uint4 v) {
+  auto up = [](uint32_t w) { return (w & 0x7F807F80u) + 0x00800080u; };
+  return ((up(v.x) | up(v.y) | up(v.z) | up(v.w)) & 0x80008000u) != 0;
+}
+__device__ __forceinline__ uint4 ld_shared16(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ void st_shared16(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};\n" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
 
 // This lane's V columns of a row of D fp32 that another thread block wrote.

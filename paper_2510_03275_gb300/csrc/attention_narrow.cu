@@ -435,16 +435,29 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!ok) break;
         const uint32_t kb = ring_a + st * 2 * S::kMat, vb = kb + S::kMat;
         const bool edge = (t + 1) * kTile > seen;
-        if (edge && (t + 1) * kTile > u.keys) {
-          // values past the last key are leftovers (perhaps NaN): zero times them has to be zero
+        // values from key `from` of the tile's on: zero times them has to be zero
+        auto drop = [&](int from) {
+#pragma unroll 1
           for (int i = lane; i < kTile * (D / 8); i += 32) {
             const int r = i / (D / 8), c = i % (D / 8);
-            if (t * kTile + r >= u.keys)
-              asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};\n" ::"r"((uint32_t)(vb + (c >> 3) * kHalf + r * 128 + ((c & 7) << 4))),
-                           "r"(0) : "memory");
+            if (t * kTile + r >= from) st_shared16(vb + (c >> 3) * kHalf + r * 128 + ((c & 7) << 4), 0, 0, 0, 0);
           }
           fence_proxy_async_smem();   // (before the next copy into this stage)
           __syncwarp();
+        };
+        bool apart = false;   // a token's value that is not finite, and tokens before it
+        if (edge) {
+          if ((t + 1) * kTile > u.keys) drop(u.keys);   // past the last key: leftovers (perhaps NaN)
+          if (seen < u.keys) {
+            bool bad = false;
+#pragma unroll 1
+            for (int i = lane; i < kTile * (D / 8); i += 32) {
+              const int r = i / (D / 8), c = i % (D / 8);
+              const uint4 v = ld_shared16(vb + (c >> 3) * kHalf + r * 128 + ((c & 7) << 4));
+              if (t * kTile + r >= seen) bad |= some_not_finite(v);
+            }
+            apart = __any_sync(0xffffffffu, bad);
+          }
         }
         float s[NT][2][4];   // even and odd 16 elements, so that the chain of sums is half as long
 #pragma unroll
@@ -501,15 +514,38 @@ __global__ void __launch_bounds__(kThreads, 1)
           pf[n][1] = movmatrix(pack_bf16x2(e[2], e[3]));
         }
         const uint32_t vr = ((lane >> 4) << 3) + (lane & 7), vc = (lane >> 3) & 1;
+        if (!apart) {
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d) {
-          uint32_t a[4];
-          const uint32_t c = 2 * d + vc;
-          ldmatrix4_trans(a, vb + (c >> 3) * kHalf + vr * 128 + (((c & 7) ^ (vr & 7)) << 4));
+          for (int d = 0; d < D / 16; ++d) {
+            uint32_t a[4];
+            const uint32_t c = 2 * d + vc;
+            ldmatrix4_trans(a, vb + (c >> 3) * kHalf + vr * 128 + (((c & 7) ^ (vr & 7)) << 4));
 #pragma unroll
-          for (int n = 0; n < NT; ++n) mma_bf16_16816(o[n][d], a, pf[n][0], pf[n][1]);
+            for (int n = 0; n < NT; ++n) mma_bf16_16816(o[n][d], a, pf[n][0], pf[n][1]);
+          }
+          __syncwarp();   // every lane has read the stage
+        } else {
+          // token by token, the last first, each without the values that it does not see
+#pragma unroll 1
+          for (int i = u.count - 1; i >= 0; --i) {
+            drop(u.keys - u.count + i + 1);
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d) {
+              uint32_t a[4];
+              const uint32_t c = 2 * d + vc;
+              ldmatrix4_trans(a, vb + (c >> 3) * kHalf + vr * 128 + (((c & 7) ^ (vr & 7)) << 4));
+#pragma unroll
+              for (int n = 0; n < NT; ++n) {
+                float x[4] = {o[n][d][0], o[n][d][1], o[n][d][2], o[n][d][3]};
+                mma_bf16_16816(x, a, pf[n][0], pf[n][1]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                  if (token_of(p, 8 * n + c2 + (j & 1)) == i) o[n][d][j] = x[j];
+              }
+            }
+            __syncwarp();
+          }
         }
-        __syncwarp();   // every lane has read the stage
         issue();
       }
       if (!ok) break;

@@ -90,15 +90,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
-__device__ __forceinline__ void st_shared16(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
-  asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};\n" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
-}
-__device__ __forceinline__ uint4 ld_shared16(uint32_t a) {
-  uint4 v;
-  asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
-  return v;
-}
-
 // Operand with its second dimension contiguous (V: keys x 64 elements per
 // 128-byte row, 128-byte swizzle): 8-key groups 1024 bytes apart, the next 64
 // elements kHalf bytes on.
@@ -186,6 +177,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t full[S::kRing], empty[S::kRing], q_full, s_full[2], p_full[2][2], pv_done[2], mma_done;
   __shared__ uint32_t tmem_base;
+  __shared__ volatile int tainted;   // a value that is not finite was taken out
   const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
   const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t ring = sbase + 2 * S::kMat;
@@ -202,6 +194,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       mbar_init(&pv_done[i], 1);
     }
     mbar_init(&mma_done, 1);
+    tainted = 0;
     fence_mbar_init();
   }
   if (warp == 8) {
@@ -343,6 +336,10 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       // own keys that this row sees, and that every row of its half does
       const int lim = live ? w.own - w.count + tok + 1 : w.own;
       const int all = w.own - w.count + (w.r0 + 128 * half) / p.group + 1;
+      // and that every row of the block does.  Values of later ones that are not
+      // finite are taken out of the tile, as zero times them is not zero, and added
+      // at the end to the rows that see them
+      const int all_rows = max(0, w.own - w.count + w.r0 / p.group + 1);
       const uint32_t ts = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + 128 * half;
       const uint32_t to = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + 256 + D * half;
       float m = -INFINITY;        // reference maximum (log2 units)
@@ -367,21 +364,41 @@ __global__ void __launch_bounds__(kWideThreads, 1)
 #pragma unroll
           for (int c = 0; c < kSub; ++c)
             if (c >= see) x[c] = 0xFF800000u;
-          if (k0 + kSub > keys) {
-            // values past the last key are leftovers (perhaps NaN): zero times them has to be zero
-            const int vs = (2 * i + 1) % S::kRing, r = kSub * j + wtid;
-            if (!mbar_wait_warp(&full[vs], ((2 * i + 1) / S::kRing) & 1)) {
-              ok = false;
-              break;
-            }
-            if (wtid < kSub && k0 + wtid >= keys) {
-#pragma unroll
-              for (int c = 0; c < D / 8; ++c)
-                asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};\n" ::"r"(
-                                 (uint32_t)(ring + vs * S::kMat + (c >> 3) * kHalf + r * 128 + ((c & 7) << 4))), "r"(0) : "memory");
-            }
-            fence_proxy_async_smem();
+        }
+        if (half == 0 && k0 + kSub > (pre ? keys : min(keys, all_rows))) {
+          // (for both halves: the second's product is issued after the first's)
+          // values past the last key are leftovers (perhaps NaN): zero times them has to be zero too
+          const int vs = (2 * i + 1) % S::kRing, from = 8 * max(0, (pre ? keys : min(keys, all_rows)) - k0);
+          if (!mbar_wait_warp(&full[vs], ((2 * i + 1) / S::kRing) & 1)) {
+            ok = false;
+            break;
           }
+          const uint32_t at = ring + vs * S::kMat + (kSub * j) * 128;   // 16-byte pieces c of the rows
+#pragma unroll 1
+          for (int c = from + wtid; c < 8 * kSub; c += 256) {
+            uint4 v[2][D / 64];
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+              for (int d = 0; d < D / 64; ++d) v[k][d] = ld_shared16(at + d * kHalf + 16 * min(c + 128 * k, 8 * kSub - 1));
+            bool any = false;
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+              for (int d = 0; d < D / 64; ++d) any |= some_not_finite(v[k][d]);
+            if (!any) continue;
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+              for (int d = 0; d < D / 64; ++d) {
+                const uint4 x = v[k][d];
+                if (c + 128 * k >= 8 * kSub || !some_not_finite(x)) continue;
+                if (k0 + ((c + 128 * k) >> 3) < keys) tainted = 1;
+                st_shared16(at + d * kHalf + 16 * (c + 128 * k), x.x & ~not_finite(x.x), x.y & ~not_finite(x.y), x.z & ~not_finite(x.z),
+                            x.w & ~not_finite(x.w));
+              }
+          }
+          fence_proxy_async_smem();
         }
         float mx[4];
 #pragma unroll
@@ -436,6 +453,30 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       // ------------------------------------------------------------- out
       if (n > 0 && ok) ok = mbar_wait_warp(&mma_done, 0);
       tc_fence_after();
+      if (n > 0 && ok && tainted) {
+#pragma unroll 1
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t o[32];
+          tmem_ld32(to + 32 * c, o);
+          tmem_ld_wait();
+#pragma unroll 1
+          for (int key = all_rows; live && key < lim; ++key) {
+            const int pg = __ldg(p.b.pages + (int64_t)w.s * p.b.page_stride + (key >> p.page_shift));
+            if (pg < 0 || pg >= p.n_pages) continue;
+            const uint32_t* v = reinterpret_cast<const uint32_t*>(
+                p.v + ((((int64_t)pg * p.kv_heads + w.h) << p.page_shift) + (key & ((1 << p.page_shift) - 1))) * D + 32 * c);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              const uint32_t x = __ldg(v + j), bad = not_finite(x);
+              if (bad & 0xFFFFu) o[2 * j] = __float_as_uint(__uint_as_float(o[2 * j]) + __uint_as_float(x << 16));
+              if (bad >> 16) o[2 * j + 1] = __float_as_uint(__uint_as_float(o[2 * j + 1]) + __uint_as_float(x & 0xFFFF0000u));
+            }
+          }
+          __syncwarp();
+          tmem_st32(to + 32 * c, o);
+        }
+        tmem_st_wait();
+      }
       if (joins) {
         // fp32 rows through shared memory, over operands that nothing reads any
         // more (nor has still to arrive: the barrier is behind all copies of Q)

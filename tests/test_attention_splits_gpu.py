@@ -65,3 +65,45 @@ def test_a_value_that_is_not_finite_reaches_those_that_see_it(sdq, name, bad):
     hit[:new[0], :group] = True
     assert torch.isnan(out[hit]).all() and torch.isnan(lse[:new[0], :group]).all()
     assert torch.equal(out[~hit], want[~hit])
+
+
+MASKED = {
+    "draft": (H70, [3, 2, 4], [30, 130, 67], 0, 16, 1),
+    "draft-whole": (H70, [4, 1], [3, 9], 0, 16, 2),          # (a slot whose first new token has no place)
+    "draft-odd": (ODD, [5, 3], [205, 140], 60, 64, 3),
+    "draft-64": (H125, [30, 1], [30, 20], 0, 32, 11),
+    "prompt": (H70, [70, 1, 37], [70, 50, 200], 0, 32, 40),
+    "prompt-last": (H7, [300], [420], 0, 16, 299),
+    "prompt-64": (H125, [260, 5], [300, 5], 0, 16, 131),
+    "prompt-behind": ((4, 4, 64), [300, 260], [300, 700], 257, 32, 200),
+    "shares": (H70, [40, 1, 0], [3000, 1, 0], 0, 16, 25),
+    "both": (H70, [20] + [1] * 9, [1200] + [5] * 9, 2900, 16, 12),
+}
+
+
+@pytest.mark.parametrize("name", MASKED)
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_tokens_do_not_meet_later_ones(sdq, name, bad):
+    """Key and value of new token j of sequence 0, one head: the tokens before it are as without it."""
+    import torch
+    heads, new, own, prefix, page, j = MASKED[name]
+    c = Case(heads, new, own, prefix, page, seed=len(name))
+    want, _ = _run(sdq, torch, c)
+    batch, q = c.batch(sdq, torch), to_bf16(torch, c.q)
+    at, group = own[0] - new[0] + j, c.q_heads // c.kv_heads
+    spot = int(c.pages[0, at // page]), c.kv_heads - 1, at % page
+    for key in (False, True):
+        cache = c.cache(sdq, torch)
+        cache.v_pages[spot][7] = bad
+        cache.v_pages[spot][c.dim - 2] = bad
+        if key:
+            cache.k_pages[spot][1] = bad
+        out = cache.attend(batch, q)
+        hit = torch.zeros(out.shape, dtype=torch.bool, device="cuda")
+        rows = hit[j:new[0], (c.kv_heads - 1) * group:]
+        if key:
+            rows[:] = True   # (a score that is not finite: what is left of the row is not looked at)
+        else:
+            rows[..., 7] = rows[..., c.dim - 2] = True
+            assert not torch.isfinite(out[hit]).any()
+        assert torch.equal(out[~hit], want[~hit])
