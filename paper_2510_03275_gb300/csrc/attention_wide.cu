@@ -33,8 +33,9 @@ namespace {
 // shared memory, they took 4 to 10 us longer, and the device holds fewer.)
 // A tile takes 2320 cycles (2048 of products), a thread block's start 5000, its
 // output 3000 (6500 as fp32 sums).  Prompts of 400 to 2500 tokens behind 1021,
-// 64 heads: 197 us, 68 % of the measured bf16 rate; 64 tokens of 64 heads
-// against 8199 keys alone: 28 us.
+// 64 heads: 200 us, 67 % of the measured bf16 rate (196 without the look for
+// values that are not finite); 64 tokens of 64 heads against 8199 keys alone: 28
+// us.
 // Registers: 384 threads hold 168 each at launch; the first two warpgroups go
 // to 224 once the third has gone down to 56 (224 + 224 + 56 = 3 x 168).
 constexpr int kWideThreads = 384;
