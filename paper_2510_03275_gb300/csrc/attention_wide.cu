@@ -514,7 +514,10 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         if (live) (split ? p.split_ml[part] : p.ml[part])[slot] = make_float2(l == l ? m : l, l);   // (NaN scores leave no maximum)
       } else if (ok) {
         // rows to memory over the place of Q, which nothing reads any more: a
-        // thread's row would go out in 16-byte pieces, 32 rows at a time
+        // thread's row would go out in 16-byte pieces, 32 rows at a time.  (Nor
+        // has Q still to arrive: the products began behind all copies of it; where
+        // there was none, a warp's place may be the target of another's copies)
+        if (n == 0) named_bar_sync(1, 128 * halves);
         const int64_t at = (int64_t)(w.first + tok) * p.q_heads + w.h * p.group + g;
         const float k = l > 0.f ? 1.f / l : l;       // (0 where nothing is seen; NaN stays)
         constexpr int kChunks = D / 8;
