@@ -676,15 +676,17 @@ __global__ void __launch_bounds__(kThreads, 1)
           finish<D, NT, 1>(sp, pc, smem, part, u, m, Source{0, 0, first, n}, -1, warp / kPer);
       }
     }
-    // sequences without keys of their own: 0, or nothing to join
+    // sequences without keys of their own: 0, or nothing to join.  (Any number of
+    // rows, where no sequence has keys: by tokens, whose rows are neighbours)
     if (part == kOwn)
       for (int s = blockIdx.x; s < p.b.n_seqs; s += gridDim.x) {
         const SeqSpan q = seq_span(p.b, s);
-        if (q.own > 0 || q.count == 0) continue;
-        Unit u{s, 0, q.first, q.count * p.group, 0, q.count, 0, 0};
-        for (int i = warp; i < p.kv_heads * ((u.rows + 7) / 8); i += kWarps) {
-          u.h = i % p.kv_heads;
-          finish<D, NT, D / 16>(sp, pc, smem, part, u, i / p.kv_heads, Source{0, 0, 0, 0}, -1, 0);
+        if (q.own > 0) continue;
+        const int64_t r1 = (int64_t)(q.first + q.count) * p.q_heads;
+        for (int64_t row = (int64_t)q.first * p.q_heads + warp; row < r1; row += kWarps) {
+          const float none[D / 32] = {};
+          if (p.parts == 1) write_row<D, D / 32>(p, row, none, -INFINITY, 0.f);
+          else if (lane == 0) p.ml[part][row] = make_float2(-INFINITY, 0.f);   // (the join reads no sums of it)
         }
       }
   }

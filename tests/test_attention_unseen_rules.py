@@ -27,3 +27,17 @@ def test_wide_kernel_orders_its_output_behind_the_queries_copies():
     rows = _rows_out(_source("attention_wide.cu"))
     barrier = re.search(r"if \(n == 0\) named_bar_sync\(1, 128 \* halves\);", rows)
     assert barrier and barrier.end() < rows.index("st_shared16(")
+
+
+def test_narrow_kernel_splits_rows_by_multiplication_within_its_range_only():
+    """token_of is exact below 32 rows (a unit with keys has no more), and not far beyond; a sequence without keys may
+    bring any number of rows and goes another way."""
+    def token_of(r, group):
+        return (r * (65536 // group + 1) & 0xFFFFFFFF) >> 16
+    assert all(token_of(r, g) == r // g for g in range(1, 4097) for r in range(32))
+    assert token_of(8199, 8) != 8199 // 8 and token_of(4111, 16) != 4111 // 16 and token_of(65536, 1) != 65536
+    text = _source("attention_narrow.cu")
+    assert "(uint32_t)r * p.group_inverse >> 16" in text and "65536u / (uint32_t)group + 1" in _source("attention.cu")
+    m = re.search(r"for \(int s = blockIdx\.x; s < p\.b\.n_seqs; s \+= gridDim\.x\)", text)
+    a, b = _block(text, m.end())
+    assert "own > 0" in text[a:b] and not re.search(r"\b(finish|token_of|group_inverse)\b", text[a:b])
