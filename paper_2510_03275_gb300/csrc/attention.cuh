@@ -106,7 +106,7 @@ __device__ __forceinline__ void write_row(const AttendParams& p, int64_t row, co
 
 // The narrow kernel on `part`; late: behind this call's kernel on the prefix,
 // beside which it may run.
-int narrow_groups(const sdq_batch* b, int group, int part);   // of 8 query rows
+int narrow_groups(const sdq_batch* b, int group, int part);   // of 8 query rows (1 to 4; 0 without keys)
 int narrow_warps();                                           // per thread block
 cudaError_t launch_narrow(const sdq_cache_s* c, const AttendParams& p, int part, bool late, cudaStream_t st);
 // The wide kernel on `part`, and how many thread blocks share the keys of a

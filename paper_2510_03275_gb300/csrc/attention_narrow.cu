@@ -707,6 +707,7 @@ cudaError_t launch(const sdq_cache_s* c, const AttendParams& p, int part, bool l
 template <int D>
 cudaError_t launch_nt(const sdq_cache_s* c, const AttendParams& p, int part, bool late, cudaStream_t st) {
   switch (narrow_groups(&p.b, p.group, part)) {
+    case 0:   // (no keys: zeros)
     case 1: return launch<D, 1>(c, p, part, late, st);
     case 2: return launch<D, 2>(c, p, part, late, st);
     case 3: return launch<D, 3>(c, p, part, late, st);
@@ -717,6 +718,7 @@ cudaError_t launch_nt(const sdq_cache_s* c, const AttendParams& p, int part, boo
 }  // namespace
 
 int narrow_groups(const sdq_batch* b, int group, int part) {
+  if ((part == kPrefix ? b->prefix_len : b->max_own) == 0) return 0;
   return (int)(((int64_t)(part == kPrefix ? b->n_tokens : b->max_new) * group + 7) / 8);
 }
 

@@ -75,3 +75,13 @@ def test_calls_without_any_keys(sdq, name):
         assert not out[:rows].any() and (out[rows:] == 7).all()
         assert torch.isneginf(lse[:rows]).all() if with_lse else (lse == 7).all()
         assert (lse[rows:] == 7).all()
+
+
+@pytest.mark.parametrize("name", NO_KEYS)
+def test_workspace_of_calls_without_any_keys(sdq, name):
+    """Tickets, and no room for partial results (fp32 rows of them would take gigabytes)."""
+    import torch
+    heads, new, page = NO_KEYS[name]
+    cache, batch = _no_keys(sdq, torch, heads, new, page)
+    size = sdq.sdq_attention_workspace_bytes(cache.handle, batch, heads[0])
+    assert 0 < size <= 8 * len(new) * heads[1] + 4096
