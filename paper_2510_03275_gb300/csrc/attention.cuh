@@ -59,6 +59,12 @@ __device__ __forceinline__ float log2_approx(float x) {
   return r;
 }
 
+// Natural log-sum-exp of a row from its maximum and sum.  (Scores that are all
+// NaN leave no maximum, but a sum that is NaN; -inf is a row that sees nothing.)
+__device__ __forceinline__ float natural_lse(float top, float sum) {
+  return top == -INFINITY && sum == sum ? top : (top + log2_approx(sum)) * 0.69314718056f;
+}
+
 // Of two bf16: which are infinite or NaN, as their 16 bits each.
 __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
   return ((w & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((w & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
@@ -101,7 +107,7 @@ __device__ __forceinline__ void write_row(const AttendParams& p, int64_t row, co
   uint32_t* dst = reinterpret_cast<uint32_t*>(p.out + row * D + V * lane);
   if (V == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(acc[0] * k, acc[1] * k), pack_bf16x2(acc[V - 2] * k, acc[V - 1] * k));
   else *dst = pack_bf16x2(acc[0] * k, acc[1] * k);
-  if (p.lse && lane == 0) p.lse[row] = top == -INFINITY ? top : (top + log2_approx(sum)) * 0.69314718056f;
+  if (p.lse && lane == 0) p.lse[row] = natural_lse(top, sum);
 }
 
 // The narrow kernel on `part`; late: behind this call's kernel on the prefix,

@@ -324,7 +324,7 @@ __device__ __forceinline__ void finish(const AttendParams& p, const Pieces<NT>& 
   for (int k = 0; k < K; ++k)
     *reinterpret_cast<uint2*>(p.out + row * D + 4 * (c + 4 * k)) =
         make_uint2(pack_bf16x2(acc[k].x * inv, acc[k].y * inv), pack_bf16x2(acc[k].z * inv, acc[k].w * inv));
-  if (p.lse && first) p.lse[row] = top == -INFINITY ? top : (top + log2_approx(sum)) * 0.69314718056f;
+  if (p.lse && first) p.lse[row] = natural_lse(top, sum);
 }
 
 template <int D, int NT>
@@ -579,8 +579,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int j = 0; j < 2; ++j) {
               const int rj = 8 * n + c2 + j, tj = token_of(p, rj);
               if (rj < u.rows)
-                p.lse[(int64_t)(u.first + tj) * p.q_heads + u.h * p.group + rj - tj * p.group] =
-                    m[n][j] == -INFINITY && l[n][j] == l[n][j] ? m[n][j] : (m[n][j] + log2_approx(l[n][j])) * 0.69314718056f;
+                p.lse[(int64_t)(u.first + tj) * p.q_heads + u.h * p.group + rj - tj * p.group] = natural_lse(m[n][j], l[n][j]);
             }
         }
         continue;

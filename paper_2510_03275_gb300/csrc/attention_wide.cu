@@ -552,7 +552,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
           const uint4 v = ld_shared16(stage + (uint32_t)(r * 2 * D) + ((c ^ (r & 7)) << 4));
           if (lives >> r & 1) *to_row = v;
         }
-        if (live && p.lse) p.lse[at] = m == -INFINITY ? m : (m + log2_approx(l)) * 0.69314718056f;
+        if (live && p.lse) p.lse[at] = natural_lse(m, l);
       }
     }
     else mbar_arrive(&q_full);
