@@ -645,6 +645,8 @@ class KVCache:
         batch.check(d.page_tokens)
         if ws is None:
             ws = self.alloc_workspace(batch, heads, stream)
+        elif not ws.is_cuda or not ws.is_contiguous():
+            raise ValueError("KVCache.attend: ws must be a contiguous CUDA tensor")
         out = _empty((tokens, heads, dim), torch.bfloat16, q.device, stream)
         sdq_attention(self.handle, batch, heads, q, stride[0] if tokens > 1 else heads * dim,
                       dim ** -0.5 if scale is None else scale, out, lse, ws, stream)
