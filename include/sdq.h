@@ -469,14 +469,19 @@ int sdq_cache_append(sdq_cache cache, const sdq_batch* batch, int32_t q_heads, c
 /* Attention of a batch's new tokens over the cache: for every token and
  * query head, out = sum_j softmax_j(scale q . k_j) v_j over the keys that the
  * token sees (sdq_batch), query head i reading key head i / (q_heads /
- * kv_heads).  The prefix is computed once for all sequences: its keys and
- * values are read once for the whole batch, and joined with each sequence's
- * own part by the parts' maxima and sums.  q: bf16, q_heads x head_dim per
+ * kv_heads).  The prefix is a part of its own for all sequences together, and
+ * joined with each sequence's own part by the parts' maxima and sums: its keys
+ * and values are read once for every 256 rows (a token and a query head) per
+ * key head that the batch has, so once for a small decoding batch.  Where the
+ * sequences bring 128 such rows and more on the average, every 256 rows of a
+ * sequence run over the prefix and its own keys in one line instead; a long
+ * prompt beside many decoding sequences is therefore better a call of its
+ * own.  q: bf16, q_heads x head_dim per
  * token, token stride ldq in elements (sdq_cache_append's q_out has ldq =
  * q_heads * head_dim); out: bf16, n_tokens x q_heads x head_dim; lse (may be
  * NULL): fp32, n_tokens x q_heads, the natural logarithm of the sum of
  * exp(scale q . k_j), for a caller that joins further parts.  A token that
- * sees nothing: out 0, lse -inf.  Scores, maxima, sums and outputs are kept in
+ * sees nothing: out 0, lse -inf; a row with a score that is NaN: both NaN.  Scores, maxima, sums and outputs are kept in
  * fp32; the softmax weights are rounded to bf16 for their product with v, the
  * output once at the end.  Results do not depend on timing: partial sums are
  * joined in a fixed order.  scale: positive and finite.  q, out 16-byte

@@ -62,8 +62,8 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendParams p) {
 
 // ------------------------------------------------------------------- host
 // A prefix's rows go to the wide kernel from 9 on (16 rows of 32 heads against
-// 2051 keys: 25 us on the narrow one, whose warps then hold 16 rows each and
-// spend more on them than on the keys), a sequence's from 33 on, since the wide
+// 2051 keys: 15.6 us, 20.6 on the narrow one, whose warps then hold 16 rows each
+// and spend more on them than on the keys), a sequence's from 33 on, since the wide
 // kernel takes a thread block for every 256 of them, or fewer.  Where a sequence
 // brings 128 rows and more on the average, its row blocks run over the prefix
 // and its own keys in one line; below that the batch's rows share blocks against

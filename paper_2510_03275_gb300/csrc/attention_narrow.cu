@@ -21,11 +21,11 @@ namespace {
 //   columns (the other way round half of a 16-row tile would be padding), O^T
 //   += V^T P^T; K and V fragments come by ldmatrix, P^T is turned from the
 //   accumulator's layout into the operand's by movmatrix.
-// P is rounded to bf16 for its product (relative 2^-9 at most per weight, as
+// P is rounded to bf16 for its product (relative 2^-8 at most per weight, as
 // the values themselves carry); sums, maxima and outputs are fp32.
 // 64 tokens of 64 heads (8 key heads of 128) on 1 to 4096 keys each: 43 us, 4.7
 // TB/s; 2 x 3 tokens on 65537 to 131072: 164 us, 5.9 TB/s.  One token on 1037
-// keys takes 11.6 us, a chain of latencies: a block's tables and queries 4000
+// keys takes 10.7 us in a graph, a chain of latencies: a block's tables and queries 4000
 // cycles, its tiles 2500, its pieces 3300, the ticket 3000 to 6000, the join of
 // the blocks 3500.
 constexpr int kWarps = 8, kThreads = 32 * kWarps, kTile = 16;
@@ -33,9 +33,8 @@ constexpr int kWarps = 8, kThreads = 32 * kWarps, kTile = 16;
 // kUnitCost more: its queries, its output and the join cost its warp about as
 // much time as that many tiles.
 constexpr int kUnitCost = 2;
-// Places of a warp's share at least (1 instead: 27.7 us in place of 23.1 for 16
-// sequences of 32 heads with 1 to 300 keys each behind 2051; 3: 0.5 us more for
-// one sequence of 1037).
+// Places of a warp's share at least (one sequence of 1037 keys, 8 key heads: 10.7
+// us; with 1 instead 11.0, with 3 11.3).
 constexpr int64_t kMinShare = 2;
 
 template <int D, int NT> struct NarrowShape {

@@ -600,10 +600,13 @@ double wide_time(const sdq_cache_s* c, const sdq_batch* b, int q_heads, int part
 // The least of: its time; the join of the parts' sums, a launch (3 us) and 4
 // TB/s; and what the narrow kernel beside it, where that takes the other part,
 // needs longer: kNarrowStart and its reading (40 bytes a ns and SM) on the SMs
-// left free, or on all of them afterwards.  (The lengths are not known here: a
-// sixth of their bound, as for lengths spread over their logarithm.)  64 rows of 8 heads a key
-// head against 8199 keys, and 1 to 512 of each sequence: 7 parts take 32 us, 6
-// 34, 8 42; 16 of 32 against 2051 and 1 to 300: 3 take 20 us, 4 28.
+// left free, or on all of them afterwards.  (The lengths are not known here, only
+// their bound: a sixth of it stands for them, the mean of lengths spread over
+// their logarithm.)  64 sequences of 8 heads a key head behind 8199 keys, own
+// lengths up to 512, 7 parts by this rule, us for 3, 5, 6, 7, 8 parts: lengths
+// over their logarithm 45, 35, 33, 31, 41; all at the bound 50, 52, 52, 53, 57;
+// all of 1 but one 44, 34, 32, 31, 31.  16 of 32 heads behind 2051, up to 300,
+// 3 parts, us for 2, 3, 4: 21, 19, 24; at the bound 34, 33, 37; 21, 19, 23.
 int wide_splits(const sdq_cache_s* c, const sdq_batch* b, int q_heads, int part, bool chained, bool narrow) {
   const double own = narrow ? (double)b->n_seqs * c->desc.kv_heads * b->max_own / 6 * c->desc.head_dim * 4 : 0.0;   // bytes
   auto time = [&](int s) {

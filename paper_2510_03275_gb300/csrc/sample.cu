@@ -31,8 +31,8 @@
 // shared memory, which is a compare-and-swap loop.
 // What bounds it: the instructions of the passes over many rows (a row is read
 // once from HBM); for few rows the chain of passes and cluster barriers.  96 rows
-// of 128255 fp32 with settings of all kinds: 73.5 us (two waves of clusters of
-// 3); 32 of 50272 bf16: 23.5; one of 32000: 7.6.
+// of 128255 fp32 with settings of all kinds: 66 to 80 us by the logits (two waves
+// of clusters of 3); 32 of 50272 bf16: 17 to 48 likewise; one of 32000: 6.5.
 #include <algorithm>
 
 #include "common.cuh"
