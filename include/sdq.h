@@ -434,6 +434,52 @@ typedef struct {
   const int32_t* prefix_pages; /* ceil(prefix_len / page_tokens); unused without a prefix */
 } sdq_batch;
 
+/* A step's block tables, made on the GPU.  The pool: free_pages holds n_pages
+ * entries, of which the first *n_free are the free pages, the top of the stack
+ * last.  Sequence s has own_len[s] tokens on pages[s * page_stride + i], i <
+ * ceil(own_len / page_tokens); negative lengths count as 0.
+ *   1. Sequences whose `done` is not 0 give their pages back: sequence by
+ *      sequence, column by column, onto the stack; they then have 0 tokens.
+ *      (An entry is pushed as it stands; pages beyond n_pages are dropped.)
+ *   2. Sequence s asks for new_len[s] tokens and the pages that they begin.  One
+ *      whose table has too few columns gets nothing and does not count below.
+ *      The others get what they ask for if the tokens asked for up to and with s
+ *      are at most n_tokens, and, where s needs a page, the pages asked for up to
+ *      and with s are at most the free ones; else nothing in this step.
+ *   3. Pages go out in the order of the sequences and of their tokens, from
+ *      the top of the stack, into the tables; other entries stay.
+ * token_start (n_seqs + 1) and own_out (n_seqs, with the new tokens) are those
+ * of an sdq_batch with n_tokens rows; *n_free_out: what the pool has left.
+ * own_out may be own_len, n_free_out n_free (a captured step); the stack's
+ * entries below *n_free_out are then the free pages.  slots, positions (n_tokens
+ * each, may be NULL): page * page_tokens + place in the page, and prefix_len +
+ * place in the sequence, of each token; -1 and 0 for rows that no sequence
+ * has, slot -1 also where a page is outside the pool.  Nothing else overlaps.
+ * One kernel (a cluster of 1 to 8 thread blocks), launched with programmatic
+ * dependent launch; no workspace.  Errors: INVALID_ARG, UNSUPPORTED (current
+ * device is not compute capability 10.3), CUDA. */
+typedef struct {
+  int32_t page_tokens;    /* 16, 32, 64 or 128 */
+  int32_t n_pages;        /* n_pages * page_tokens < 2^31 */
+  int32_t n_seqs;         /* 1 .. 65535 */
+  int32_t n_tokens;       /* 1 .. 2^20 */
+  int32_t page_columns;   /* of the tables; page_columns * page_tokens < 2^30 */
+  int32_t page_stride;    /* >= page_columns */
+  int32_t prefix_len;     /* 0 .. 2^30 - 1 */
+  const int32_t* own_len;
+  const int32_t* new_len;
+  const int32_t* done;    /* may be NULL */
+  int32_t* pages;
+  int32_t* free_pages;
+  const int32_t* n_free;
+  int32_t* token_start;
+  int32_t* own_out;
+  int32_t* n_free_out;
+  int32_t* slots;
+  int32_t* positions;
+} sdq_pages;
+int sdq_pages_step(const sdq_pages* step, void* stream);
+
 /* Position rotation: elements (j, j + dim / 2) of a head, or (2 j, 2 j + 1)
  * where interleaved, j < dim / 2, are turned by the angle whose cosine and
  * sine stand at [position][j] of the tables (device, fp32, n_pos x dim / 2):
@@ -465,6 +511,24 @@ int sdq_rope_table(int32_t n_pos, int32_t dim, double base, float* cos_host, flo
 int sdq_cache_append(sdq_cache cache, const sdq_batch* batch, int32_t q_heads, const void* q, int64_t ldq,
                      const void* k, int64_t ldk, const void* v, int64_t ldv, int32_t type, const sdq_rope* rope,
                      uint16_t* q_out, void* stream);
+
+/* The same with every head of q and k normalised before its rotation: x ->
+ * x / sqrt(mean(x^2) + eps) * weight, the mean over the head's head_dim
+ * elements.  q, k: fp32 weights on the device, 16-byte aligned, head_dim of them for all
+ * heads, or where the flag is 1 head_dim for each (q_heads or kv_heads x
+ * head_dim); NULL: those heads stay as they are.  v is never normalised.  All
+ * in fp32; each result is rounded to bf16 once, after the rotation.  eps:
+ * positive and finite.  As sdq_cache_append otherwise. */
+typedef struct {
+  const float* q;
+  const float* k;
+  int32_t q_per_head; /* 0 or 1 */
+  int32_t k_per_head; /* 0 or 1 */
+  float eps;
+} sdq_head_norm;
+int sdq_cache_append_norm(sdq_cache cache, const sdq_batch* batch, int32_t q_heads, const void* q, int64_t ldq,
+                          const void* k, int64_t ldk, const void* v, int64_t ldv, int32_t type, const sdq_rope* rope,
+                          const sdq_head_norm* norm, uint16_t* q_out, void* stream);
 
 /* Attention of a batch's new tokens over the cache: for every token and
  * query head, out = sum_j softmax_j(scale q . k_j) v_j over the keys that the
@@ -526,6 +590,45 @@ int sdq_attention_status(const void* ws, void* stream);
 int sdq_sample(const void* logits, int32_t type, int32_t rows, int32_t vocab, int64_t ld, const float* u,
                const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
                int32_t* tokens, void* stream);
+
+/* Logits before the choice of a token: for row i and token t, with z the
+ * logit (fp32 or bf16 as `type`, rows x vocab with row stride ld in elements),
+ *   penalties  t among the row's history: z > 0 ? z / repetition : z *
+ *              repetition; if it stands there c > 0 times from place
+ *              prompt_len on (among the answer's tokens), then z - (frequency
+ *              c + presence);
+ *   biases     z + the sum of the biases of the list's entries for t, added up
+ *              in the list's order (no entry: z stays);
+ *   grammar    t not in the row's allowed set: -inf.
+ * In fp32, rounded once to the logits' type; a logit that nothing of it meets
+ * keeps its bits.  Written to `out` (same type, row stride ldo), which may be
+ * the logits themselves (the same pointer and stride: then only what changes is
+ * read and written) but not overlap them in another way.  Every part may be left
+ * out.  All arrays are device memory, read when the kernel runs; lengths
+ * beyond the bounds are cut to them, tokens outside the vocabulary and
+ * negative ids are passed over.  vocab up to 393216, rows up to 65535; no
+ * workspace; one kernel, launched with programmatic dependent launch.  Errors:
+ * INVALID_ARG, UNSUPPORTED (current device is not compute capability 10.3),
+ * CUDA. */
+typedef struct {
+  const int32_t* history;      /* rows x history_stride: each row's tokens so far, prompt first; NULL: no penalties */
+  const int32_t* history_len;  /* per row; NULL: history_max */
+  const int32_t* prompt_len;   /* per row, how many of them the prompt's are; NULL: 0 */
+  const float* repetition;     /* per row, positive; NULL: 1 */
+  const float* frequency;      /* per row; NULL: 0 */
+  const float* presence;       /* per row; NULL: 0 */
+  const int32_t* bias_ids;     /* rows x bias_ids_stride: tokens; negative: an entry that is not used */
+  const float* bias;           /* rows x bias_stride */
+  const uint32_t* allowed;     /* n_allowed x allowed_stride (ceil(vocab / 32) words of each are read): token t is bit t % 32
+                                * of word t / 32; NULL: no grammar */
+  const int32_t* allowed_row;  /* per row, its set; outside 0 .. n_allowed - 1: every token.  NULL: set i for row i */
+  int64_t history_stride, bias_ids_stride, bias_stride, allowed_stride;   /* (0: one row for all) */
+  int32_t history_max;         /* bound of the lengths */
+  int32_t n_bias;              /* 0 .. 4096 entries per row */
+  int32_t n_allowed;
+} sdq_adjust;
+int sdq_adjust_logits(const void* logits, int32_t type, int32_t rows, int32_t vocab, int64_t ld, const sdq_adjust* adjust,
+                      void* out, int64_t ldo, void* stream);
 
 /* Static string for a status code. */
 const char* sdq_status_string(int status);

@@ -7,7 +7,7 @@ from __future__ import annotations
 
 import numpy as np
 
-__all__ = ["rotate", "append", "visible_keys", "attend", "sample", "sample_row"]
+__all__ = ["rotate", "head_norm", "append", "visible_keys", "attend", "sample", "sample_row", "adjust_row", "pages_step"]
 
 
 def rotate(x, pos, cos, sin, interleaved):
@@ -20,6 +20,14 @@ def rotate(x, pos, cos, sin, interleaved):
         y[:, a] = x[:, a] * c - x[:, b] * s
         y[:, b] = x[:, b] * c + x[:, a] * s
     return y
+
+
+def head_norm(x, weight, eps):
+    """x (tokens, heads, dim), each head over its root mean square, times weight ((dim) or (heads, dim)); None: x."""
+    x = np.asarray(x, np.float64)
+    if weight is None:
+        return x
+    return x / np.sqrt(np.square(x).mean(-1, keepdims=True) + eps) * np.asarray(weight, np.float64)
 
 
 def append(q, k, v, k_pages, v_pages, token_start, own_len, pages, prefix_len, cos, sin, interleaved):
@@ -43,14 +51,17 @@ def append(q, k, v, k_pages, v_pages, token_start, own_len, pages, prefix_len, c
     return q_out, k_pages, v_pages
 
 
-def visible_keys(s, i, token_start, own_len, pages, prefix_pages, prefix_len, page):
-    """(page, slot) of every key that new token i of sequence s sees."""
+def visible_keys(s, i, token_start, own_len, pages, prefix_pages, prefix_len, page, window=0, sinks=0):
+    """(page, slot) of every key that new token i of sequence s sees; window > 0: of its last `window` positions,
+    its own among them, and of the first `sinks` positions."""
     n = token_start[s + 1] - token_start[s]
     seen = [(prefix_pages[j // page], j % page) for j in range(prefix_len)]
-    return seen + [(pages[s][j // page], j % page) for j in range(max(0, own_len[s] - n + i + 1))]
+    seen += [(pages[s][j // page], j % page) for j in range(max(0, own_len[s] - n + i + 1))]
+    last = len(seen) - 1
+    return [k for j, k in enumerate(seen) if window == 0 or j > last - window or j < sinks]
 
 
-def attend(q, k_pages, v_pages, token_start, own_len, pages, prefix_pages, prefix_len, scale):
+def attend(q, k_pages, v_pages, token_start, own_len, pages, prefix_pages, prefix_len, scale, window=0, sinks=0):
     """q (tokens, q_heads, dim) -> (outputs, natural log-sum-exps, sum of |p v|) in fp64; a token that sees
     nothing: 0, -inf, 0."""
     q = np.asarray(q, np.float64)
@@ -59,7 +70,7 @@ def attend(q, k_pages, v_pages, token_start, own_len, pages, prefix_pages, prefi
     out, lse, mag = np.zeros_like(q), np.full(q.shape[:2], -np.inf), np.zeros_like(q)
     for s in range(len(own_len)):
         for i in range(token_start[s + 1] - token_start[s]):
-            keys = visible_keys(s, i, token_start, own_len, pages, prefix_pages, prefix_len, page)
+            keys = visible_keys(s, i, token_start, own_len, pages, prefix_pages, prefix_len, page, window, sinks)
             if not keys:
                 continue
             t = token_start[s] + i
@@ -111,3 +122,59 @@ def sample_row(z, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
 def sample(z, u, temperature, top_k, top_p, min_p):
     rows = [sample_row(*a) for a in zip(z, u, temperature, top_k, top_p, min_p)]
     return np.array([r[0] for r in rows]), np.array([r[1] for r in rows])
+
+
+def adjust_row(z, history=(), prompt_len=0, repetition=1.0, frequency=0.0, presence=0.0, bias=(), allowed=None):
+    """A row of logits with the penalties of the tokens in `history`, biases ((token, bias) one after another) and
+    an allowed set (None: all)."""
+    z = np.array(z, np.float64)
+    for t in set(history):
+        if 0 <= t < len(z):
+            z[t] = z[t] / repetition if z[t] > 0 else z[t] * repetition
+    answer = [t for t in history[prompt_len:]]
+    for t in set(answer):
+        if 0 <= t < len(z):
+            z[t] -= frequency * answer.count(t) + presence
+    total = {}
+    for t, b in bias:
+        total[t] = total.get(t, 0.0) + b
+    for t, b in total.items():
+        if 0 <= t < len(z):
+            z[t] += b
+    if allowed is not None:
+        for t in range(len(z)):
+            if t not in allowed:
+                z[t] = -np.inf
+    return z
+
+
+def pages_step(page, n_pages, free, own_len, new_len, done, tables, n_tokens, prefix_len=0):
+    """(token_start, own_len, free, slots, positions, tables) after a step; free: the stack's pages, top last."""
+    free, tables = list(free), [list(t) for t in tables]
+    own = [max(0, m) for m in own_len]
+    for s, d in enumerate(done):
+        if d:
+            free += tables[s][:-(-own[s] // page)]
+            own[s] = 0
+    free = free[:n_pages]
+    have, asked_tokens, asked_pages = len(free), 0, 0
+    start, slots, positions = [0], [], []
+    for s, n in enumerate(new_len):
+        n = max(0, n)
+        need = -(-(own[s] + n) // page) - -(-own[s] // page)
+        if -(-(own[s] + n) // page) > len(tables[s]):
+            n = 0
+        else:
+            asked_tokens, asked_pages = asked_tokens + n, asked_pages + need
+            if asked_tokens > n_tokens or (need > 0 and asked_pages > have):
+                n = 0
+        for _ in range(n):
+            if own[s] % page == 0:
+                tables[s][own[s] // page] = free.pop()
+            p = tables[s][own[s] // page]
+            slots.append(p * page + own[s] % page if 0 <= p < n_pages else -1)
+            positions.append(prefix_len + own[s])
+            own[s] += 1
+        start.append(start[-1] + n)
+    rest = n_tokens - len(slots)
+    return start, own, free, slots + [-1] * rest, positions + [0] * rest, tables

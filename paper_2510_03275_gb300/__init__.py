@@ -16,6 +16,7 @@ import ctypes
 import os
 from dataclasses import dataclass
 from fractions import Fraction
+from typing import NamedTuple
 
 __all__ = [
     "SDQ_OK", "SDQ_BINARY", "SDQ_TERNARY", "SDQ_ALPHA_MAXABS", "SDQ_ALPHA_MEANABS",
@@ -30,6 +31,7 @@ __all__ = [
     "sdq_cache_bytes", "sdq_cache_create", "sdq_cache_destroy", "sdq_rope_table", "sdq_cache_append",
     "sdq_attention_workspace_bytes", "sdq_attention", "sdq_attention_status",
     "sdq_sample", "sample",
+    "HeadNorm", "sdq_cache_append_norm", "PagePool", "PageStep", "sdq_pages_step", "sdq_adjust_logits", "adjust_logits",
 ]
 
 SDQ_OK = 0
@@ -92,6 +94,25 @@ class _Rope(ctypes.Structure):
                 ("interleaved", ctypes.c_int32)]
 
 
+class _HeadNorm(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("q_per_head", ctypes.c_int32), ("k_per_head", ctypes.c_int32),
+                ("eps", ctypes.c_float)]
+
+
+class _Adjust(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("history", "history_len", "prompt_len", "repetition", "frequency", "presence",
+                                                "bias_ids", "bias", "allowed", "allowed_row")]
+                + [(n, ctypes.c_int64) for n in ("history_stride", "bias_ids_stride", "bias_stride", "allowed_stride")]
+                + [(n, ctypes.c_int32) for n in ("history_max", "n_bias", "n_allowed")])
+
+
+class _Pages(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("page_tokens", "n_pages", "n_seqs", "n_tokens", "page_columns", "page_stride",
+                                               "prefix_len")]
+                + [(n, ctypes.c_void_p) for n in ("own_len", "new_len", "done", "pages", "free_pages", "n_free", "token_start",
+                                                  "own_out", "n_free_out", "slots", "positions")])
+
+
 @dataclass(frozen=True)
 class CacheDesc:
     """Mirror of ``sdq_cache_desc``."""
@@ -145,10 +166,13 @@ _SIGS = {
     "sdq_cache_destroy": (ctypes.c_int, [_vp]),
     "sdq_rope_table": (ctypes.c_int, [_i32, _i32, ctypes.c_double, _vp, _vp]),
     "sdq_cache_append": (ctypes.c_int, [_vp, _vp, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _vp, _vp, _vp]),
+    "sdq_cache_append_norm": (ctypes.c_int, [_vp, _vp, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _vp, _vp, _vp, _vp]),
     "sdq_attention_workspace_bytes": (_sz, [_vp, _vp, _i32]),
     "sdq_attention": (ctypes.c_int, [_vp, _vp, _i32, _vp, _i64, ctypes.c_float, _vp, _vp, _vp, _sz, _vp]),
     "sdq_attention_status": (ctypes.c_int, [_vp, _vp]),
     "sdq_sample": (ctypes.c_int, [_vp, _i32, _i32, _i32, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "sdq_pages_step": (ctypes.c_int, [_vp, _vp]),
+    "sdq_adjust_logits": (ctypes.c_int, [_vp, _i32, _i32, _i32, _i64, _vp, _vp, _i64, _vp]),
     "sdq_status_string": (ctypes.c_char_p, [ctypes.c_int]),
 }
 
@@ -418,11 +442,21 @@ def _dtype(t) -> int:
 
 def sdq_cache_append(cache, batch, q_heads, q, k, v, rope, q_out, stream=None):
     """q, k, v: one row per token, of one type; their row strides are the tensors'."""
+    _check(lib().sdq_cache_append(cache, batch.ref, q_heads, *_rows_of(q, k, v), rope.ref, q_out.data_ptr(), _stream(stream)),
+           "sdq_cache_append")
+
+
+def _rows_of(q, k, v):
     kind = _dtype(q) if k.dtype == v.dtype == q.dtype else -1
     # (a single row has no stride of its own)
     ldq, ldk, ldv = (q.shape[1], k.shape[1], v.shape[1]) if q.shape[0] == 1 else (q.stride()[0], k.stride()[0], v.stride()[0])
-    _check(lib().sdq_cache_append(cache, batch.ref, q_heads, q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
-                                  kind, rope.ref, q_out.data_ptr(), _stream(stream)), "sdq_cache_append")
+    return q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, kind
+
+
+def sdq_cache_append_norm(cache, batch, q_heads, q, k, v, rope, norm, q_out, stream=None):
+    """As sdq_cache_append, the heads of q and k normalised by `norm` (a HeadNorm)."""
+    _check(lib().sdq_cache_append_norm(cache, batch.ref, q_heads, *_rows_of(q, k, v), rope.ref, norm.ref, q_out.data_ptr(),
+                                       _stream(stream)), "sdq_cache_append_norm")
 
 
 def sdq_attention_workspace_bytes(cache, batch, q_heads) -> int:
@@ -445,6 +479,19 @@ def sdq_sample(logits, u, temperature, top_k, top_p, min_p, tokens, stream=None)
     _check(lib().sdq_sample(logits.data_ptr(), _dtype(logits), rows, vocab, logits.stride(0) if rows > 1 else vocab,
                             u.data_ptr(), _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), tokens.data_ptr(),
                             _stream(stream)), "sdq_sample")
+
+
+def sdq_pages_step(step, stream=None):
+    """step: a ctypes struct ``sdq_pages``."""
+    _check(lib().sdq_pages_step(ctypes.addressof(step), _stream(stream)), "sdq_pages_step")
+
+
+def sdq_adjust_logits(logits, adjust, out, stream=None):
+    """logits, out: rows x vocab of one type, adjacent in a row; adjust: a ctypes struct ``sdq_adjust``."""
+    rows, vocab = logits.shape
+    _check(lib().sdq_adjust_logits(logits.data_ptr(), _dtype(logits), rows, vocab, logits.stride(0) if rows > 1 else vocab,
+                                   ctypes.addressof(adjust), out.data_ptr(), out.stride(0) if rows > 1 else vocab,
+                                   _stream(stream)), "sdq_adjust_logits")
 
 
 def sdq_status_string(status: int) -> str:
@@ -552,6 +599,66 @@ class Batch:
         self._checked = page_tokens
 
 
+class PageStep(NamedTuple):
+    """What ``PagePool.step`` found: token_start and own_len are a ``Batch``'s;
+    slots and positions are those of the step's tokens."""
+    token_start: object
+    own_len: object
+    n_free: object
+    slots: object
+    positions: object
+
+
+class PagePool:
+    """The free pages of a cache: ``free`` (int32, one entry per page, device),
+    of which the first ``n_free`` (int32, one element, device) are free, the
+    next to go out last.  Without tensors: all of n_pages pages, page 0 first."""
+
+    def __init__(self, page_tokens, free=None, n_free=None, n_pages=None, device="cuda"):
+        import torch
+        if free is None:
+            if n_pages is None or n_pages < 1:
+                raise ValueError("PagePool: needs the free pages, or how many pages there are")
+            free = torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device)
+        if n_free is None:
+            n_free = torch.full((1,), free.numel(), dtype=torch.int32, device=free.device)
+        for t in (free, n_free):
+            if t.dtype != torch.int32 or t.dim() != 1 or not t.is_cuda or not t.is_contiguous():
+                raise ValueError("PagePool: free and n_free must be contiguous 1-d int32 CUDA tensors")
+        if n_free.numel() != 1:
+            raise ValueError("PagePool: n_free has one element")
+        self.page_tokens, self.free, self.n_free = page_tokens, free, n_free
+
+    def step(self, own_len, new_len, pages, n_tokens, done=None, prefix_len=0, in_place=True, stream=None):
+        """One step's block tables (``sdq_pages_step``): sequences that are
+        `done` (int32, may be None) give their pages back, then each gets the
+        pages of its new_len new tokens, all of them or none; `pages` (sequences
+        x columns, int32) holds the tables.  n_tokens: the rows of the step.
+        own_len and the pool's count move on in place, or (in_place=False) stay
+        and come back as new tensors."""
+        import torch
+        i32, n_seqs = torch.int32, own_len.shape[0]
+        for t in (own_len, new_len, done):
+            if t is not None and (t.dtype is not i32 or tuple(t.shape) != (n_seqs,) or not t.is_contiguous() or not t.is_cuda):
+                raise ValueError("PagePool.step: own_len, new_len and done must be contiguous int32 CUDA tensors, one element "
+                                 "per sequence")
+        if pages.dtype is not i32 or pages.dim() != 2 or pages.shape[0] != n_seqs or not pages.is_cuda or (
+                pages.shape[1] > 1 and pages.stride(1) != 1):
+            raise ValueError("PagePool.step: pages must be an int32 CUDA tensor (sequences, columns), adjacent in a row")
+        if in_place and n_seqs > 0 and own_len.data_ptr() in (new_len.data_ptr(), None if done is None else done.data_ptr()):
+            raise ValueError("PagePool.step: own_len moves on in place and cannot be new_len or done too")
+        new = _empty((2 * n_seqs + 2 * n_tokens + 2,), i32, own_len.device, stream)
+        start, at = new[:n_seqs + 1], 2 * n_seqs + 2
+        own_out, n_free = (own_len, self.n_free) if in_place else (new[n_seqs + 1:2 * n_seqs + 1], new[2 * n_seqs + 1:at])
+        slots, positions = new[at:at + n_tokens], new[at + n_tokens:at + 2 * n_tokens]
+        columns = pages.shape[1]
+        sdq_pages_step(_Pages(self.page_tokens, self.free.shape[0], n_seqs, n_tokens, columns,
+                              pages.stride(0) if n_seqs > 1 else columns, prefix_len, own_len.data_ptr(), new_len.data_ptr(),
+                              _ptr(done), pages.data_ptr(), self.free.data_ptr(), self.n_free.data_ptr(), start.data_ptr(),
+                              own_out.data_ptr(), n_free.data_ptr(), slots.data_ptr(), positions.data_ptr()), stream)
+        return PageStep(start, own_out, n_free, slots, positions)
+
+
 class Rope:
     """Mirror of ``sdq_rope``: cos and sin tables (n_pos x dim / 2, fp32,
     device); ``Rope.table`` makes the usual ones, ``Rope()`` rotates nothing."""
@@ -574,6 +681,32 @@ class Rope:
         import torch
         cos, sin = sdq_rope_table(n_pos, dim, base)
         return cls(torch.from_numpy(cos).to(device), torch.from_numpy(sin).to(device), interleaved)
+
+
+class HeadNorm:
+    """Mirror of ``sdq_head_norm``: the weights of the heads' norms (fp32,
+    device, head_dim of them or heads x head_dim; None: those heads stay)."""
+
+    def __init__(self, q=None, k=None, eps=1e-6):
+        import torch
+        for t in (q, k):
+            if t is not None and (t.dtype != torch.float32 or t.dim() not in (1, 2) or not t.is_cuda or not t.is_contiguous()):
+                raise ValueError("HeadNorm: weights must be contiguous float32 CUDA tensors (head_dim) or (heads, head_dim)")
+        if not 0 < eps < float("inf"):
+            raise ValueError("HeadNorm: eps must be positive and finite")
+        self.tensors = (q, k)
+        self._c = _HeadNorm(_ptr(q), _ptr(k), int(q is not None and q.dim() == 2), int(k is not None and k.dim() == 2), eps)
+        self.ref = ctypes.addressof(self._c)
+        self._checked = None
+
+    def check(self, q_heads: int, kv_heads: int, head_dim: int):
+        """Raise where a weight is not of these heads."""
+        if self._checked == (q_heads, kv_heads, head_dim):
+            return
+        for t, heads in zip(self.tensors, (q_heads, kv_heads)):
+            if t is not None and tuple(t.shape) not in ((head_dim,), (heads, head_dim)):
+                raise ValueError("HeadNorm: weights are not of head_dim, or heads x head_dim, elements")
+        self._checked = q_heads, kv_heads, head_dim
 
 
 class KVCache:
@@ -603,10 +736,11 @@ class KVCache:
         except Exception:
             pass
 
-    def append(self, batch: Batch, q, k, v, rope: Rope, stream=None):
+    def append(self, batch: Batch, q, k, v, rope: Rope, stream=None, norm=None):
         """q, k, v: one row per token (fp32 or bf16; rows may be strided) ->
         the rotated queries (tokens x q_heads x head_dim, bf16); keys and
-        values go to the cache."""
+        values go to the cache.  norm: a HeadNorm, applied to every head of q
+        and k ahead of the rotation."""
         import torch
         d, tokens, shape = self.desc, batch.n_tokens, q.shape
         if (len(shape) != 2 or shape[0] != tokens or not k.shape == v.shape == (tokens, d.kv_heads * d.head_dim)
@@ -617,7 +751,11 @@ class KVCache:
             raise ValueError("KVCache.append: q's rows are not whole heads")
         batch.check(d.page_tokens)
         out = _empty((tokens, q_heads, d.head_dim), torch.bfloat16, q.device, stream)
-        sdq_cache_append(self.handle, batch, q_heads, q, k, v, rope, out, stream)
+        if norm is None:
+            sdq_cache_append(self.handle, batch, q_heads, q, k, v, rope, out, stream)
+        else:
+            norm.check(q_heads, d.kv_heads, d.head_dim)
+            sdq_cache_append_norm(self.handle, batch, q_heads, q, k, v, rope, norm, out, stream)
         return out
 
     def alloc_workspace(self, batch: Batch, q_heads: int, stream=None):
@@ -668,3 +806,56 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, stre
     tokens = _empty(rows, torch.int32, logits.device, stream)
     sdq_sample(logits, u, temperature, top_k, top_p, min_p, tokens, stream)
     return tokens
+
+
+def adjust_logits(logits, history=None, history_len=None, prompt_len=None, repetition=None, frequency=None, presence=None,
+                  bias_ids=None, bias=None, allowed=None, allowed_row=None, out=None, stream=None):
+    """Penalties for repeated tokens, biases and a grammar's allowed tokens on
+    logits (rows x vocab, fp32 or bf16; rows may be strided) -> logits of the
+    same type, in ``out`` if given (may be ``logits``).  history (rows x places,
+    int32; rows may be strided) holds each row's tokens so far, of which
+    history_len count (None: all) and prompt_len are the prompt's (None: 0);
+    repetition, frequency, presence: float32, one per row.  bias_ids (int32,
+    negative: unused) and bias (float32): rows x entries.  allowed (int32 words
+    of 32 tokens, sets x ceil(vocab / 32)), allowed_row: the set of each row
+    (int32, -1 for none; None: row i has set i)."""
+    import torch
+    shape, i32, f32 = logits.shape, torch.int32, torch.float32
+    if len(shape) != 2 or logits.stride()[1] != 1 or not logits.is_cuda:
+        raise ValueError("adjust_logits: logits must be a CUDA tensor (rows, vocab) with adjacent elements in a row")
+    rows, vocab = shape
+    for t, dtype in ((history_len, i32), (prompt_len, i32), (repetition, f32), (frequency, f32), (presence, f32), (allowed_row, i32)):
+        if t is not None and (t.dtype is not dtype or t.shape != shape[:1] or not t.is_contiguous() or not t.is_cuda):
+            raise ValueError("adjust_logits: repetition, frequency and presence are float32, history_len, prompt_len and "
+                             "allowed_row int32, one per row, on the GPU")
+    for t, dtype, n in ((history, i32, rows), (bias_ids, i32, rows), (bias, f32, rows), (allowed, i32, None)):
+        if t is not None and (t.dtype is not dtype or t.dim() != 2 or not t.is_cuda or (n is not None and t.shape[0] != n)
+                              or (t.shape[1] > 1 and t.stride()[1] != 1)):
+            raise ValueError("adjust_logits: history, bias_ids and bias need one row for each of logits, allowed one for each "
+                             "set: 2-d CUDA tensors, int32 (bias: float32), adjacent in a row")
+    if (bias_ids is None) != (bias is None) or (bias is not None and bias.shape != bias_ids.shape):
+        raise ValueError("adjust_logits: bias_ids and bias come together, of one shape")
+    if history is None and (history_len is not None or prompt_len is not None):
+        raise ValueError("adjust_logits: history_len and prompt_len belong to a history")
+    if allowed is None and allowed_row is not None:
+        raise ValueError("adjust_logits: allowed_row belongs to allowed")
+    if out is None:
+        out = _empty(shape, logits.dtype, logits.device, stream)
+    elif out.shape != shape or out.dtype is not logits.dtype or out.stride()[1] != 1 or not out.is_cuda:
+        raise ValueError("adjust_logits: out must be like logits")
+    a = _Adjust()
+    if history is not None:
+        a.history, a.history_max = history.data_ptr() or None, history.shape[1]
+        a.history_stride = history.stride(0)
+        a.history_len, a.prompt_len = _ptr(history_len), _ptr(prompt_len)
+        a.repetition, a.frequency, a.presence = _ptr(repetition), _ptr(frequency), _ptr(presence)
+    if bias is not None and bias.shape[1]:
+        a.bias_ids, a.bias, a.n_bias = bias_ids.data_ptr(), bias.data_ptr(), bias.shape[1]
+        a.bias_ids_stride, a.bias_stride = bias_ids.stride(0), bias.stride(0)
+    if allowed is not None:
+        if allowed.shape[1] < (vocab + 31) // 32:
+            raise ValueError("adjust_logits: the sets of allowed have too few words")
+        a.allowed, a.allowed_row, a.n_allowed = allowed.data_ptr(), _ptr(allowed_row), allowed.shape[0]
+        a.allowed_stride = allowed.stride(0)
+    sdq_adjust_logits(logits, a, out, stream)
+    return out

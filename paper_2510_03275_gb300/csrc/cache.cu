@@ -23,6 +23,7 @@ struct AppendParams {
   uint16_t *kp, *vp, *q_out;
   int q_heads, kv_heads, dim, page, n_pages;
   int per_part;   // 8-element units of a token that one block of a part takes
+  sdq_head_norm norm;
 };
 
 // Four consecutive elements in fp32.
@@ -43,7 +44,9 @@ __device__ __forceinline__ void store4(uint16_t* p, float4 a) {
 // tokens, grid.y: parts of a token's heads.  2566 tokens of 64 + 2 x 8 heads of
 // 128, fp32: 28 us (84 % of the measured copy bandwidth); one token: 1.8 us (a
 // graph of 30 calls).
-template <class T>
+// kNorm: a head's threads are neighbours in one warp (8 or 16 of them) and add up
+// its squares, all in fp32; whole warps stay in the loop for it.
+template <class T, bool kNorm>
 __global__ void __launch_bounds__(kThreads) append_kernel(AppendParams p) {
   pdl_wait();
   pdl_launch_dependents();
@@ -57,10 +60,11 @@ __global__ void __launch_bounds__(kThreads) append_kernel(AppendParams p) {
   const bool keep = page >= 0 && page < p.n_pages;
   const int units = (p.q_heads + 2 * p.kv_heads) * per_head;
   const int end = min(units, ((int)blockIdx.y + 1) * p.per_part);
-  for (int u = blockIdx.y * p.per_part + threadIdx.x; u < end; u += kThreads) {
+  for (int i = blockIdx.y * p.per_part + threadIdx.x; (kNorm ? i & ~31 : i) < end; i += kThreads) {
+    const int u = kNorm ? min(i, end - 1) : i;   // (parts are whole heads; a lane past the end only takes part in the sums)
     const int h = u / per_head, c = u - h * per_head;
     const bool is_q = h < p.q_heads, is_v = h >= p.q_heads + p.kv_heads;
-    const int kh = is_v ? h - p.q_heads - p.kv_heads : h - p.q_heads;
+    const int kh = is_v ? h - p.q_heads - p.kv_heads : is_q ? h : h - p.q_heads;
     const T* src = is_q   ? static_cast<const T*>(p.q) + t * p.ldq + h * p.dim
                    : is_v ? static_cast<const T*>(p.v) + t * p.ldv + kh * p.dim
                           : static_cast<const T*>(p.k) + t * p.ldk + kh * p.dim;
@@ -68,6 +72,19 @@ __global__ void __launch_bounds__(kThreads) append_kernel(AppendParams p) {
     const bool split = turn && !p.rope.interleaved;
     const int ea = split ? 4 * c : 8 * c, eb = split ? 4 * c + half : 8 * c + 4;
     float4 a = load4(src + ea), b = load4(src + eb);
+    if (kNorm) {
+      float sq = a.x * a.x + a.y * a.y + (a.z * a.z + a.w * a.w) + (b.x * b.x + b.y * b.y + (b.z * b.z + b.w * b.w));
+      for (int d = 1; d < per_head; d <<= 1) sq += __shfl_xor_sync(0xffffffffu, sq, d);
+      const float* w = is_q ? p.norm.q : is_v ? nullptr : p.norm.k;
+      if (w) {
+        if (is_q ? p.norm.q_per_head : p.norm.k_per_head) w += kh * p.dim;
+        const float r = rsqrtf(sq / (float)p.dim + p.norm.eps);
+        const float4 wa = load4(w + ea), wb = load4(w + eb);
+        a = make_float4(a.x * r * wa.x, a.y * r * wa.y, a.z * r * wa.z, a.w * r * wa.w);
+        b = make_float4(b.x * r * wb.x, b.y * r * wb.y, b.z * r * wb.z, b.w * r * wb.w);
+      }
+      if (i >= end) continue;
+    }
     if (turn) {
       const float4 cs = load4(p.rope.cos + (int64_t)pos * half + 4 * c);
       const float4 sn = load4(p.rope.sin + (int64_t)pos * half + 4 * c);
@@ -189,9 +206,9 @@ extern "C" int sdq_rope_table(int32_t n_pos, int32_t dim, double base, float* co
   return SDQ_OK;
 }
 
-extern "C" int sdq_cache_append(sdq_cache c, const sdq_batch* b, int32_t q_heads, const void* q, int64_t ldq,
-                                const void* k, int64_t ldk, const void* v, int64_t ldv, int32_t type,
-                                const sdq_rope* rope, uint16_t* q_out, void* stream) {
+static int append(sdq_cache c, const sdq_batch* b, int32_t q_heads, const void* q, int64_t ldq, const void* k, int64_t ldk,
+                  const void* v, int64_t ldv, int32_t type, const sdq_rope* rope, const sdq_head_norm* norm, uint16_t* q_out,
+                  void* stream) {
   int st = check_batch(c, b, q_heads);
   if (st != SDQ_OK) return st;
   if ((st = check_cache_device(c)) != SDQ_OK) return st;
@@ -204,7 +221,13 @@ extern "C" int sdq_cache_append(sdq_cache c, const sdq_batch* b, int32_t q_heads
     if (!rope->cos || !rope->sin || !multiple16(rope->cos, 0, 4) || !multiple16(rope->sin, 0, 4)) return SDQ_ERR_INVALID_ARG;
     if (rope->n_pos < 1 || rope->n_pos < (int64_t)b->prefix_len + b->max_own) return SDQ_ERR_INVALID_ARG;
   }
+  if (norm) {
+    if (!multiple16(norm->q, 0, 4) || !multiple16(norm->k, 0, 4)) return SDQ_ERR_INVALID_ARG;
+    if ((norm->q_per_head != 0 && norm->q_per_head != 1) || (norm->k_per_head != 0 && norm->k_per_head != 1)) return SDQ_ERR_INVALID_ARG;
+    if (!(norm->eps > 0.f) || !std::isfinite(norm->eps)) return SDQ_ERR_INVALID_ARG;
+  }
   AppendParams p;
+  p.norm = norm ? *norm : sdq_head_norm{};
   p.b = *b;
   p.rope = *rope;
   p.q = q; p.k = k; p.v = v;
@@ -215,8 +238,23 @@ extern "C" int sdq_cache_append(sdq_cache c, const sdq_batch* b, int32_t q_heads
   const int parts = std::max(1, std::min((units + kThreads - 1) / kThreads, 2 * c->sm_count / b->n_tokens));
   p.per_part = ((units + parts - 1) / parts + kThreads - 1) / kThreads * kThreads;
   const dim3 grid((unsigned)b->n_tokens, (unsigned)((units + p.per_part - 1) / p.per_part));
-  const cudaError_t e = type == SDQ_F32
-                            ? launch_pdl(append_kernel<float>, grid, dim3(kThreads), 0, (cudaStream_t)stream, p)
-                            : launch_pdl(append_kernel<uint16_t>, grid, dim3(kThreads), 0, (cudaStream_t)stream, p);
+  cudaStream_t cs = (cudaStream_t)stream;
+  auto run = [&](auto kernel) { return launch_pdl(kernel, grid, dim3(kThreads), 0, cs, p); };
+  const cudaError_t e = type == SDQ_F32 ? norm ? run(append_kernel<float, true>) : run(append_kernel<float, false>)
+                        : norm          ? run(append_kernel<uint16_t, true>)
+                                        : run(append_kernel<uint16_t, false>);
   return e == cudaSuccess ? SDQ_OK : SDQ_ERR_CUDA;
+}
+
+extern "C" int sdq_cache_append(sdq_cache c, const sdq_batch* b, int32_t q_heads, const void* q, int64_t ldq,
+                                const void* k, int64_t ldk, const void* v, int64_t ldv, int32_t type,
+                                const sdq_rope* rope, uint16_t* q_out, void* stream) {
+  return append(c, b, q_heads, q, ldq, k, ldk, v, ldv, type, rope, nullptr, q_out, stream);
+}
+
+extern "C" int sdq_cache_append_norm(sdq_cache c, const sdq_batch* b, int32_t q_heads, const void* q, int64_t ldq,
+                                     const void* k, int64_t ldk, const void* v, int64_t ldv, int32_t type,
+                                     const sdq_rope* rope, const sdq_head_norm* norm, uint16_t* q_out, void* stream) {
+  if (!norm) return SDQ_ERR_INVALID_ARG;
+  return append(c, b, q_heads, q, ldq, k, ldk, v, ldv, type, rope, norm, q_out, stream);
 }
