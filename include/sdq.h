@@ -562,8 +562,20 @@ int sdq_cache_append_norm(sdq_cache cache, const sdq_batch* batch, int32_t q_hea
 size_t sdq_attention_workspace_bytes(sdq_cache cache, const sdq_batch* batch, int32_t q_heads);
 int sdq_attention(sdq_cache cache, const sdq_batch* batch, int32_t q_heads, const uint16_t* q, int64_t ldq,
                   float scale, uint16_t* out, float* lse, void* ws, size_t ws_bytes, void* stream);
-/* Wait for `stream`, then report whether the last sdq_attention call on `ws`
- * completed its bounded device-side waits: SDQ_OK or SDQ_ERR_TIMEOUT (as
+/* The same where a token sees a window of positions and the first ones: a token
+ * at position p = prefix_len + a (an empty slot, and a token without a place of
+ * its own, stands at prefix_len - 1) sees, of the keys at positions j <= p,
+ * those with j > p - window or j < sinks.  Positions count the prefix; keys that
+ * no token of a sequence sees are not read.  window 1 .. 2^30 - 1 (its own key among them), sinks 0 ..
+ * 2^30 - 1.  Every sequence reads what it sees of the prefix for itself.  All
+ * else as sdq_attention; the workspace is this call's own size. */
+size_t sdq_attention_window_workspace_bytes(sdq_cache cache, const sdq_batch* batch, int32_t q_heads, int32_t window,
+                                            int32_t sinks);
+int sdq_attention_window(sdq_cache cache, const sdq_batch* batch, int32_t q_heads, const uint16_t* q, int64_t ldq,
+                         float scale, int32_t window, int32_t sinks, uint16_t* out, float* lse, void* ws, size_t ws_bytes,
+                         void* stream);
+/* Wait for `stream`, then report whether the last sdq_attention or
+ * sdq_attention_window call on `ws` completed its bounded device-side waits: SDQ_OK or SDQ_ERR_TIMEOUT (as
  * sdq_workspace_status). */
 int sdq_attention_status(const void* ws, void* stream);
 

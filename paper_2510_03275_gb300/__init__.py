@@ -32,6 +32,7 @@ __all__ = [
     "sdq_attention_workspace_bytes", "sdq_attention", "sdq_attention_status",
     "sdq_sample", "sample",
     "HeadNorm", "sdq_cache_append_norm", "PagePool", "PageStep", "sdq_pages_step", "sdq_adjust_logits", "adjust_logits",
+    "sdq_attention_window", "sdq_attention_window_workspace_bytes",
 ]
 
 SDQ_OK = 0
@@ -169,6 +170,8 @@ _SIGS = {
     "sdq_cache_append_norm": (ctypes.c_int, [_vp, _vp, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _vp, _vp, _vp, _vp]),
     "sdq_attention_workspace_bytes": (_sz, [_vp, _vp, _i32]),
     "sdq_attention": (ctypes.c_int, [_vp, _vp, _i32, _vp, _i64, ctypes.c_float, _vp, _vp, _vp, _sz, _vp]),
+    "sdq_attention_window_workspace_bytes": (_sz, [_vp, _vp, _i32, _i32, _i32]),
+    "sdq_attention_window": (ctypes.c_int, [_vp, _vp, _i32, _vp, _i64, ctypes.c_float, _i32, _i32, _vp, _vp, _vp, _sz, _vp]),
     "sdq_attention_status": (ctypes.c_int, [_vp, _vp]),
     "sdq_sample": (ctypes.c_int, [_vp, _i32, _i32, _i32, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
     "sdq_pages_step": (ctypes.c_int, [_vp, _vp]),
@@ -468,6 +471,16 @@ def sdq_attention(cache, batch, q_heads, q, ldq, scale, out, lse, ws, stream=Non
                                ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream)), "sdq_attention")
 
 
+def sdq_attention_window_workspace_bytes(cache, batch, q_heads, window, sinks) -> int:
+    return lib().sdq_attention_window_workspace_bytes(cache, batch.ref, q_heads, window, sinks)
+
+
+def sdq_attention_window(cache, batch, q_heads, q, ldq, scale, window, sinks, out, lse, ws, stream=None):
+    _check(lib().sdq_attention_window(cache, batch.ref, q_heads, q.data_ptr(), ldq, scale, window, sinks, out.data_ptr(),
+                                      _ptr(lse), ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream)),
+           "sdq_attention_window")
+
+
 def sdq_attention_status(ws, stream=None) -> int:
     """Synchronize and return the status of the last attention call on ``ws``."""
     return lib().sdq_attention_status(_ptr(ws), _stream(stream))
@@ -758,18 +771,23 @@ class KVCache:
             sdq_cache_append_norm(self.handle, batch, q_heads, q, k, v, rope, norm, out, stream)
         return out
 
-    def alloc_workspace(self, batch: Batch, q_heads: int, stream=None):
-        """For ``attend`` on this batch (or one of the same integers)."""
+    def alloc_workspace(self, batch: Batch, q_heads: int, stream=None, window=None, sinks=0):
+        """For ``attend`` on this batch (or one of the same integers) with this window."""
         import torch
-        n = sdq_attention_workspace_bytes(self.handle, batch, q_heads)
+        if window is None:
+            n = sdq_attention_workspace_bytes(self.handle, batch, q_heads)
+        else:
+            n = sdq_attention_window_workspace_bytes(self.handle, batch, q_heads, window, sinks)
         if n == 0:
-            raise SdqError(-1, "sdq_attention_workspace_bytes")
+            raise SdqError(-1, "sdq_attention_workspace_bytes" if window is None else "sdq_attention_window_workspace_bytes")
         return _empty(n, torch.uint8, self.k_pages.device, stream)
 
-    def attend(self, batch: Batch, q, scale=None, ws=None, lse=None, stream=None):
+    def attend(self, batch: Batch, q, scale=None, ws=None, lse=None, stream=None, window=None, sinks=0):
         """q (tokens x q_heads x head_dim, bf16; tokens may be strided) ->
         outputs of the same shape in bf16.  scale: 1 / sqrt(head_dim) unless
-        given; lse: fp32 (tokens x q_heads), written if given."""
+        given; lse: fp32 (tokens x q_heads), written if given.  window: a token
+        sees that many positions up to its own, and the first `sinks` ones
+        (positions count the prefix); None: all of them."""
         import torch
         d, tokens, dim, shape = self.desc, batch.n_tokens, self.desc.head_dim, q.shape
         if len(shape) != 3 or shape[0] != tokens or shape[2] != dim or q.dtype != torch.bfloat16 or not q.is_cuda:
@@ -780,14 +798,19 @@ class KVCache:
         if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (tokens, heads)
                                 or not lse.is_contiguous() or not lse.is_cuda):
             raise ValueError("KVCache.attend: lse must be a contiguous float32 CUDA tensor (tokens, q_heads)")
+        if window is None and sinks != 0:
+            raise ValueError("KVCache.attend: sinks belong to a window")
         batch.check(d.page_tokens)
         if ws is None:
-            ws = self.alloc_workspace(batch, heads, stream)
+            ws = self.alloc_workspace(batch, heads, stream, window, sinks)
         elif not ws.is_cuda or not ws.is_contiguous():
             raise ValueError("KVCache.attend: ws must be a contiguous CUDA tensor")
         out = _empty((tokens, heads, dim), torch.bfloat16, q.device, stream)
-        sdq_attention(self.handle, batch, heads, q, stride[0] if tokens > 1 else heads * dim,
-                      dim ** -0.5 if scale is None else scale, out, lse, ws, stream)
+        ldq, scale = stride[0] if tokens > 1 else heads * dim, dim ** -0.5 if scale is None else scale
+        if window is None:
+            sdq_attention(self.handle, batch, heads, q, ldq, scale, out, lse, ws, stream)
+        else:
+            sdq_attention_window(self.handle, batch, heads, q, ldq, scale, window, sinks, out, lse, ws, stream)
         return out
 
 

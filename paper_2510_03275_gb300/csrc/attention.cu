@@ -67,13 +67,18 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendParams p) {
 // kernel takes a thread block for every 256 of them, or fewer.  Where a sequence
 // brings 128 rows and more on the average, its row blocks run over the prefix
 // and its own keys in one line; below that the batch's rows share blocks against
-// the prefix, and the two parts' results are joined.
+// the prefix, and the two parts' results are joined.  With a window every
+// sequence's rows run over what they see of the prefix and of their own keys in
+// one line, on the kernel of their number.
 constexpr int kPrefixNarrowRows = 8;
 
 void set_route(const sdq_cache_s* c, const sdq_batch* b, int q_heads, AttendParams* p) {
   const int group = q_heads / c->desc.kv_heads;
-  const int64_t own_rows = b->max_own > 0 ? (int64_t)b->max_new * group : 0;
-  const int64_t prefix_rows = b->prefix_len > 0 ? (int64_t)b->n_tokens * group : 0;
+  // (a window, or first tokens, that cover every position leave nothing out)
+  if ((int64_t)std::max(p->window, p->sinks) >= (int64_t)b->prefix_len + b->max_own) p->window = p->sinks = 0;
+  const bool window = p->window > 0;
+  const int64_t own_rows = b->max_own > 0 || (window && b->prefix_len > 0) ? (int64_t)b->max_new * group : 0;
+  const int64_t prefix_rows = b->prefix_len > 0 && !window ? (int64_t)b->n_tokens * group : 0;
   const bool own_wide = own_rows > kNarrowRows;
   p->b = *b;
   p->group = group;
@@ -86,7 +91,7 @@ void set_route(const sdq_cache_s* c, const sdq_batch* b, int q_heads, AttendPara
   p->narrow[kPrefix] = prefix_rows > 0 && prefix_rows <= kPrefixNarrowRows;
   p->parts = p->wide[kOwn] + p->narrow[kOwn] + p->wide[kPrefix] + p->narrow[kPrefix];
   for (int part = 0; part < 2; ++part) {
-    p->splits[part] = p->wide[part] ? wide_splits(c, b, q_heads, part, p->chained, part == kPrefix && p->narrow[kOwn]) : 0;
+    p->splits[part] = p->wide[part] ? wide_splits(c, *p, q_heads, part, part == kPrefix && p->narrow[kOwn]) : 0;
   }
   p->ctas = c->sm_count;
   // Beside a wide kernel that leaves SMs free, the narrow one's first thread
@@ -94,7 +99,7 @@ void set_route(const sdq_cache_s* c, const sdq_batch* b, int q_heads, AttendPara
   // take ahead what they can read until then (40 bytes a ns and SM).
   if (p->wide[kPrefix] && p->narrow[kOwn]) {
     p->early = c->sm_count - (int)std::min<int64_t>(wide_grid(c, *p, kPrefix), c->sm_count);
-    p->ahead = (int)((wide_time(c, b, q_heads, kPrefix, false, p->splits[kPrefix]) + kNarrowStart) * 40e3 / (64.0 * c->desc.head_dim * narrow_warps()));
+    p->ahead = (int)((wide_time(c, *p, q_heads, kPrefix, p->splits[kPrefix]) + kNarrowStart) * 40e3 / (64.0 * c->desc.head_dim * narrow_warps()));
   }
 }
 
@@ -115,7 +120,7 @@ AttendWs attend_workspace(const sdq_cache_s* c, const sdq_batch* b, int q_heads,
     L.o[part] = take(p.parts > 1 && p.splits[part] <= 1 ? sizeof(float) * rows * d : 0);
     L.split_ml[part] = take(p.splits[part] > 1 ? sizeof(float2) * p.splits[part] * rows : 0);
     L.split_o[part] = take(p.splits[part] > 1 ? sizeof(float) * p.splits[part] * rows * d : 0);
-    const size_t slots = p.narrow[part] ? (size_t)p.ctas * 8 * narrow_groups(b, p.group, part) : 0;
+    const size_t slots = p.narrow[part] ? (size_t)p.ctas * 8 * narrow_groups(p, part) : 0;
     L.warp_o[part] = take(sizeof(float) * slots * narrow_warps() * d);
     L.block_ml[part] = take(sizeof(float2) * 2 * slots);
     L.block_o[part] = take(sizeof(float) * 2 * slots * d);
@@ -152,15 +157,26 @@ int log2_of(int v) {
 
 using namespace sdq;
 
-extern "C" size_t sdq_attention_workspace_bytes(sdq_cache c, const sdq_batch* b, int32_t q_heads) {
+static size_t workspace_bytes(sdq_cache c, const sdq_batch* b, int32_t q_heads, int32_t window, int32_t sinks) {
   if (check_batch(c, b, q_heads) != SDQ_OK) return 0;
   AttendParams p{};
+  p.window = window;
+  p.sinks = sinks;
   set_route(c, b, q_heads, &p);
   return attend_workspace(c, b, q_heads, p).total;
 }
 
-extern "C" int sdq_attention(sdq_cache c, const sdq_batch* b, int32_t q_heads, const uint16_t* q, int64_t ldq, float scale,
-                             uint16_t* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+static bool valid_window(int32_t window, int32_t sinks) { return window >= 1 && window < (1 << 30) && sinks >= 0 && sinks < (1 << 30); }
+
+extern "C" size_t sdq_attention_workspace_bytes(sdq_cache c, const sdq_batch* b, int32_t q_heads) {
+  return workspace_bytes(c, b, q_heads, 0, 0);
+}
+extern "C" size_t sdq_attention_window_workspace_bytes(sdq_cache c, const sdq_batch* b, int32_t q_heads, int32_t window, int32_t sinks) {
+  return valid_window(window, sinks) ? workspace_bytes(c, b, q_heads, window, sinks) : 0;
+}
+
+static int attention(sdq_cache c, const sdq_batch* b, int32_t q_heads, const uint16_t* q, int64_t ldq, float scale, int32_t window,
+                     int32_t sinks, uint16_t* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
   int st = check_batch(c, b, q_heads);
   if (st != SDQ_OK) return st;
   if ((st = check_cache_device(c)) != SDQ_OK) return st;
@@ -170,6 +186,8 @@ extern "C" int sdq_attention(sdq_cache c, const sdq_batch* b, int32_t q_heads, c
   if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & 15u) return SDQ_ERR_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(ws) & 255u) || (reinterpret_cast<uintptr_t>(lse) & 3u)) return SDQ_ERR_INVALID_ARG;
   AttendParams p{};
+  p.window = window;
+  p.sinks = sinks;
   set_route(c, b, q_heads, &p);
   const AttendWs L = attend_workspace(c, b, q_heads, p);
   if (ws_bytes < L.total) return SDQ_ERR_WORKSPACE;
@@ -194,6 +212,18 @@ extern "C" int sdq_attention(sdq_cache c, const sdq_batch* b, int32_t q_heads, c
   }
   const cudaError_t e = launch_parts(c, p, (cudaStream_t)stream);
   return e == cudaSuccess ? SDQ_OK : SDQ_ERR_CUDA;
+}
+
+extern "C" int sdq_attention(sdq_cache c, const sdq_batch* b, int32_t q_heads, const uint16_t* q, int64_t ldq, float scale,
+                             uint16_t* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  return attention(c, b, q_heads, q, ldq, scale, 0, 0, out, lse, ws, ws_bytes, stream);
+}
+
+extern "C" int sdq_attention_window(sdq_cache c, const sdq_batch* b, int32_t q_heads, const uint16_t* q, int64_t ldq, float scale,
+                                    int32_t window, int32_t sinks, uint16_t* out, float* lse, void* ws, size_t ws_bytes,
+                                    void* stream) {
+  if (!valid_window(window, sinks)) return SDQ_ERR_INVALID_ARG;
+  return attention(c, b, q_heads, q, ldq, scale, window, sinks, out, lse, ws, ws_bytes, stream);
 }
 
 extern "C" int sdq_attention_status(const void* ws, void* stream) {

@@ -35,6 +35,7 @@ struct AttendParams {
   float scale;              // softmax scale times log2(e)
   int q_heads, kv_heads, group, page_shift, box_shift, n_pages;
   uint32_t group_inverse;   // 2^16 / group + 1
+  int window, sinks;        // a token sees its last `window` positions and the first `sinks` (window 0: all)
   int narrow[2], wide[2];   // which kernel takes a part (neither: it has no keys)
   int parts;                // parts that are computed apart (1, 2)
   int chained;              // the wide kernel's rows of kOwn run over the prefix first (no kPrefix part)
@@ -47,6 +48,26 @@ struct AttendParams {
   float2 *ml[2], *split_ml[2], *block_ml[2];
   int ctas;                 // thread blocks of the narrow kernel
 };
+
+// With a window: the tiles of `keys` keys, the first at position `base`, that a
+// run of tokens sees, whose first is at position `first` and whose last sees up
+// to the last key.  They are tiles 0 .. a - 1 and those from a + skip on.
+struct Line {
+  int a, skip, tiles;
+  __device__ int tile(int i) const { return i < a ? i : i + skip; }
+};
+template <int K>
+__device__ __forceinline__ Line line_of(const AttendParams& p, int keys, int base, int first) {
+  Line l;
+  const int all = (keys + K - 1) / K, low = first - p.window + 1 - base;
+  l.a = (min(max(p.sinks - base, 0), keys) + K - 1) / K;
+  l.skip = max(l.a, low >= keys ? all : max(low, 0) / K) - l.a;
+  l.tiles = all - l.skip;
+  return l;
+}
+// The position of a sequence's token at place `at` among its own (a token that
+// has none stands behind the prefix).
+__device__ __forceinline__ int position_of(const AttendParams& p, int at) { return p.b.prefix_len + max(at, -1); }
 
 __device__ __forceinline__ float exp2_approx(float x) {
   float r;
@@ -112,15 +133,15 @@ __device__ __forceinline__ void write_row(const AttendParams& p, int64_t row, co
 
 // The narrow kernel on `part`; late: behind this call's kernel on the prefix,
 // beside which it may run.
-int narrow_groups(const sdq_batch* b, int group, int part);   // of 8 query rows (1 to 4; 0 without keys)
+int narrow_groups(const AttendParams& p, int part);           // of 8 query rows (1 to 4; 0 without keys)
 int narrow_warps();                                           // per thread block
 cudaError_t launch_narrow(const sdq_cache_s* c, const AttendParams& p, int part, bool late, cudaStream_t st);
 // The wide kernel on `part`, and how many thread blocks share the keys of a
 // row block (p.splits[part]); narrow: the narrow kernel runs beside it.
 constexpr int kMaxWideSplits = 16;
 constexpr double kNarrowStart = 4.0;   // us that the narrow kernel takes beyond its reading
-int wide_splits(const sdq_cache_s* c, const sdq_batch* b, int q_heads, int part, bool chained, bool narrow);
-double wide_time(const sdq_cache_s* c, const sdq_batch* b, int q_heads, int part, bool chained, int splits);   // us, estimated
+int wide_splits(const sdq_cache_s* c, const AttendParams& p, int q_heads, int part, bool narrow);
+double wide_time(const sdq_cache_s* c, const AttendParams& p, int q_heads, int part, int splits);   // us, estimated
 int64_t wide_grid(const sdq_cache_s* c, const AttendParams& p, int part);   // thread blocks
 cudaError_t launch_wide(const sdq_cache_s* c, const AttendParams& p, int part, cudaStream_t st);
 

@@ -83,8 +83,21 @@ struct Unit {
 // Row r of a unit: its token (r below 32: exact).
 __device__ __forceinline__ int token_of(const AttendParams& p, int r) { return (int)((uint32_t)r * p.group_inverse >> 16); }
 
+// With a window: the tiles of a sequence's unit, first those of the prefix.
+struct UnitLine {
+  Line prefix, own;
+  __device__ int tiles() const { return prefix.tiles + own.tiles; }
+  __device__ bool in_prefix(int i) const { return i < prefix.tiles; }
+  __device__ int tile(int i) const { return i < prefix.tiles ? prefix.tile(i) : own.tile(i - prefix.tiles); }
+};
+__device__ __forceinline__ UnitLine unit_line(const AttendParams& p, int count, int own) {
+  const int first = position_of(p, own - count);
+  return UnitLine{line_of<kTile>(p, p.b.prefix_len, 0, first), line_of<kTile>(p, own, p.b.prefix_len, first)};
+}
+
 // The line of units that have tiles.  All of it by whole warps: a lane holds
 // the span of one of 32 consecutive sequences.
+template <bool kWindow>
 struct Walk {
   const AttendParams& p;
   const int part;
@@ -98,7 +111,10 @@ struct Walk {
     held = SeqSpan{0, 0, 0};
     if (s < p.b.n_seqs) held = seq_span(p.b, s);
   }
-  __device__ static int tiles_of(const SeqSpan& q) { return q.count > 0 ? (q.own + kTile - 1) / kTile : 0; }   // per key head
+  __device__ int tiles_of(const SeqSpan& q) const {   // per key head
+    if (kWindow) return q.count > 0 ? unit_line(p, q.count, q.own).tiles() : 0;
+    return q.count > 0 ? (q.own + kTile - 1) / kTile : 0;
+  }
   __device__ static int places_of(int tiles) { return tiles > 0 ? tiles + kUnitCost : 0; }
   // All places.
   __device__ int64_t total() {
@@ -326,7 +342,7 @@ __device__ __forceinline__ void finish(const AttendParams& p, const Pieces<NT>& 
   if (p.lse && first) p.lse[row] = natural_lse(top, sum);
 }
 
-template <int D, int NT>
+template <int D, int NT, bool kWindow>
 __global__ void __launch_bounds__(kThreads, 1)
     narrow_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
                   const __grid_constant__ AttendParams p, const int part, const int late) {
@@ -354,7 +370,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (!late) pdl_wait();
   pdl_launch_dependents();
   call_record_start(p.rec, p.call, blockIdx.x == 0 && tid == 0);
-  Walk walk(p, part);
+  Walk<kWindow> walk(p, part);
   const int64_t total = walk.total();
   const Shares shares(p, part, total, gridDim.x);
   const int64_t share = shares.of(blockIdx.x), ct0 = shares.begin(blockIdx.x), ct1 = min(total, ct0 + kWarps * share);
@@ -371,23 +387,27 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (warp == 0 && lane == 0 && u.a < ct0) ticket_install(p.tickets[part] + (part == kPrefix ? u.h : (int64_t)u.s * p.kv_heads + u.h), p.call);
     // ---- copies: tile ti of unit ui is the next, if it is one of this share's; `page` of tile pb + lane of sequence ps
     int ti = (int)(t0 - u.a), ki = 0, pb = 0, ps = -2, page = -1;
+    UnitLine line, line_i;   // with a window: of u, of ui
+    if (kWindow) line = line_i = unit_line(p, u.count, u.keys);
     const int per_page = p.page_shift - 4;   // log2 of tiles per page
     auto issue = [&]() {
       if (ti >= ui.tiles) {
-        if (ui.a + Walk::places_of(ui.tiles) >= t1) return;
+        if (ui.a + walk.places_of(ui.tiles) >= t1) return;
         walk.next(ui);
         ti = 0;
+        if (kWindow) line_i = unit_line(p, ui.count, ui.keys);
       }
       if (ui.a + ti >= t1) return;
       if (ui.s != ps || ti < pb || ti >= pb + 32) {
         ps = ui.s;
         pb = ti;
-        const int32_t* table = part == kPrefix ? p.b.prefix_pages : p.b.pages + (int64_t)ui.s * p.b.page_stride;
-        page = ti + lane < ui.tiles ? __ldg(table + ((ti + lane) >> per_page)) : -1;
+        const int32_t* table = part == kPrefix || (kWindow && line_i.in_prefix(ti + lane)) ? p.b.prefix_pages
+                                                                                           : p.b.pages + (int64_t)ui.s * p.b.page_stride;
+        page = ti + lane < ui.tiles ? __ldg(table + ((kWindow ? line_i.tile(ti + lane) : ti + lane) >> per_page)) : -1;
       }
-      const int pg = __shfl_sync(0xffffffffu, page, ti - pb);
+      const int pg = __shfl_sync(0xffffffffu, page, ti - pb), tile = kWindow ? line_i.tile(ti) : ti;
       // (a page outside the cache: rows outside the arrays, which read as zeros)
-      const int y = pg >= 0 && pg < p.n_pages ? ((pg * p.kv_heads + ui.h) << p.page_shift) + ((ti & ((1 << per_page) - 1)) << 4) : -kTile;
+      const int y = pg >= 0 && pg < p.n_pages ? ((pg * p.kv_heads + ui.h) << p.page_shift) + ((tile & ((1 << per_page) - 1)) << 4) : -kTile;
       const int st = ki % ST;
       const uint32_t bar = smem_u32(&full[warp][st]), dst = ring_a + st * 2 * S::kMat;
       mbar_expect_tx_warp(&full[warp][st], 2 * S::kMat);
@@ -406,6 +426,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       // query rows as the products' B operand; rows past the last are zero
       uint32_t qf[NT][D / 16][2];
       int lim[NT][2];   // keys that this lane's two queries of each 8 see
+      int low[NT][2];   // with a window: the first position of theirs
+      if (kWindow) line = unit_line(p, u.count, u.keys);
       float o[NT][D / 16][4], m[NT][2], l[NT][2];
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
@@ -419,6 +441,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int j = 0; j < 2; ++j) {
           const int rj = 8 * n + c2 + j;
           lim[n][j] = part == kPrefix || rj >= u.rows ? u.keys : u.keys - u.count + token_of(p, rj) + 1;
+          if (kWindow) low[n][j] = rj >= u.rows ? 0 : position_of(p, u.keys - u.count + token_of(p, rj)) - p.window + 1;
           m[n][j] = -INFINITY;
           l[n][j] = 0.f;
         }
@@ -427,13 +450,24 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int j = 0; j < 4; ++j) o[n][d][j] = 0.f;
       }
-      const int seen = part == kPrefix ? u.keys : u.keys - u.count + 1;   // by every row
-      for (int t = lo; t < hi; ++t, ++k) {
+      const int seen_own = part == kPrefix ? u.keys : u.keys - u.count + 1;   // by every row
+      const int low_all = kWindow ? position_of(p, u.keys - 1) - p.window + 1 : 0;   // the first position that every row's window has
+      for (int i = lo; i < hi; ++i, ++k) {
+        // tile t of the unit's keys (of the prefix's or its own), of which there are `end`
+        const bool pre = kWindow && line.in_prefix(i);
+        const int t = kWindow ? line.tile(i) : i, end = pre ? p.b.prefix_len : u.keys, seen = pre ? end : seen_own;
+        const int base = kWindow && !pre ? p.b.prefix_len : 0;      // position of the first
+        // with a window: keys from `sinks` up to `low_all - base` are not every row's
+        const int sinks = p.sinks - base;
+        const bool low_edge = kWindow && t * kTile < low_all - base && (t + 1) * kTile > sinks;
+        auto sees = [&](int n, int j, int key) {
+          return key < (pre ? end : lim[n][j]) && (!kWindow || key >= low[n][j] - base || key < sinks);
+        };
         const int st = k % ST;
         ok = mbar_wait_warp(&full[warp][st], (k / ST) & 1);
         if (!ok) break;
         const uint32_t kb = ring_a + st * 2 * S::kMat, vb = kb + S::kMat;
-        const bool edge = (t + 1) * kTile > seen;
+        const bool edge = (t + 1) * kTile > seen || low_edge;
         // values from key `from` of the tile's on: zero times them has to be zero
         auto drop = [&](int from) {
 #pragma unroll 1
@@ -446,14 +480,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         };
         bool apart = false;   // a token's value that is not finite, and tokens before it
         if (edge) {
-          if ((t + 1) * kTile > u.keys) drop(u.keys);   // past the last key: leftovers (perhaps NaN)
-          if (seen < u.keys) {
+          if ((t + 1) * kTile > end) drop(end);   // past the last key: leftovers (perhaps NaN)
+          if (seen < end || low_edge) {
             bool bad = false;
 #pragma unroll 1
             for (int i = lane; i < kTile * (D / 8); i += 32) {
               const int r = i / (D / 8), c = i % (D / 8);
               const uint4 v = ld_shared16(vb + (c >> 3) * kHalf + r * 128 + ((c & 7) << 4));
-              if (t * kTile + r >= seen) bad |= some_not_finite(v);
+              if (t * kTile + r >= seen || (low_edge && t * kTile + r < low_all - base && t * kTile + r >= sinks)) bad |= some_not_finite(v);
             }
             apart = __any_sync(0xffffffffu, bad);
           }
@@ -480,7 +514,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             x[j] = (s[n][0][j] + s[n][1][j]) * p.scale;
-            if (edge && key + 8 * (j >> 1) >= lim[n][j & 1]) x[j] = -INFINITY;
+            if (edge && !sees(n, j & 1, key + 8 * (j >> 1))) x[j] = -INFINITY;
           }
           float mx[2];
 #pragma unroll
@@ -513,7 +547,43 @@ __global__ void __launch_bounds__(kThreads, 1)
           pf[n][1] = movmatrix(pack_bf16x2(e[2], e[3]));
         }
         const uint32_t vr = ((lane >> 4) << 3) + (lane & 7), vc = (lane >> 3) & 1;
-        if (!apart) {
+        if (kWindow && apart) {
+          // what the tokens see is not a part of what the next one sees: values
+          // that are not finite and not every row's go to the rows that see them
+          // by an addition, and out of the tile
+          auto shared = [&](int kk) { return kk < seen && (kk >= low_all - base || kk < sinks); };
+#pragma unroll 1
+          for (int r = 0; r < kTile; ++r) {
+            const int kk = t * kTile + r;
+            if (kk >= end || shared(kk)) continue;
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                const int c = 2 * d + h;   // 8 elements, of which this lane has number g8
+                const uint8_t* at = ring + (vb - ring_a) + (c >> 3) * kHalf + r * 128 + (((c & 7) ^ (r & 7)) << 4) + 2 * g8;
+                const uint32_t bits = *reinterpret_cast<const volatile uint16_t*>(at);
+                if (!not_finite(bits)) continue;
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                  for (int j = 0; j < 2; ++j)
+                    if (sees(n, j, kk)) o[n][d][2 * h + j] += __uint_as_float(bits << 16);
+              }
+          }
+          __syncwarp();
+#pragma unroll 1
+          for (int i16 = lane; i16 < kTile * (D / 8); i16 += 32) {
+            const int r = i16 / (D / 8), c = i16 % (D / 8), kk = t * kTile + r;
+            const uint32_t at = vb + (c >> 3) * kHalf + r * 128 + ((c & 7) << 4);
+            const uint4 v = ld_shared16(at);
+            if (kk < end && !shared(kk) && some_not_finite(v))
+              st_shared16(at, v.x & ~not_finite(v.x), v.y & ~not_finite(v.y), v.z & ~not_finite(v.z), v.w & ~not_finite(v.w));
+          }
+          fence_proxy_async_smem();   // (before the next copy into this stage)
+          __syncwarp();
+        }
+        if (kWindow || !apart) {
 #pragma unroll
           for (int d = 0; d < D / 16; ++d) {
             uint32_t a[4];
@@ -679,7 +749,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (part == kOwn)
       for (int s = blockIdx.x; s < p.b.n_seqs; s += gridDim.x) {
         const SeqSpan q = seq_span(p.b, s);
-        if (q.own > 0) continue;
+        if (q.own > 0 || (kWindow && p.b.prefix_len > 0)) continue;
         const int64_t r1 = (int64_t)(q.first + q.count) * p.q_heads;
         for (int64_t row = (int64_t)q.first * p.q_heads + warp; row < r1; row += kWarps) {
           const float none[D / 32] = {};
@@ -692,19 +762,24 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (late) pdl_wait();
 }
 
-template <int D, int NT>
-cudaError_t launch(const sdq_cache_s* c, const AttendParams& p, int part, bool late, cudaStream_t st) {
+template <int D, int NT, bool kWindow>
+cudaError_t launch_kernel(const sdq_cache_s* c, const AttendParams& p, int part, bool late, cudaStream_t st) {
   using S = NarrowShape<D, NT>;
   static std::atomic<int> smem_set[64];
-  const cudaError_t e = smem_limit_once(narrow_kernel<D, NT>, S::kSmem, c->device, smem_set);
+  const cudaError_t e = smem_limit_once(narrow_kernel<D, NT, kWindow>, S::kSmem, c->device, smem_set);
   if (e != cudaSuccess) return e;
-  return launch_pdl(narrow_kernel<D, NT>, dim3((unsigned)p.ctas), dim3(kThreads), (size_t)S::kSmem, st, c->ktile, c->vtile, p, part,
+  return launch_pdl(narrow_kernel<D, NT, kWindow>, dim3((unsigned)p.ctas), dim3(kThreads), (size_t)S::kSmem, st, c->ktile, c->vtile, p, part,
                     late ? 1 : 0);
+}
+
+template <int D, int NT>
+cudaError_t launch(const sdq_cache_s* c, const AttendParams& p, int part, bool late, cudaStream_t st) {
+  return p.window > 0 ? launch_kernel<D, NT, true>(c, p, part, late, st) : launch_kernel<D, NT, false>(c, p, part, late, st);
 }
 
 template <int D>
 cudaError_t launch_nt(const sdq_cache_s* c, const AttendParams& p, int part, bool late, cudaStream_t st) {
-  switch (narrow_groups(&p.b, p.group, part)) {
+  switch (narrow_groups(p, part)) {
     case 0:   // (no keys: zeros)
     case 1: return launch<D, 1>(c, p, part, late, st);
     case 2: return launch<D, 2>(c, p, part, late, st);
@@ -715,9 +790,9 @@ cudaError_t launch_nt(const sdq_cache_s* c, const AttendParams& p, int part, boo
 
 }  // namespace
 
-int narrow_groups(const sdq_batch* b, int group, int part) {
-  if ((part == kPrefix ? b->prefix_len : b->max_own) == 0) return 0;
-  return (int)(((int64_t)(part == kPrefix ? b->n_tokens : b->max_new) * group + 7) / 8);
+int narrow_groups(const AttendParams& p, int part) {
+  if (part == kPrefix ? p.b.prefix_len == 0 : p.b.max_own == 0 && (p.window == 0 || p.b.prefix_len == 0)) return 0;
+  return (int)(((int64_t)(part == kPrefix ? p.b.n_tokens : p.b.max_new) * p.group + 7) / 8);
 }
 
 int narrow_warps() { return kWarps; }

@@ -111,9 +111,11 @@ struct WideItem {
   int s;                     // sequence, -1: the whole batch
   int own, count;            // its own tokens and new tokens
   int prefix_tiles, t0, t1;  // of the line: the prefix's tiles, this block's [t0, t1)
+  Line lines[2];             // with a window: which of the prefix's and of the own tiles
 };
 
 // (a whole warp; false: nothing to do)
+template <bool kWindow>
 __device__ __forceinline__ bool wide_item(const AttendParams& p, int part, WideItem* w) {
   const int splits = p.splits[part];
   const int id = blockIdx.x / (p.kv_heads * splits), rest = blockIdx.x % (p.kv_heads * splits);
@@ -162,7 +164,16 @@ __device__ __forceinline__ bool wide_item(const AttendParams& p, int part, WideI
     w->r0 = rb * 256;
     w->prefix_tiles = p.chained ? ptiles : 0;
     const int last = min(w->rows, w->r0 + 256) - 1;   // its last row sees the most
-    tiles = w->prefix_tiles + (max(0, q.own - q.count + last / p.group + 1) + kKeys - 1) / kKeys;
+    const int keys = max(0, q.own - q.count + last / p.group + 1);
+    if (kWindow) {
+      const int first = position_of(p, q.own - q.count + w->r0 / p.group);
+      w->lines[0] = line_of<kKeys>(p, p.b.prefix_len, 0, first);
+      w->lines[1] = line_of<kKeys>(p, keys, p.b.prefix_len, first);
+      w->prefix_tiles = w->lines[0].tiles;
+      tiles = w->prefix_tiles + w->lines[1].tiles;
+    } else {
+      tiles = w->prefix_tiles + (keys + kKeys - 1) / kKeys;
+    }
   }
   const int per = (tiles + splits - 1) / splits;
   w->t0 = min(tiles, w->split * per);
@@ -170,7 +181,7 @@ __device__ __forceinline__ bool wide_item(const AttendParams& p, int part, WideI
   return true;
 }
 
-template <int D>
+template <int D, bool kWindow>
 __global__ void __launch_bounds__(kWideThreads, 1)
     wide_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const AttendParams p,
                 const int part) {
@@ -209,7 +220,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
   pdl_launch_dependents();
   call_record_start(p.rec, p.call, blockIdx.x == 0 && tid == 0);
   WideItem w;
-  if (!wide_item(p, part, &w)) {   // (all warps alike)
+  if (!wide_item<kWindow>(p, part, &w)) {   // (all warps alike)
     if (warp == 8) tmem_dealloc(tmem_base, 512);
     return;
   }
@@ -218,6 +229,11 @@ __global__ void __launch_bounds__(kWideThreads, 1)
   const bool joins = p.splits[part] > 1 || p.parts > 1;
   const uint32_t tmem = tmem_base;
   bool ok = true;
+  // which tile of the prefix's or of the own ones stands at place t of the line
+  auto tile_at = [&](int t) {
+    if (kWindow) return t < w.prefix_tiles ? w.lines[0].tile(t) : w.lines[1].tile(t - w.prefix_tiles);
+    return t < w.prefix_tiles ? t : t - w.prefix_tiles;
+  };
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;\n");
     if (warp == 9) {
@@ -226,11 +242,11 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       const int32_t* own_table = p.b.pages + (int64_t)(w.s < 0 ? 0 : w.s) * p.b.page_stride;
       // the page of the lane's box of line tile t (-1: past the last token), and the tile's boxes
       auto boxes_of = [&](int t) {
-        const int keys = t < w.prefix_tiles ? p.b.prefix_len : w.own, at = (t < w.prefix_tiles ? t : t - w.prefix_tiles) * per_tile;
+        const int keys = t < w.prefix_tiles ? p.b.prefix_len : w.own, at = tile_at(t) * per_tile;
         return max(0, min(per_tile, ((keys + box - 1) >> p.box_shift) - at));
       };
       auto row_of = [&](int t) {
-        const int at = (t < w.prefix_tiles ? t : t - w.prefix_tiles) * per_tile + lane;
+        const int at = tile_at(t) * per_tile + lane;
         const int pg = t < w.t1 && lane < boxes_of(t) ? __ldg((t < w.prefix_tiles ? p.b.prefix_pages : own_table) + at / per_page) : -1;
         // (a page outside the cache: rows outside the arrays, which read as zeros)
         return pg >= 0 && pg < p.n_pages ? ((pg * p.kv_heads + w.h) << p.page_shift) + ((at & (per_page - 1)) << p.box_shift) : -box;
@@ -341,6 +357,17 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       // finite are taken out of the tile, as zero times them is not zero, and added
       // at the end to the rows that see them
       const int all_rows = max(0, w.own - w.count + w.r0 / p.group + 1);
+      // with a window: the first position of this row's, and of the window of the
+      // last row of its half and of the block (the latest ones)
+      const int last = min(w.rows, w.r0 + 256) - 1;
+      auto low_of = [&](int r) { return position_of(p, w.own - w.count + r / p.group) - p.window + 1; };
+      const int low = kWindow && live ? position_of(p, w.own - w.count + tok) - p.window + 1 : 0;
+      const int low_half = kWindow ? low_of(min(last, w.r0 + 128 * half + 127)) : 0, low_rows = kWindow ? low_of(last) : 0;
+      // do 64 keys from k0 of the prefix's or own ones hold some that not all rows of the block see?
+      auto partial = [&](bool pre, int k0) {
+        const int keys = pre ? p.b.prefix_len : w.own, base = pre ? 0 : p.b.prefix_len;
+        return k0 + kSub > (pre ? keys : min(keys, all_rows)) || (kWindow && k0 < low_rows - base && k0 + kSub > p.sinks - base);
+      };
       const uint32_t ts = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + 128 * half;
       const uint32_t to = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + 256 + D * half;
       float m = -INFINITY;        // reference maximum (log2 units)
@@ -359,17 +386,26 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         tmem_ld_wait();
         const int t = w.t0 + i;
         const bool pre = t < w.prefix_tiles;
-        const int k0 = (pre ? t : t - w.prefix_tiles) * kKeys + kSub * j, keys = pre ? p.b.prefix_len : w.own;
+        const int k0 = tile_at(t) * kKeys + kSub * j, keys = pre ? p.b.prefix_len : w.own;
         if (k0 + kSub > (pre ? keys : all)) {
           const int see = (pre ? keys : lim) - k0;   // of these 64
 #pragma unroll
           for (int c = 0; c < kSub; ++c)
             if (c >= see) x[c] = 0xFF800000u;
         }
-        if (half == 0 && k0 + kSub > (pre ? keys : min(keys, all_rows))) {
+        if (kWindow) {
+          const int base = pre ? 0 : p.b.prefix_len;
+          if (k0 < low_half - base && k0 + kSub > p.sinks - base) {
+            const int from = p.sinks - base - k0, to = low - base - k0;   // of these 64
+#pragma unroll
+            for (int c = 0; c < kSub; ++c)
+              if (c >= from && c < to) x[c] = 0xFF800000u;
+          }
+        }
+        if (half == 0 && partial(pre, k0)) {
           // (for both halves: the second's product is issued after the first's)
           // values past the last key are leftovers (perhaps NaN): zero times them has to be zero too
-          const int vs = (2 * i + 1) % S::kRing, from = 8 * max(0, (pre ? keys : min(keys, all_rows)) - k0);
+          const int vs = (2 * i + 1) % S::kRing, from = kWindow ? 0 : 8 * max(0, (pre ? keys : min(keys, all_rows)) - k0);
           if (!mbar_wait_warp(&full[vs], ((2 * i + 1) / S::kRing) & 1)) {
             ok = false;
             break;
@@ -460,10 +496,10 @@ __global__ void __launch_bounds__(kWideThreads, 1)
           uint32_t o[32];
           tmem_ld32(to + 32 * c, o);
           tmem_ld_wait();
-#pragma unroll 1
-          for (int key = all_rows; live && key < lim; ++key) {
-            const int pg = __ldg(p.b.pages + (int64_t)w.s * p.b.page_stride + (key >> p.page_shift));
-            if (pg < 0 || pg >= p.n_pages) continue;
+          // element 2 j and 2 j + 1 of these 32 of a key's value
+          auto add_value = [&](const int32_t* table, int key) {
+            const int pg = __ldg(table + (key >> p.page_shift));
+            if (pg < 0 || pg >= p.n_pages) return;
             const uint32_t* v = reinterpret_cast<const uint32_t*>(
                 p.v + ((((int64_t)pg * p.kv_heads + w.h) << p.page_shift) + (key & ((1 << p.page_shift) - 1))) * D + 32 * c);
 #pragma unroll
@@ -472,6 +508,22 @@ __global__ void __launch_bounds__(kWideThreads, 1)
               if (bad & 0xFFFFu) o[2 * j] = __float_as_uint(__uint_as_float(o[2 * j]) + __uint_as_float(x << 16));
               if (bad >> 16) o[2 * j + 1] = __float_as_uint(__uint_as_float(o[2 * j + 1]) + __uint_as_float(x & 0xFFFF0000u));
             }
+          };
+          const int32_t* own_table = p.b.pages + (int64_t)w.s * p.b.page_stride;
+          if (kWindow) {
+#pragma unroll 1
+            for (int q = 0; live && q < 2 * n; ++q) {
+              const bool pre = w.t0 + (q >> 1) < w.prefix_tiles;
+              const int k0 = tile_at(w.t0 + (q >> 1)) * kKeys + kSub * (q & 1), base = pre ? 0 : p.b.prefix_len;
+              if (!partial(pre, k0)) continue;
+              const int end = min(k0 + kSub, pre ? p.b.prefix_len : lim);
+#pragma unroll 1
+              for (int key = k0; key < end; ++key)
+                if (key >= low - base || key < p.sinks - base) add_value(pre ? p.b.prefix_pages : own_table, key);
+            }
+          } else {
+#pragma unroll 1
+            for (int key = all_rows; live && key < lim; ++key) add_value(own_table, key);
           }
           __syncwarp();
           tmem_st32(to + 32 * c, o);
@@ -573,12 +625,12 @@ int64_t wide_blocks(const sdq_batch* b, int group, int part) {
   return part == kPrefix ? (rows + 255) / 256 : rows / 256 + std::min(b->n_seqs, b->n_tokens);
 }
 
-template <int D>
+template <int D, bool kWindow>
 cudaError_t launch(const sdq_cache_s* c, const AttendParams& p, int part, cudaStream_t st) {
   static std::atomic<int> smem_set[64];
-  const cudaError_t e = smem_limit_once(wide_kernel<D>, WideShape<D>::kSmem, c->device, smem_set);
+  const cudaError_t e = smem_limit_once(wide_kernel<D, kWindow>, WideShape<D>::kSmem, c->device, smem_set);
   if (e != cudaSuccess) return e;
-  return launch_pdl(wide_kernel<D>, dim3((unsigned)wide_grid(c, p, part)), dim3(kWideThreads), (size_t)WideShape<D>::kSmem, st, c->kmap,
+  return launch_pdl(wide_kernel<D, kWindow>, dim3((unsigned)wide_grid(c, p, part)), dim3(kWideThreads), (size_t)WideShape<D>::kSmem, st, c->kmap,
                     c->vmap, p, part);
 }
 
@@ -590,10 +642,13 @@ int64_t wide_grid(const sdq_cache_s* c, const AttendParams& p, int part) {
 
 // us, over waves of thread blocks: a tile (256 rows) takes 1.3 us, a thread
 // block's two ends 5 us.
-double wide_time(const sdq_cache_s* c, const sdq_batch* b, int q_heads, int part, bool chained, int s) {
+double wide_time(const sdq_cache_s* c, const AttendParams& p, int q_heads, int part, int s) {
+  const sdq_batch* b = &p.b;
   const int64_t blocks = wide_blocks(b, q_heads / c->desc.kv_heads, part) * c->desc.kv_heads * s;
-  const int64_t tiles = (part == kPrefix || chained ? ((int64_t)b->prefix_len + kKeys - 1) / kKeys : 0) +
-                        (part == kOwn ? ((int64_t)b->max_own + kKeys - 1) / kKeys : 0);
+  int64_t tiles = (part == kPrefix || p.chained || p.window > 0 ? ((int64_t)b->prefix_len + kKeys - 1) / kKeys : 0) +
+                  (part == kOwn ? ((int64_t)b->max_own + kKeys - 1) / kKeys : 0);
+  // (a window, moved on by the tokens of a row block, and the first keys, each with a tile's rest at its ends)
+  if (p.window > 0) tiles = std::min<int64_t>(tiles, (p.window + 256 / p.group) / kKeys + 2 + (p.sinks + kKeys - 1) / kKeys);
   return (double)((blocks + c->sm_count - 1) / c->sm_count) * (5.0 + 1.3 * (double)((tiles + s - 1) / s));
 }
 
@@ -607,10 +662,11 @@ double wide_time(const sdq_cache_s* c, const sdq_batch* b, int q_heads, int part
 // over their logarithm 45, 35, 33, 31, 41; all at the bound 50, 52, 52, 53, 57;
 // all of 1 but one 44, 34, 32, 31, 31.  16 of 32 heads behind 2051, up to 300,
 // 3 parts, us for 2, 3, 4: 21, 19, 24; at the bound 34, 33, 37; 21, 19, 23.
-int wide_splits(const sdq_cache_s* c, const sdq_batch* b, int q_heads, int part, bool chained, bool narrow) {
+int wide_splits(const sdq_cache_s* c, const AttendParams& p, int q_heads, int part, bool narrow) {
+  const sdq_batch* b = &p.b;
   const double own = narrow ? (double)b->n_seqs * c->desc.kv_heads * b->max_own / 6 * c->desc.head_dim * 4 : 0.0;   // bytes
   auto time = [&](int s) {
-    const double t = wide_time(c, b, q_heads, part, chained, s);
+    const double t = wide_time(c, p, q_heads, part, s);
     const int64_t grid = wide_blocks(b, q_heads / c->desc.kv_heads, part) * c->desc.kv_heads * s;
     const double free = 40e3 * (double)std::max<int64_t>(0, c->sm_count - grid);   // bytes a us
     const double both = own <= free * t ? std::max(t, kNarrowStart + own / std::max(1.0, free))
@@ -624,7 +680,8 @@ int wide_splits(const sdq_cache_s* c, const sdq_batch* b, int q_heads, int part,
 }
 
 cudaError_t launch_wide(const sdq_cache_s* c, const AttendParams& p, int part, cudaStream_t st) {
-  return c->desc.head_dim == 128 ? launch<128>(c, p, part, st) : launch<64>(c, p, part, st);
+  if (p.window > 0) return c->desc.head_dim == 128 ? launch<128, true>(c, p, part, st) : launch<64, true>(c, p, part, st);
+  return c->desc.head_dim == 128 ? launch<128, false>(c, p, part, st) : launch<64, false>(c, p, part, st);
 }
 
 }  // namespace sdq
