@@ -1,6 +1,7 @@
 // Logits before the choice of a token: penalties for repeated tokens, biases, a
 // grammar's allowed tokens (include/sdq.h).
 #include <cmath>
+#include <type_traits>
 
 #include "common.cuh"
 
@@ -43,8 +44,9 @@ struct Row {
 // boundary).  Each logit is read and written once: HBM bounds it.  What the
 // history says of the block's tokens is counted in shared memory first (a word
 // per token; whole numbers, so that no order of atomics shows), beside the
-// first loads of the logits, which are under way meanwhile.  The few tokens
-// with a bias are worked out one by a warp, the list's entries for one token
+// first loads of the logits, which are under way meanwhile; every block of a
+// row looks through all of its history, 4 tokens a load.  The few tokens
+// with a bias are worked out one by a thread, the list's entries for one token
 // added up in their order, and written behind the others.
 template <class T, int kV, bool kInPlace>
 __global__ void __launch_bounds__(kThreads) adjust_kernel(const AdjustParams p) {
@@ -54,14 +56,14 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(const AdjustParams p) 
   int* tok = reinterpret_cast<int*>(smem + kChunk);         // of the biases in this block's range: the token,
   float* add = reinterpret_cast<float*>(tok + p.a.n_bias);  // the bias
   float* res = add + p.a.n_bias;                            // and the logit that comes of it
-  __shared__ int n_here;
+  __shared__ int counts[kWarps];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int row = blockIdx.y;
+  const int row = blockIdx.x;   // (a row's common tokens, mostly its low ones, are counted first: the last blocks have least to do)
   const T* in = static_cast<const T*>(p.in) + row * p.ld;
   T* out = static_cast<T*>(p.out) + row * p.ldo;
   const int lead = (int)((reinterpret_cast<uintptr_t>(in) & 15u) / sizeof(T));
   const bool even = ((reinterpret_cast<uintptr_t>(in) ^ reinterpret_cast<uintptr_t>(out)) & 15u) == 0;
-  const int t0 = blockIdx.x * kChunk - lead, t1 = min(p.vocab, t0 + kChunk);   // tokens (those below 0: none)
+  const int t0 = (int)blockIdx.y * kChunk - lead, t1 = min(p.vocab, t0 + kChunk);   // tokens (those below 0: none)
   pdl_wait();
   pdl_launch_dependents();
   auto whole = [&](int t) { return even && t >= 0 && t + kVec <= p.vocab; };
@@ -79,49 +81,71 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(const AdjustParams p) 
   r.presence = p.a.presence ? __ldg(p.a.presence + row) : 0.f;
   const int set = p.a.allowed ? (p.a.allowed_row ? __ldg(p.a.allowed_row + row) : row) : -1;
   r.allowed = set >= 0 && set < p.a.n_allowed ? p.a.allowed + set * p.a.allowed_stride : nullptr;
-  for (int i = tid; i < kChunk / 4; i += kThreads) reinterpret_cast<uint4*>(seen)[i] = make_uint4(0, 0, 0, 0);
-  __syncthreads();
-  if (warp == 0) {
-    // biases of tokens in this block's range, in the list's order
-    int n = 0;
-    for (int i0 = 0; i0 < p.a.n_bias; i0 += 32) {
-      const int i = i0 + lane, t = i < p.a.n_bias ? __ldg(p.a.bias_ids + row * p.a.bias_ids_stride + i) : -1;
-      const bool here = t >= 0 && t >= t0 && t < t1;
-      const uint32_t which = __ballot_sync(0xffffffffu, here);
-      if (here) {
-        const int at = n + __popc(which & ((1u << lane) - 1));
-        tok[at] = t;
-        add[at] = __ldg(p.a.bias + row * p.a.bias_stride + i);
-      }
-      n += __popc(which);
-    }
-    if (lane == 0) n_here = n;
-  }
   if (p.a.history) {
+    for (int i = tid; i < kChunk / 4; i += kThreads) reinterpret_cast<uint4*>(seen)[i] = make_uint4(0, 0, 0, 0);
+    __syncthreads();
     const int len = p.a.history_len ? min(max(__ldg(p.a.history_len + row), 0), p.a.history_max) : p.a.history_max;
     const int prompt = p.a.prompt_len ? __ldg(p.a.prompt_len + row) : 0;
     const int32_t* h = p.a.history + row * p.a.history_stride;
-#pragma unroll 4
-    for (int i = tid; i < len; i += kThreads) {
-      const int t = __ldg(h + i);
-      if (t < 0 || t < t0 || t >= t1) continue;
+    const uint32_t width = (uint32_t)(t1 - max(t0, 0)), low = (uint32_t)max(t0, 0);
+    auto count = [&](int i, int t) {
+      if ((uint32_t)t - low >= width) return;   // (also below 0)
       if (i < prompt) atomicOr(seen + (t - t0), ~kCount);
       else atomicAdd(seen + (t - t0), 1u);
+    };
+    // places 0 .. head - 1 lie before a 16-byte boundary, the last ones behind whole pieces
+    const int head = min(len, (int)(-(reinterpret_cast<uintptr_t>(h) >> 2) & 3u)), pieces = (len - head) / 4;
+    if (t0 < t1) {
+      const int4* h4 = reinterpret_cast<const int4*>(h + head);
+      constexpr int kAhead = 4;
+      for (int i0 = tid; i0 < pieces; i0 += kAhead * kThreads) {
+        int4 q[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) q[k] = i0 + k * kThreads < pieces ? __ldg(h4 + i0 + k * kThreads) : make_int4(-1, -1, -1, -1);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          const int i = head + 4 * (i0 + k * kThreads);
+          count(i, q[k].x);
+          count(i + 1, q[k].y);
+          count(i + 2, q[k].z);
+          count(i + 3, q[k].w);
+        }
+      }
+      if (tid < head) count(tid, __ldg(h + tid));
+      const int i = head + 4 * pieces + tid - 4;
+      if (tid >= 4 && i < len) count(i, __ldg(h + i));
+    }
+  }
+  // biases of tokens in this block's range, in the list's order
+  int n = 0;
+  for (int i0 = 0; i0 < p.a.n_bias; i0 += kThreads) {
+    const int i = i0 + tid, t = i < p.a.n_bias ? __ldg(p.a.bias_ids + row * p.a.bias_ids_stride + i) : -1;
+    const bool here = t >= 0 && t >= t0 && t < t1;
+    const uint32_t which = __ballot_sync(0xffffffffu, here);
+    __syncthreads();   // (counts of the pieces before are read)
+    if (lane == 0) counts[warp] = __popc(which);
+    __syncthreads();
+    int at = n;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      if (w < warp) at += counts[w];
+      n += counts[w];
+    }
+    if (here) {
+      at += __popc(which & ((1u << lane) - 1));
+      tok[at] = t;
+      add[at] = __ldg(p.a.bias + row * p.a.bias_stride + i);
     }
   }
   __syncthreads();
-  const int n = n_here;
-  for (int e = warp; e < n; e += kWarps) {
+  for (int e = tid; e < n; e += kThreads) {
     const int t = tok[e];
+    const float z = to_float(in[t]);
     float sum = 0.f;
-    for (int i0 = 0; i0 < n; i0 += 32) {
-      uint32_t same = __ballot_sync(0xffffffffu, i0 + lane < n && tok[min(i0 + lane, n - 1)] == t);
-      for (; same; same &= same - 1) sum += add[i0 + __ffs(same) - 1];
-    }
-    if (lane == 0) {   // (entries of one token: the same value)
-      const float z = r.penalized(to_float(in[t]), seen[t - t0]) + sum;
-      res[e] = r.may(t) ? z : -INFINITY;
-    }
+#pragma unroll 8
+    for (int k = 0; k < n; ++k)
+      if (tok[k] == t) sum += add[k];
+    res[e] = r.may(t) ? r.penalized(z, p.a.history ? seen[t - t0] : 0) + sum : -INFINITY;   // (entries of one token: the same)
   }
   if (n > 0) __syncthreads();
 #pragma unroll
@@ -131,7 +155,7 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(const AdjustParams p) 
     uint32_t w[kVec], any = 0;
 #pragma unroll
     for (int j = 0; j < kVec; j += 4) {
-      const uint4 q = *reinterpret_cast<const uint4*>(seen + at + j);
+      const uint4 q = p.a.history ? *reinterpret_cast<const uint4*>(seen + at + j) : make_uint4(0, 0, 0, 0);
       w[j] = q.x;
       w[j + 1] = q.y;
       w[j + 2] = q.z;
@@ -180,7 +204,7 @@ cudaError_t launch(const AdjustParams& p, int rows, int device, cudaStream_t st)
   static std::atomic<int> smem_set[64];
   const cudaError_t e = smem_limit_once(adjust_kernel<T, kV, kInPlace>, 4 * kChunk + 12 * kMaxBiases, device, smem_set);
   if (e != cudaSuccess) return e;
-  const dim3 grid((unsigned)((p.vocab + kVec - 1 + kChunk - 1) / kChunk), (unsigned)rows);
+  const dim3 grid((unsigned)rows, (unsigned)((p.vocab + kVec - 1 + kChunk - 1) / kChunk));
   return launch_pdl(adjust_kernel<T, kV, kInPlace>, grid, dim3(kThreads), 4 * (size_t)kChunk + 12 * (size_t)p.a.n_bias, st, p);
 }
 
@@ -204,10 +228,11 @@ extern "C" int sdq_adjust_logits(const void* logits, int32_t type, int32_t rows,
   if ((a->history && a->history_max < 0) || a->n_bias < 0 || a->n_bias > kMaxBiases) return SDQ_ERR_INVALID_ARG;
   if (a->n_bias > 0 && (!a->bias_ids || !a->bias)) return SDQ_ERR_INVALID_ARG;
   if (a->allowed && a->n_allowed < (a->allowed_row ? 1 : rows)) return SDQ_ERR_INVALID_ARG;
-  int dev = -1, major = 0, minor = 0;
+  int dev = -1, major = 0, minor = 0, sms = 0;
   if (cudaGetDevice(&dev) != cudaSuccess ||
       cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev) != cudaSuccess)
+      cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
     return SDQ_ERR_CUDA;
   if (major != 10 || minor != 3) return SDQ_ERR_UNSUPPORTED;
   AdjustParams p;
@@ -216,8 +241,16 @@ extern "C" int sdq_adjust_logits(const void* logits, int32_t type, int32_t rows,
   p.ld = ld; p.ldo = ldo;
   p.vocab = vocab;
   cudaStream_t st = (cudaStream_t)stream;
-  const cudaError_t e = type == SDQ_F32 ? in_place ? launch<float, 4, true>(p, rows, dev, st) : launch<float, 4, false>(p, rows, dev, st)
-                        : in_place      ? launch<uint16_t, 2, true>(p, rows, dev, st)
-                                        : launch<uint16_t, 2, false>(p, rows, dev, st);
+  // 16384 logits a thread block where the rows fill the device with that, else 4096
+  const bool large = (int64_t)rows * ((vocab + 16383) / 16384) >= 2 * sms;
+  auto run = [&](auto zero, auto place) {
+    using T = decltype(zero);
+    constexpr int kVec = 16 / sizeof(T);
+    constexpr bool kInPlace = decltype(place)::value;
+    return large ? launch<T, 16384 / kVec / kThreads, kInPlace>(p, rows, dev, st) : launch<T, 4096 / kVec / kThreads, kInPlace>(p, rows, dev, st);
+  };
+  const std::true_type yes;
+  const std::false_type no;
+  const cudaError_t e = type == SDQ_F32 ? in_place ? run(0.f, yes) : run(0.f, no) : in_place ? run((uint16_t)0, yes) : run((uint16_t)0, no);
   return e == cudaSuccess ? SDQ_OK : SDQ_ERR_CUDA;
 }

@@ -426,7 +426,6 @@ __global__ void __launch_bounds__(kThreads, 1)
       // query rows as the products' B operand; rows past the last are zero
       uint32_t qf[NT][D / 16][2];
       int lim[NT][2];   // keys that this lane's two queries of each 8 see
-      int low[NT][2];   // with a window: the first position of theirs
       if (kWindow) line = unit_line(p, u.count, u.keys);
       float o[NT][D / 16][4], m[NT][2], l[NT][2];
 #pragma unroll
@@ -441,7 +440,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int j = 0; j < 2; ++j) {
           const int rj = 8 * n + c2 + j;
           lim[n][j] = part == kPrefix || rj >= u.rows ? u.keys : u.keys - u.count + token_of(p, rj) + 1;
-          if (kWindow) low[n][j] = rj >= u.rows ? 0 : position_of(p, u.keys - u.count + token_of(p, rj)) - p.window + 1;
           m[n][j] = -INFINITY;
           l[n][j] = 0.f;
         }
@@ -461,7 +459,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int sinks = p.sinks - base;
         const bool low_edge = kWindow && t * kTile < low_all - base && (t + 1) * kTile > sinks;
         auto sees = [&](int n, int j, int key) {
-          return key < (pre ? end : lim[n][j]) && (!kWindow || key >= low[n][j] - base || key < sinks);
+          return key < (pre ? end : lim[n][j]) && (!kWindow || key >= position_of(p, lim[n][j] - 1) - p.window + 1 - base || key < sinks);
         };
         const int st = k % ST;
         ok = mbar_wait_warp(&full[warp][st], (k / ST) & 1);
