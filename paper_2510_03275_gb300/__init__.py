@@ -14,6 +14,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass
 from fractions import Fraction
 from typing import NamedTuple
@@ -100,18 +101,9 @@ class _HeadNorm(ctypes.Structure):
                 ("eps", ctypes.c_float)]
 
 
-class _Adjust(ctypes.Structure):
-    _fields_ = ([(n, ctypes.c_void_p) for n in ("history", "history_len", "prompt_len", "repetition", "frequency", "presence",
-                                                "bias_ids", "bias", "allowed", "allowed_row")]
-                + [(n, ctypes.c_int64) for n in ("history_stride", "bias_ids_stride", "bias_stride", "allowed_stride")]
-                + [(n, ctypes.c_int32) for n in ("history_max", "n_bias", "n_allowed")])
-
-
-class _Pages(ctypes.Structure):
-    _fields_ = ([(n, ctypes.c_int32) for n in ("page_tokens", "n_pages", "n_seqs", "n_tokens", "page_columns", "page_stride",
-                                               "prefix_len")]
-                + [(n, ctypes.c_void_p) for n in ("own_len", "new_len", "done", "pages", "free_pages", "n_free", "token_start",
-                                                  "own_out", "n_free_out", "slots", "positions")])
+# (packed by `struct`: a third of the time of a ctypes structure)
+_ADJUST = struct.Struct("10P4q3i4x")   # sdq_adjust
+_PAGES = struct.Struct("7i11P")        # sdq_pages
 
 
 @dataclass(frozen=True)
@@ -494,17 +486,17 @@ def sdq_sample(logits, u, temperature, top_k, top_p, min_p, tokens, stream=None)
                             _stream(stream)), "sdq_sample")
 
 
-def sdq_pages_step(step, stream=None):
-    """step: a ctypes struct ``sdq_pages``."""
-    _check(lib().sdq_pages_step(ctypes.addressof(step), _stream(stream)), "sdq_pages_step")
+def sdq_pages_step(step: bytes, stream=None):
+    """step: the bytes of an ``sdq_pages``."""
+    _check(lib().sdq_pages_step(step, _stream(stream)), "sdq_pages_step")
 
 
-def sdq_adjust_logits(logits, adjust, out, stream=None):
-    """logits, out: rows x vocab of one type, adjacent in a row; adjust: a ctypes struct ``sdq_adjust``."""
+def sdq_adjust_logits(logits, adjust: bytes, out, stream=None):
+    """logits, out: rows x vocab of one type, adjacent in a row; adjust: the bytes of an ``sdq_adjust``."""
     rows, vocab = logits.shape
-    _check(lib().sdq_adjust_logits(logits.data_ptr(), _dtype(logits), rows, vocab, logits.stride(0) if rows > 1 else vocab,
-                                   ctypes.addressof(adjust), out.data_ptr(), out.stride(0) if rows > 1 else vocab,
-                                   _stream(stream)), "sdq_adjust_logits")
+    _check(lib().sdq_adjust_logits(logits.data_ptr(), _dtype(logits), rows, vocab, logits.stride()[0] if rows > 1 else vocab,
+                                   adjust, out.data_ptr(), out.stride()[0] if rows > 1 else vocab, _stream(stream)),
+           "sdq_adjust_logits")
 
 
 def sdq_status_string(status: int) -> str:
@@ -651,24 +643,30 @@ class PagePool:
         and come back as new tensors."""
         import torch
         i32, n_seqs = torch.int32, own_len.shape[0]
-        for t in (own_len, new_len, done):
-            if t is not None and (t.dtype is not i32 or tuple(t.shape) != (n_seqs,) or not t.is_contiguous() or not t.is_cuda):
+        one, at_own, at_new, at_done = (n_seqs,), own_len.data_ptr(), new_len.data_ptr(), 0
+        for t in (own_len, new_len) if done is None else (own_len, new_len, done):
+            if t.dtype is not i32 or t.shape != one or not t.is_contiguous() or not t.is_cuda:
                 raise ValueError("PagePool.step: own_len, new_len and done must be contiguous int32 CUDA tensors, one element "
                                  "per sequence")
-        if pages.dtype is not i32 or pages.dim() != 2 or pages.shape[0] != n_seqs or not pages.is_cuda or (
-                pages.shape[1] > 1 and pages.stride(1) != 1):
+        (rows, columns), (stride, adjacent) = (pages.shape, pages.stride()) if pages.dim() == 2 else ((-1, 0), (0, 0))
+        if rows != n_seqs or pages.dtype is not i32 or not pages.is_cuda or (columns > 1 and adjacent != 1):
             raise ValueError("PagePool.step: pages must be an int32 CUDA tensor (sequences, columns), adjacent in a row")
-        if in_place and n_seqs > 0 and own_len.data_ptr() in (new_len.data_ptr(), None if done is None else done.data_ptr()):
+        if done is not None:
+            at_done = done.data_ptr()
+        if in_place and n_seqs > 0 and at_own in (at_new, at_done):
             raise ValueError("PagePool.step: own_len moves on in place and cannot be new_len or done too")
+        # one piece of memory: token_start, own_len, the count, slots, positions
+        sizes = (n_seqs + 1, n_seqs, 1, n_tokens, n_tokens)
         new = _empty((2 * n_seqs + 2 * n_tokens + 2,), i32, own_len.device, stream)
-        start, at = new[:n_seqs + 1], 2 * n_seqs + 2
-        own_out, n_free = (own_len, self.n_free) if in_place else (new[n_seqs + 1:2 * n_seqs + 1], new[2 * n_seqs + 1:at])
-        slots, positions = new[at:at + n_tokens], new[at + n_tokens:at + 2 * n_tokens]
-        columns = pages.shape[1]
-        sdq_pages_step(_Pages(self.page_tokens, self.free.shape[0], n_seqs, n_tokens, columns,
-                              pages.stride(0) if n_seqs > 1 else columns, prefix_len, own_len.data_ptr(), new_len.data_ptr(),
-                              _ptr(done), pages.data_ptr(), self.free.data_ptr(), self.n_free.data_ptr(), start.data_ptr(),
-                              own_out.data_ptr(), n_free.data_ptr(), slots.data_ptr(), positions.data_ptr()), stream)
+        start, own_out, n_free, slots, positions = new.split_with_sizes(sizes)
+        at, at_free = new.data_ptr(), self.n_free.data_ptr()
+        out, out_free = at + 4 * n_seqs + 4, at + 8 * n_seqs + 4
+        at_slots, at_positions = out_free + 4, out_free + 4 + 4 * n_tokens
+        if in_place:
+            own_out, n_free, out, out_free = own_len, self.n_free, at_own, at_free
+        sdq_pages_step(_PAGES.pack(self.page_tokens, self.free.shape[0], n_seqs, n_tokens, columns, stride if n_seqs > 1 else columns,
+                                   prefix_len, at_own, at_new, at_done, pages.data_ptr(), self.free.data_ptr(), at_free, at, out,
+                                   out_free, at_slots, at_positions), stream)
         return PageStep(start, own_out, n_free, slots, positions)
 
 
@@ -755,20 +753,31 @@ class KVCache:
         values go to the cache.  norm: a HeadNorm, applied to every head of q
         and k ahead of the rotation."""
         import torch
-        d, tokens, shape = self.desc, batch.n_tokens, q.shape
-        if (len(shape) != 2 or shape[0] != tokens or not k.shape == v.shape == (tokens, d.kv_heads * d.head_dim)
-                or not q.stride()[1] == k.stride()[1] == v.stride()[1] == 1 or not (q.is_cuda and k.is_cuda and v.is_cuda)):
+        d, tokens, shape, rows = self.desc, batch.n_tokens, q.shape, k.shape
+        dim = d.head_dim
+        if (len(shape) != 2 or shape[0] != tokens or rows != (tokens, d.kv_heads * dim) or v.shape != rows
+                or not (q.is_cuda and k.is_cuda and v.is_cuda)):
             raise ValueError("KVCache.append: q, k and v need one row of heads x head_dim elements per token")
-        q_heads, rest = divmod(shape[1], d.head_dim)
+        (ldq, q1), (ldk, k1), (ldv, v1) = q.stride(), k.stride(), v.stride()
+        if not q1 == k1 == v1 == 1:
+            raise ValueError("KVCache.append: the elements of a row of q, k and v must be adjacent")
+        q_heads, rest = divmod(shape[1], dim)
         if rest:
             raise ValueError("KVCache.append: q's rows are not whole heads")
+        if tokens == 1:   # (a single row has no stride of its own)
+            ldq, ldk, ldv = shape[1], rows[1], rows[1]
         batch.check(d.page_tokens)
-        out = _empty((tokens, q_heads, d.head_dim), torch.bfloat16, q.device, stream)
+        kind = q.dtype
+        kind = -1 if k.dtype is not kind or v.dtype is not kind else SDQ_F32 if kind is torch.float32 else SDQ_BF16 if kind is torch.bfloat16 else -1
+        out = _empty((tokens, q_heads, dim), torch.bfloat16, q.device, stream)
         if norm is None:
-            sdq_cache_append(self.handle, batch, q_heads, q, k, v, rope, out, stream)
+            _check(lib().sdq_cache_append(self.handle, batch.ref, q_heads, q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
+                                          kind, rope.ref, out.data_ptr(), _stream(stream)), "sdq_cache_append")
         else:
-            norm.check(q_heads, d.kv_heads, d.head_dim)
-            sdq_cache_append_norm(self.handle, batch, q_heads, q, k, v, rope, norm, out, stream)
+            norm.check(q_heads, d.kv_heads, dim)
+            _check(lib().sdq_cache_append_norm(self.handle, batch.ref, q_heads, q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(),
+                                               ldv, kind, rope.ref, norm.ref, out.data_ptr(), _stream(stream)),
+                   "sdq_cache_append_norm")
         return out
 
     def alloc_workspace(self, batch: Batch, q_heads: int, stream=None, window=None, sinks=0):
@@ -847,38 +856,44 @@ def adjust_logits(logits, history=None, history_len=None, prompt_len=None, repet
     if len(shape) != 2 or logits.stride()[1] != 1 or not logits.is_cuda:
         raise ValueError("adjust_logits: logits must be a CUDA tensor (rows, vocab) with adjacent elements in a row")
     rows, vocab = shape
-    for t, dtype in ((history_len, i32), (prompt_len, i32), (repetition, f32), (frequency, f32), (presence, f32), (allowed_row, i32)):
-        if t is not None and (t.dtype is not dtype or t.shape != shape[:1] or not t.is_contiguous() or not t.is_cuda):
+    one = (rows,)
+
+    def per_row(t, dtype):
+        if t is None:
+            return 0
+        if t.dtype is not dtype or t.shape != one or not t.is_contiguous() or not t.is_cuda:
             raise ValueError("adjust_logits: repetition, frequency and presence are float32, history_len, prompt_len and "
                              "allowed_row int32, one per row, on the GPU")
-    for t, dtype, n in ((history, i32, rows), (bias_ids, i32, rows), (bias, f32, rows), (allowed, i32, None)):
-        if t is not None and (t.dtype is not dtype or t.dim() != 2 or not t.is_cuda or (n is not None and t.shape[0] != n)
-                              or (t.shape[1] > 1 and t.stride()[1] != 1)):
+        return t.data_ptr()
+
+    def table(t, dtype, n):
+        if t is None:
+            return 0, 0, 0
+        columns, stride = t.shape, t.stride()
+        if (t.dtype is not dtype or len(columns) != 2 or not t.is_cuda or (n is not None and columns[0] != n)
+                or (columns[1] > 1 and stride[1] != 1)):
             raise ValueError("adjust_logits: history, bias_ids and bias need one row for each of logits, allowed one for each "
                              "set: 2-d CUDA tensors, int32 (bias: float32), adjacent in a row")
-    if (bias_ids is None) != (bias is None) or (bias is not None and bias.shape != bias_ids.shape):
+        return t.data_ptr(), stride[0], columns[1]
+
+    at_history, ld_history, places = table(history, i32, rows)
+    at_ids, ld_ids, n_ids = table(bias_ids, i32, rows)
+    at_bias, ld_bias, n_bias = table(bias, f32, rows)
+    at_allowed, ld_allowed, words = table(allowed, i32, None)
+    if (bias_ids is None) != (bias is None) or n_ids != n_bias:
         raise ValueError("adjust_logits: bias_ids and bias come together, of one shape")
     if history is None and (history_len is not None or prompt_len is not None):
         raise ValueError("adjust_logits: history_len and prompt_len belong to a history")
     if allowed is None and allowed_row is not None:
         raise ValueError("adjust_logits: allowed_row belongs to allowed")
+    if allowed is not None and words < (vocab + 31) // 32:
+        raise ValueError("adjust_logits: the sets of allowed have too few words")
     if out is None:
         out = _empty(shape, logits.dtype, logits.device, stream)
     elif out.shape != shape or out.dtype is not logits.dtype or out.stride()[1] != 1 or not out.is_cuda:
         raise ValueError("adjust_logits: out must be like logits")
-    a = _Adjust()
-    if history is not None:
-        a.history, a.history_max = history.data_ptr() or None, history.shape[1]
-        a.history_stride = history.stride(0)
-        a.history_len, a.prompt_len = _ptr(history_len), _ptr(prompt_len)
-        a.repetition, a.frequency, a.presence = _ptr(repetition), _ptr(frequency), _ptr(presence)
-    if bias is not None and bias.shape[1]:
-        a.bias_ids, a.bias, a.n_bias = bias_ids.data_ptr(), bias.data_ptr(), bias.shape[1]
-        a.bias_ids_stride, a.bias_stride = bias_ids.stride(0), bias.stride(0)
-    if allowed is not None:
-        if allowed.shape[1] < (vocab + 31) // 32:
-            raise ValueError("adjust_logits: the sets of allowed have too few words")
-        a.allowed, a.allowed_row, a.n_allowed = allowed.data_ptr(), _ptr(allowed_row), allowed.shape[0]
-        a.allowed_stride = allowed.stride(0)
+    a = _ADJUST.pack(at_history, per_row(history_len, i32), per_row(prompt_len, i32), per_row(repetition, f32),
+                     per_row(frequency, f32), per_row(presence, f32), at_ids, at_bias, at_allowed, per_row(allowed_row, i32),
+                     ld_history, ld_ids, ld_bias, ld_allowed, places, n_bias, 0 if allowed is None else allowed.shape[0])
     sdq_adjust_logits(logits, a, out, stream)
     return out

@@ -505,6 +505,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int n = 0; n < NT; ++n) mma_bf16_16816(s[n][d & 1], a, qf[n][d][0], qf[n][d][1]);
         }
         const int key = t * kTile + g8;   // and key + 8
+        uint32_t hidden = 0;   // with a window: which scores are left out (a bit each; worked out behind a branch)
+        if (kWindow && edge) {
+#pragma unroll
+          for (int b = 0; b < 4 * NT; ++b)
+            if (!sees(b >> 2, b & 1, key + 8 * (b >> 1 & 1))) hidden |= 1u << b;
+        }
         uint32_t pf[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -512,7 +518,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             x[j] = (s[n][0][j] + s[n][1][j]) * p.scale;
-            if (edge && !sees(n, j & 1, key + 8 * (j >> 1))) x[j] = -INFINITY;
+            if (kWindow ? hidden >> (4 * n + j) & 1u : edge && key + 8 * (j >> 1) >= lim[n][j & 1]) x[j] = -INFINITY;
           }
           float mx[2];
 #pragma unroll

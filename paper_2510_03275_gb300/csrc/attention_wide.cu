@@ -111,12 +111,19 @@ struct WideItem {
   int s;                     // sequence, -1: the whole batch
   int own, count;            // its own tokens and new tokens
   int prefix_tiles, t0, t1;  // of the line: the prefix's tiles, this block's [t0, t1)
-  Line lines[2];             // with a window: which of the prefix's and of the own tiles
+};
+
+// With a window the line is of 64-key pieces, two to a tile, so that what is
+// left out, first keys apart from the window, and the ends cost half a tile
+// at most: which of the prefix's and of the own pieces, and how many.
+struct WideLine {
+  Line prefix, own;
+  int pieces;
 };
 
 // (a whole warp; false: nothing to do)
 template <bool kWindow>
-__device__ __forceinline__ bool wide_item(const AttendParams& p, int part, WideItem* w) {
+__device__ __forceinline__ bool wide_item(const AttendParams& p, int part, WideItem* w, WideLine* line) {
   const int splits = p.splits[part];
   const int id = blockIdx.x / (p.kv_heads * splits), rest = blockIdx.x % (p.kv_heads * splits);
   w->h = rest / splits;
@@ -167,10 +174,10 @@ __device__ __forceinline__ bool wide_item(const AttendParams& p, int part, WideI
     const int keys = max(0, q.own - q.count + last / p.group + 1);
     if (kWindow) {
       const int first = position_of(p, q.own - q.count + w->r0 / p.group);
-      w->lines[0] = line_of<kKeys>(p, p.b.prefix_len, 0, first);
-      w->lines[1] = line_of<kKeys>(p, keys, p.b.prefix_len, first);
-      w->prefix_tiles = w->lines[0].tiles;
-      tiles = w->prefix_tiles + w->lines[1].tiles;
+      line->prefix = line_of<kSub>(p, p.b.prefix_len, 0, first);
+      line->own = line_of<kSub>(p, keys, p.b.prefix_len, first);
+      line->pieces = line->prefix.tiles + line->own.tiles;
+      tiles = (line->pieces + 1) / 2;
     } else {
       tiles = w->prefix_tiles + (keys + kKeys - 1) / kKeys;
     }
@@ -190,6 +197,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
   __shared__ __align__(8) uint64_t full[S::kRing], empty[S::kRing], q_full, s_full[2], p_full[2][2], pv_done[2], mma_done;
   __shared__ uint32_t tmem_base;
   __shared__ volatile int tainted;   // a value that is not finite was taken out
+  __shared__ WideLine line_s;        // (read where it is needed: the softmax has no registers to spare)
   const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
   const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t ring = sbase + 2 * S::kMat;
@@ -220,7 +228,8 @@ __global__ void __launch_bounds__(kWideThreads, 1)
   pdl_launch_dependents();
   call_record_start(p.rec, p.call, blockIdx.x == 0 && tid == 0);
   WideItem w;
-  if (!wide_item<kWindow>(p, part, &w)) {   // (all warps alike)
+  WideLine line_r;
+  if (!wide_item<kWindow>(p, part, &w, &line_r)) {   // (all warps alike)
     if (warp == 8) tmem_dealloc(tmem_base, 512);
     return;
   }
@@ -229,10 +238,27 @@ __global__ void __launch_bounds__(kWideThreads, 1)
   const bool joins = p.splits[part] > 1 || p.parts > 1;
   const uint32_t tmem = tmem_base;
   bool ok = true;
-  // which tile of the prefix's or of the own ones stands at place t of the line
-  auto tile_at = [&](int t) {
-    if (kWindow) return t < w.prefix_tiles ? w.lines[0].tile(t) : w.lines[1].tile(t - w.prefix_tiles);
-    return t < w.prefix_tiles ? t : t - w.prefix_tiles;
+  if (kWindow) {
+    if (tid == 0) line_s = line_r;
+    __syncthreads();
+  }
+  const volatile WideLine& line = line_s;
+  // pieces of 64 keys that this thread block takes; of piece q: is it the prefix's, its first key
+  const int n_pieces = kWindow ? min(2 * n, line_r.pieces - 2 * w.t0) : 2 * n;
+  struct Piece {
+    bool pre;
+    int k0;
+  };
+  auto piece_at = [&](int q) {
+    const int c = 2 * w.t0 + q;
+    if (kWindow) {
+      const int np = line.prefix.tiles, i = c - np;
+      if (i < 0) return Piece{true, (c < line.prefix.a ? c : c + line.prefix.skip) * kSub};
+      return Piece{false, (i < line.own.a ? i : i + line.own.skip) * kSub};
+    }
+    const int t = c >> 1;
+    const bool pre = t < w.prefix_tiles;
+    return Piece{pre, (pre ? t : t - w.prefix_tiles) * kKeys + kSub * (c & 1)};
   };
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;\n");
@@ -242,19 +268,33 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       const int32_t* own_table = p.b.pages + (int64_t)(w.s < 0 ? 0 : w.s) * p.b.page_stride;
       // the page of the lane's box of line tile t (-1: past the last token), and the tile's boxes
       auto boxes_of = [&](int t) {
-        const int keys = t < w.prefix_tiles ? p.b.prefix_len : w.own, at = tile_at(t) * per_tile;
+        const int keys = t < w.prefix_tiles ? p.b.prefix_len : w.own, at = (t < w.prefix_tiles ? t : t - w.prefix_tiles) * per_tile;
         return max(0, min(per_tile, ((keys + box - 1) >> p.box_shift) - at));
       };
       auto row_of = [&](int t) {
-        const int at = tile_at(t) * per_tile + lane;
+        const int at = (t < w.prefix_tiles ? t : t - w.prefix_tiles) * per_tile + lane;
         const int pg = t < w.t1 && lane < boxes_of(t) ? __ldg((t < w.prefix_tiles ? p.b.prefix_pages : own_table) + at / per_page) : -1;
         // (a page outside the cache: rows outside the arrays, which read as zeros)
         return pg >= 0 && pg < p.n_pages ? ((pg * p.kv_heads + w.h) << p.page_shift) + ((at & (per_page - 1)) << p.box_shift) : -box;
       };
-      int y_next = row_of(w.t0), slot = 0;
+      // with a window, of the lane's box in its piece: is it one (not past the last key), its rows
+      auto window_row = [&](int t, bool* is) {
+        const int q = 2 * (t - w.t0) + lane / (per_tile / 2);
+        *is = false;
+        if (lane >= per_tile || q >= n_pieces) return -box;
+        const Piece c = piece_at(q);
+        const int at = (c.k0 >> p.box_shift) + lane % (per_tile / 2);
+        *is = at < (((c.pre ? p.b.prefix_len : w.own) + box - 1) >> p.box_shift);
+        const int pg = *is ? __ldg((c.pre ? p.b.prefix_pages : own_table) + at / per_page) : -1;
+        return pg >= 0 && pg < p.n_pages ? ((pg * p.kv_heads + w.h) << p.page_shift) + ((at & (per_page - 1)) << p.box_shift) : -box;
+      };
+      bool is_next = false;
+      int y_next = kWindow ? window_row(w.t0, &is_next) : row_of(w.t0), slot = 0;
       for (int t = w.t0; t < w.t1 && ok; ++t) {
-        const int y = y_next, nb = boxes_of(t);
-        y_next = row_of(t + 1);
+        const int y = y_next;
+        const uint32_t boxes = kWindow ? __ballot_sync(0xffffffffu, is_next) : 0;
+        const int nb = kWindow ? __popc(boxes) : boxes_of(t);
+        y_next = kWindow ? window_row(t + 1, &is_next) : row_of(t + 1);
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv, ++slot) {
           const int st = slot % S::kRing, r = slot / S::kRing;
@@ -263,7 +303,10 @@ __global__ void __launch_bounds__(kWideThreads, 1)
             break;
           }
           mbar_expect_tx_warp(&full[st], (uint32_t)((nb << p.box_shift) * 128 * (D / 64)));
-          for (int i = 0; i < nb; ++i) {
+          uint32_t left = boxes;
+          for (int k = 0; k < nb; ++k) {
+            const int i = kWindow ? __ffs(left) - 1 : k;
+            left &= left - 1;
             const int yi = __shfl_sync(0xffffffffu, y, i);
 #pragma unroll
             for (int half = 0; half < D / 64; ++half)
@@ -301,6 +344,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
           for (int half = 0; half < halves && ok; ++half) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
+              if (kWindow && 2 * i + j >= n_pieces) break;   // (the last tile may have one piece)
               if (ok) ok = mbar_wait_warp(&p_full[half][j], i & 1);
               if (ok && j + half == 0) ok = mbar_wait_warp(&full[vs], ((2 * i + 1) / S::kRing) & 1);
               if (!ok) break;
@@ -370,11 +414,21 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       };
       const uint32_t ts = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + 128 * half;
       const uint32_t to = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + 256 + D * half;
+      // does piece q need a look at what its keys are?  (Of both pieces of a tile before its scores are waited for:
+      // between the scores and the weights every instruction counts)
+      auto edge_of = [&](int q) {
+        const Piece c = piece_at(q);
+        const int base = c.pre ? 0 : p.b.prefix_len;
+        return c.k0 + kSub > (c.pre ? p.b.prefix_len : all) || (c.k0 < low_half - base && c.k0 + kSub > p.sinks - base) ||
+               (half == 0 && partial(c.pre, c.k0));
+      };
+      int edge = 3;
       float m = -INFINITY;        // reference maximum (log2 units)
       uint64_t l2 = 0;            // two sums
       const uint64_t scale2 = pair_of(p.scale, p.scale);
-      for (int q = 0; q < 2 * n; ++q) {
+      for (int q = 0; q < n_pieces; ++q) {
         const int i = q >> 1, j = q & 1;
+        if (kWindow && j == 0) edge = (int)edge_of(q) | (int)edge_of(q + 1) << 1;
         if (j == 0 && !mbar_wait_warp(&s_full[half], i & 1)) {
           ok = false;
           break;
@@ -384,58 +438,60 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         tmem_ld32(ts + kSub * j, x);
         tmem_ld32(ts + kSub * j + 32, x + 32);
         tmem_ld_wait();
-        const int t = w.t0 + i;
-        const bool pre = t < w.prefix_tiles;
-        const int k0 = tile_at(t) * kKeys + kSub * j, keys = pre ? p.b.prefix_len : w.own;
-        if (k0 + kSub > (pre ? keys : all)) {
-          const int see = (pre ? keys : lim) - k0;   // of these 64
-#pragma unroll
-          for (int c = 0; c < kSub; ++c)
-            if (c >= see) x[c] = 0xFF800000u;
-        }
-        if (kWindow) {
-          const int base = pre ? 0 : p.b.prefix_len;
-          if (k0 < low_half - base && k0 + kSub > p.sinks - base) {
-            const int from = p.sinks - base - k0, to = low - base - k0;   // of these 64
+        if (!kWindow || (edge >> j & 1)) {
+          const Piece piece = piece_at(q);
+          const bool pre = piece.pre;
+          const int k0 = piece.k0, keys = pre ? p.b.prefix_len : w.own;
+          if (k0 + kSub > (pre ? keys : all)) {
+            const int see = (pre ? keys : lim) - k0;   // of these 64
 #pragma unroll
             for (int c = 0; c < kSub; ++c)
-              if (c >= from && c < to) x[c] = 0xFF800000u;
+              if (c >= see) x[c] = 0xFF800000u;
           }
-        }
-        if (half == 0 && partial(pre, k0)) {
-          // (for both halves: the second's product is issued after the first's)
-          // values past the last key are leftovers (perhaps NaN): zero times them has to be zero too
-          const int vs = (2 * i + 1) % S::kRing, from = kWindow ? 0 : 8 * max(0, (pre ? keys : min(keys, all_rows)) - k0);
-          if (!mbar_wait_warp(&full[vs], ((2 * i + 1) / S::kRing) & 1)) {
-            ok = false;
-            break;
+          if (kWindow) {
+            const int base = pre ? 0 : p.b.prefix_len;
+            if (k0 < low_half - base && k0 + kSub > p.sinks - base) {
+              const int from = p.sinks - base - k0, to = low - base - k0;   // of these 64
+#pragma unroll
+              for (int c = 0; c < kSub; ++c)
+                if (c >= from && c < to) x[c] = 0xFF800000u;
+            }
           }
-          const uint32_t at = ring + vs * S::kMat + (kSub * j) * 128;   // 16-byte pieces c of the rows
+          if (half == 0 && partial(pre, k0)) {
+            // (for both halves: the second's product is issued after the first's)
+            // values past the last key are leftovers (perhaps NaN): zero times them has to be zero too
+            const int vs = (2 * i + 1) % S::kRing, from = kWindow ? 0 : 8 * max(0, (pre ? keys : min(keys, all_rows)) - k0);
+            if (!mbar_wait_warp(&full[vs], ((2 * i + 1) / S::kRing) & 1)) {
+              ok = false;
+              break;
+            }
+            const uint32_t at = ring + vs * S::kMat + (kSub * j) * 128;   // 16-byte pieces c of the rows
 #pragma unroll 1
-          for (int c = from + wtid; c < 8 * kSub; c += 256) {
-            uint4 v[2][D / 64];
+            for (int c = from + wtid; c < 8 * kSub; c += 256) {
+              uint4 v[2][D / 64];
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
+              for (int k = 0; k < 2; ++k)
 #pragma unroll
-              for (int d = 0; d < D / 64; ++d) v[k][d] = ld_shared16(at + d * kHalf + 16 * min(c + 128 * k, 8 * kSub - 1));
-            bool any = false;
+                for (int d = 0; d < D / 64; ++d) v[k][d] = ld_shared16(at + d * kHalf + 16 * min(c + 128 * k, 8 * kSub - 1));
+              bool any = false;
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
+              for (int k = 0; k < 2; ++k)
 #pragma unroll
-              for (int d = 0; d < D / 64; ++d) any |= some_not_finite(v[k][d]);
-            if (!any) continue;
+                for (int d = 0; d < D / 64; ++d) any |= some_not_finite(v[k][d]);
+              if (!any) continue;
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
+              for (int k = 0; k < 2; ++k)
 #pragma unroll
-              for (int d = 0; d < D / 64; ++d) {
-                const uint4 x = v[k][d];
-                if (c + 128 * k >= 8 * kSub || !some_not_finite(x)) continue;
-                if (k0 + ((c + 128 * k) >> 3) < keys) tainted = 1;
-                st_shared16(at + d * kHalf + 16 * (c + 128 * k), x.x & ~not_finite(x.x), x.y & ~not_finite(x.y), x.z & ~not_finite(x.z),
-                            x.w & ~not_finite(x.w));
-              }
+                for (int d = 0; d < D / 64; ++d) {
+                  const uint4 x = v[k][d];
+                  if (c + 128 * k >= 8 * kSub || !some_not_finite(x)) continue;
+                  if (k0 + ((c + 128 * k) >> 3) < keys) tainted = 1;
+                  st_shared16(at + d * kHalf + 16 * (c + 128 * k), x.x & ~not_finite(x.x), x.y & ~not_finite(x.y), x.z & ~not_finite(x.z),
+                              x.w & ~not_finite(x.w));
+                }
+            }
+            fence_proxy_async_smem();
           }
-          fence_proxy_async_smem();
         }
         float mx[4];
 #pragma unroll
@@ -512,9 +568,10 @@ __global__ void __launch_bounds__(kWideThreads, 1)
           const int32_t* own_table = p.b.pages + (int64_t)w.s * p.b.page_stride;
           if (kWindow) {
 #pragma unroll 1
-            for (int q = 0; live && q < 2 * n; ++q) {
-              const bool pre = w.t0 + (q >> 1) < w.prefix_tiles;
-              const int k0 = tile_at(w.t0 + (q >> 1)) * kKeys + kSub * (q & 1), base = pre ? 0 : p.b.prefix_len;
+            for (int q = 0; live && q < n_pieces; ++q) {
+              const Piece piece = piece_at(q);
+              const bool pre = piece.pre;
+              const int k0 = piece.k0, base = pre ? 0 : p.b.prefix_len;
               if (!partial(pre, k0)) continue;
               const int end = min(k0 + kSub, pre ? p.b.prefix_len : lim);
 #pragma unroll 1
@@ -647,8 +704,8 @@ double wide_time(const sdq_cache_s* c, const AttendParams& p, int q_heads, int p
   const int64_t blocks = wide_blocks(b, q_heads / c->desc.kv_heads, part) * c->desc.kv_heads * s;
   int64_t tiles = (part == kPrefix || p.chained || p.window > 0 ? ((int64_t)b->prefix_len + kKeys - 1) / kKeys : 0) +
                   (part == kOwn ? ((int64_t)b->max_own + kKeys - 1) / kKeys : 0);
-  // (a window, moved on by the tokens of a row block, and the first keys, each with a tile's rest at its ends)
-  if (p.window > 0) tiles = std::min<int64_t>(tiles, (p.window + 256 / p.group) / kKeys + 2 + (p.sinks + kKeys - 1) / kKeys);
+  // (a window, moved on by the tokens of a row block, and the first keys, each with a piece's rest at its ends)
+  if (p.window > 0) tiles = std::min<int64_t>(tiles, ((p.window + 256 / p.group) / kSub + 3 + (p.sinks + kSub - 1) / kSub) / 2 + 1);
   return (double)((blocks + c->sm_count - 1) / c->sm_count) * (5.0 + 1.3 * (double)((tiles + s - 1) / s));
 }
 
