@@ -22,7 +22,7 @@ struct AppendParams {
   int64_t ldq, ldk, ldv;
   uint16_t *kp, *vp, *q_out;
   int q_heads, kv_heads, dim, page, n_pages;
-  int per_part;   // 8-element units of a token that one block of a part takes
+  int per_part;   // heads of a token that one block of a part takes
   sdq_head_norm norm;
 };
 
@@ -33,81 +33,259 @@ __device__ __forceinline__ float4 load4(const uint16_t* p) {
   return make_float4(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xFFFF0000u), __uint_as_float(r.y << 16),
                      __uint_as_float(r.y & 0xFFFF0000u));
 }
+// (four of shared memory)
+__device__ __forceinline__ float4 shared4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ float4 shared4(const uint16_t* p) {
+  const uint2 r = *reinterpret_cast<const uint2*>(p);
+  return make_float4(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xFFFF0000u), __uint_as_float(r.y << 16),
+                     __uint_as_float(r.y & 0xFFFF0000u));
+}
 __device__ __forceinline__ void store4(uint16_t* p, float4 a) {
   *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w));
 }
 
+// A head's elements in a thread's hands (a: 4, b: 4 more), normalised and rotated.
+// (dim: a power of 2, so that its inverse is exact)
+__device__ __forceinline__ void normalise(float4& a, float4& b, float sum_of_squares, int dim, float eps, const float4& wa, const float4& wb) {
+  const float r = rsqrtf(sum_of_squares * (dim == 128 ? 1.f / 128 : 1.f / 64) + eps);
+  a = make_float4(a.x * r * wa.x, a.y * r * wa.y, a.z * r * wa.z, a.w * r * wa.w);
+  b = make_float4(b.x * r * wb.x, b.y * r * wb.y, b.z * r * wb.z, b.w * r * wb.w);
+}
+// split: a and b are the pairs' first and second elements; else neighbours are.
+__device__ __forceinline__ void rotate(float4& a, float4& b, const float4& cs, const float4& sn, bool split) {
+  const float4 x = a, y = b;
+  if (split) {
+    a = make_float4(x.x * cs.x - y.x * sn.x, x.y * cs.y - y.y * sn.y, x.z * cs.z - y.z * sn.z, x.w * cs.w - y.w * sn.w);
+    b = make_float4(y.x * cs.x + x.x * sn.x, y.y * cs.y + x.y * sn.y, y.z * cs.z + x.z * sn.z, y.w * cs.w + x.w * sn.w);
+  } else {
+    a = make_float4(x.x * cs.x - x.y * sn.x, x.y * cs.x + x.x * sn.x, x.z * cs.y - x.w * sn.y, x.w * cs.y + x.z * sn.y);
+    b = make_float4(y.x * cs.z - y.y * sn.z, y.y * cs.z + y.x * sn.z, y.z * cs.w - y.w * sn.w, y.w * cs.w + y.z * sn.w);
+  }
+}
+__device__ __forceinline__ float squares(const float4& a, const float4& b) {
+  return a.x * a.x + a.y * a.y + (a.z * a.z + a.w * a.w) + (b.x * b.x + b.y * b.y + (b.z * b.z + b.w * b.w));
+}
+// Where a token stands: its page (-1: its key and value are not kept), its place
+// among its sequence's tokens, its position.
+struct Place {
+  int page, at, pos;
+};
+__device__ __forceinline__ Place place_of(const AppendParams& p, int t, int s) {
+  const SeqSpan q = seq_span(p.b, s);
+  Place r;
+  r.at = q.own - q.count + (t - q.first);
+  r.pos = max(0, p.b.prefix_len + min(r.at, q.own - 1));   // (min: a token beyond max_new has no place of its own)
+  r.page = -1;
+  if (t < q.first + q.count && r.at >= 0 && r.at < q.own) r.page = __ldg(p.b.pages + (int64_t)s * p.b.page_stride + r.at / p.page);
+  if (r.page >= p.n_pages) r.page = -1;
+  return r;
+}
+
 // Every element is read once and written once, rounded to bf16 there; what
 // bounds it is HBM for prompts and the launch for single tokens.  A thread
-// takes 8 elements of one head: 4 and their 4 partners dim / 2 further on, or
-// 8 neighbours, so that both halves of a pair are in its registers.  grid.x:
-// tokens, grid.y: parts of a token's heads.  2566 tokens of 64 + 2 x 8 heads of
-// 128, fp32: 28 us (84 % of the measured copy bandwidth); one token: 1.8 us (a
-// graph of 30 calls).
+// takes 8 elements of a head: 4 and their 4 partners dim / 2 further on, or
+// 8 neighbours, so that both halves of a pair are in its registers, and the same
+// ones of every head that it comes to, so that their cosines, sines and weights
+// are read once per token (a read for each head, from the L1, cost as much as
+// the data).  The next head's elements are under way while one is worked on.
+// grid.x: tokens, grid.y: parts of a token's heads.  2566 tokens of 64 + 2 x 8
+// heads of 128, fp32: 27.6 us (86 % of the measured copy bandwidth); one token:
+// 1.9 us, 2.2 with norms (a graph of 30 calls).
 // kNorm: a head's threads are neighbours in one warp (8 or 16 of them) and add up
 // its squares, all in fp32; whole warps stay in the loop for it.
 template <class T, bool kNorm>
-__global__ void __launch_bounds__(kThreads) append_kernel(AppendParams p) {
+__global__ void __launch_bounds__(kThreads, kNorm ? 3 : 6) append_kernel(const AppendParams p) {
   pdl_wait();
   pdl_launch_dependents();
-  const int t = blockIdx.x, per_head = p.dim / 8, half = p.rope.dim / 2;
-  const int s = seq_of_token(p.b.token_start, p.b.n_seqs, t);
-  const SeqSpan q = seq_span(p.b, s);
-  const int at = q.own - q.count + (t - q.first);
-  const int pos = max(0, p.b.prefix_len + min(at, q.own - 1));   // (min: a token beyond max_new has no place of its own)
-  int page = -1;
-  if (t < q.first + q.count && at >= 0 && at < q.own) page = __ldg(p.b.pages + (int64_t)s * p.b.page_stride + at / p.page);
-  const bool keep = page >= 0 && page < p.n_pages;
-  const int units = (p.q_heads + 2 * p.kv_heads) * per_head;
-  const int end = min(units, ((int)blockIdx.y + 1) * p.per_part);
-  for (int i = blockIdx.y * p.per_part + threadIdx.x; (kNorm ? i & ~31 : i) < end; i += kThreads) {
-    const int u = kNorm ? min(i, end - 1) : i;   // (parts are whole heads; a lane past the end only takes part in the sums)
-    const int h = u / per_head, c = u - h * per_head;
+  const int t = blockIdx.x, lanes = p.dim / 8, half = p.rope.dim / 2;   // threads of a head
+  const int g = threadIdx.x / lanes, c = threadIdx.x - g * lanes, step = kThreads / lanes;
+  const bool turn = 8 * c < p.rope.dim, split = turn && !p.rope.interleaved;
+  const int ea = split ? 4 * c : 8 * c, eb = split ? 4 * c + half : 8 * c + 4;
+  const int n_heads = p.q_heads + 2 * p.kv_heads, last = min(n_heads, ((int)blockIdx.y + 1) * p.per_part) - 1;
+  const Place at = place_of(p, t, seq_of_token(p.b.token_start, p.b.n_seqs, t));
+  auto source = [&](int h) {
+    return (h < p.q_heads                ? static_cast<const T*>(p.q) + t * p.ldq + h * p.dim
+            : h < p.q_heads + p.kv_heads ? static_cast<const T*>(p.k) + t * p.ldk + (h - p.q_heads) * p.dim
+                                         : static_cast<const T*>(p.v) + t * p.ldv + (h - p.q_heads - p.kv_heads) * p.dim);
+  };
+  // (kNorm: the heads of a warp, all of them while one is left: a lane past the end only takes part in the sums)
+  const int together = kNorm ? 32 / lanes - 1 : 0;
+  int h = blockIdx.y * p.per_part + g;
+  if ((h & ~together) > last) return;
+  const T* src = source(min(h, last));
+  float4 xa = load4(src + ea), xb = load4(src + eb), cs = {}, sn = {}, wqa = {}, wqb = {}, wka = {}, wkb = {};
+  if (turn) {
+    cs = load4(p.rope.cos + (int64_t)at.pos * half + 4 * c);
+    sn = load4(p.rope.sin + (int64_t)at.pos * half + 4 * c);
+  }
+  if (kNorm) {
+    if (p.norm.q && !p.norm.q_per_head) wqa = load4(p.norm.q + ea), wqb = load4(p.norm.q + eb);
+    if (p.norm.k && !p.norm.k_per_head) wka = load4(p.norm.k + ea), wkb = load4(p.norm.k + eb);
+  }
+  for (; (h & ~together) <= last; h += step) {
+    float4 a = xa, b = xb;
+    if (((h + step) & ~together) <= last) {
+      src = source(min(h + step, last));
+      xa = load4(src + ea);
+      xb = load4(src + eb);
+    }
     const bool is_q = h < p.q_heads, is_v = h >= p.q_heads + p.kv_heads;
-    const int kh = is_v ? h - p.q_heads - p.kv_heads : is_q ? h : h - p.q_heads;
-    const T* src = is_q   ? static_cast<const T*>(p.q) + t * p.ldq + h * p.dim
-                   : is_v ? static_cast<const T*>(p.v) + t * p.ldv + kh * p.dim
-                          : static_cast<const T*>(p.k) + t * p.ldk + kh * p.dim;
-    const bool turn = !is_v && 8 * c < p.rope.dim;
-    const bool split = turn && !p.rope.interleaved;
-    const int ea = split ? 4 * c : 8 * c, eb = split ? 4 * c + half : 8 * c + 4;
-    float4 a = load4(src + ea), b = load4(src + eb);
+    const int kh = is_q ? h : is_v ? h - p.q_heads - p.kv_heads : h - p.q_heads;
     if (kNorm) {
-      float sq = a.x * a.x + a.y * a.y + (a.z * a.z + a.w * a.w) + (b.x * b.x + b.y * b.y + (b.z * b.z + b.w * b.w));
-      for (int d = 1; d < per_head; d <<= 1) sq += __shfl_xor_sync(0xffffffffu, sq, d);
+      float sq = squares(a, b);
+      for (int d = 1; d < lanes; d <<= 1) sq += __shfl_xor_sync(0xffffffffu, sq, d);
+      if (h > last) break;
       const float* w = is_q ? p.norm.q : is_v ? nullptr : p.norm.k;
       if (w) {
-        if (is_q ? p.norm.q_per_head : p.norm.k_per_head) w += kh * p.dim;
-        const float r = rsqrtf(sq / (float)p.dim + p.norm.eps);
-        const float4 wa = load4(w + ea), wb = load4(w + eb);
-        a = make_float4(a.x * r * wa.x, a.y * r * wa.y, a.z * r * wa.z, a.w * r * wa.w);
-        b = make_float4(b.x * r * wb.x, b.y * r * wb.y, b.z * r * wb.z, b.w * r * wb.w);
-      }
-      if (i >= end) continue;
-    }
-    if (turn) {
-      const float4 cs = load4(p.rope.cos + (int64_t)pos * half + 4 * c);
-      const float4 sn = load4(p.rope.sin + (int64_t)pos * half + 4 * c);
-      if (split) {
-        const float4 x = a, y = b;
-        a = make_float4(x.x * cs.x - y.x * sn.x, x.y * cs.y - y.y * sn.y, x.z * cs.z - y.z * sn.z, x.w * cs.w - y.w * sn.w);
-        b = make_float4(y.x * cs.x + x.x * sn.x, y.y * cs.y + x.y * sn.y, y.z * cs.z + x.z * sn.z, y.w * cs.w + x.w * sn.w);
-      } else {
-        const float4 x = a, y = b;
-        a = make_float4(x.x * cs.x - x.y * sn.x, x.y * cs.x + x.x * sn.x, x.z * cs.y - x.w * sn.y, x.w * cs.y + x.z * sn.y);
-        b = make_float4(y.x * cs.z - y.y * sn.z, y.y * cs.z + y.x * sn.z, y.z * cs.w - y.w * sn.w, y.w * cs.w + y.z * sn.w);
+        float4 wa = is_q ? wqa : wka, wb = is_q ? wqb : wkb;
+        if (is_q ? p.norm.q_per_head : p.norm.k_per_head) wa = load4(w + kh * p.dim + ea), wb = load4(w + kh * p.dim + eb);
+        normalise(a, b, sq, p.dim, p.norm.eps, wa, wb);
       }
     }
+    if (turn && !is_v) rotate(a, b, cs, sn, split);
     uint16_t* dst;
     if (is_q) {
-      dst = p.q_out + ((int64_t)t * p.q_heads + h) * p.dim;
+      dst = p.q_out + ((int64_t)t * p.q_heads + kh) * p.dim;
     } else {
-      if (!keep) continue;
-      dst = (is_v ? p.vp : p.kp) + (((int64_t)page * p.kv_heads + kh) * p.page + at % p.page) * p.dim;
+      if (at.page < 0) continue;
+      dst = (is_v ? p.vp : p.kp) + (((int64_t)at.page * p.kv_heads + kh) * p.page + at.at % p.page) * p.dim;
     }
     store4(dst + ea, a);
     store4(dst + eb, b);
   }
+}
+
+// The same for many tokens.  Loads that wait in registers are too few bytes
+// under way here (the arithmetic needs the registers): a warp streams pieces of
+// kPiece bytes, some heads of one token's q, k or v, through a ring of its own in
+// shared memory, 192 KB of an SM under way at once.  The line of pieces, token
+// by token, is cut into equal shares for all warps; what a token needs (its
+// place, its cosines and sines) is looked up when a share comes to it.
+// 3710 tokens of 64 + 2 x 8 heads of 128, normalised: fp32 42.5 us (79 % of the
+// measured copy bandwidth; append_kernel 52), bf16 38.3 (61.6: the sums'
+// shuffles, not the bytes); without norms fp32 40.0 (37.8, so these stay
+// there), bf16 28.8 (34.5).  256 tokens, normalised: fp32 7.5 (6.3), bf16 6.3
+// (6.9); 512 of 3 x 12 heads of 64: 4.6 (5.4), 256 of them 4.5 (3.5).
+constexpr int kStreamWarps = 16, kPiece = 4096, kStages = 3;
+constexpr int64_t kStreamHeads = 24576;   // of q, k and v, from which this kernel takes a call
+constexpr int kStreamSmem = kStreamWarps * kStages * kPiece;
+
+template <class T, bool kNorm>
+__global__ void __launch_bounds__(32 * kStreamWarps) append_stream_kernel(const AppendParams p) {
+  extern __shared__ __align__(16) uint8_t ring[];
+  pdl_wait();
+  pdl_launch_dependents();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  uint8_t* mine = ring + warp * (kStages * kPiece);
+  const int lanes = p.dim / 8, half = p.rope.dim / 2, c = lane & (lanes - 1);
+  const bool turn = 8 * c < p.rope.dim, split = turn && !p.rope.interleaved;
+  const int ea = split ? 4 * c : 8 * c, eb = split ? 4 * c + half : 8 * c + 4;
+  const int hp = kPiece / (p.dim * (int)sizeof(T)), nq = (p.q_heads + hp - 1) / hp, nk = (p.kv_heads + hp - 1) / hp;
+  const int64_t per_token = nq + 2 * nk, total = per_token * p.b.n_tokens, warps = (int64_t)gridDim.x * kStreamWarps;
+  const int64_t share = (total + warps - 1) / warps, i0 = min(total, ((int64_t)blockIdx.x * kStreamWarps + warp) * share);
+  const int n = (int)(min(total, i0 + share) - i0);
+  if (n <= 0) return;
+  // piece: of token t, the part-th of its pieces
+  struct Where {
+    int t, part;
+  };
+  auto next = [&](Where& w) {
+    if (++w.part == (int)per_token) w.part = 0, ++w.t;
+  };
+  // which of q, k, v (0, 1, 2), the first head, how many
+  struct Heads {
+    int of, first, count;
+  };
+  auto heads_of = [&](int part) {
+    Heads h;
+    h.of = part < nq ? 0 : part < nq + nk ? 1 : 2;
+    h.first = (part - (h.of == 0 ? 0 : h.of == 1 ? nq : nq + nk)) * hp;
+    h.count = min(hp, (h.of == 0 ? p.q_heads : p.kv_heads) - h.first);
+    return h;
+  };
+  Where in{(int)(i0 / per_token), (int)(i0 % per_token)}, at = in;
+  int issued = 0;
+  auto issue = [&]() {
+    if (issued < n) {
+      const Heads h = heads_of(in.part);
+      const T* src = (h.of == 0   ? static_cast<const T*>(p.q) + in.t * p.ldq
+                      : h.of == 1 ? static_cast<const T*>(p.k) + in.t * p.ldk
+                                  : static_cast<const T*>(p.v) + in.t * p.ldv) + h.first * p.dim;
+      uint8_t* dst = mine + (issued % kStages) * kPiece;
+      for (int j = 16 * lane; j < h.count * p.dim * (int)sizeof(T); j += 512) cp_async16(dst + j, reinterpret_cast<const uint8_t*>(src) + j, 16);
+      next(in);
+    }
+    cp_async_commit();
+    ++issued;
+  };
+  for (int k = 0; k < kStages - 1; ++k) issue();
+  float4 cs = {}, sn = {}, wqa = {}, wqb = {}, wka = {}, wkb = {};
+  if (kNorm) {
+    if (p.norm.q && !p.norm.q_per_head) wqa = load4(p.norm.q + ea), wqb = load4(p.norm.q + eb);
+    if (p.norm.k && !p.norm.k_per_head) wka = load4(p.norm.k + ea), wkb = load4(p.norm.k + eb);
+  }
+  int s = -1, s_end = 0, t = -1;   // the sequence, the token behind it, the token that is looked up
+  Place place{};
+  for (int i = 0; i < n; ++i, next(at)) {
+    issue();
+    if (at.t != t) {
+      t = at.t;
+      if (s < 0 || t >= s_end) {
+        s = seq_of_token(p.b.token_start, p.b.n_seqs, t);
+        s_end = s + 1 < p.b.n_seqs ? __ldg(p.b.token_start + s + 1) : p.b.n_tokens;
+      }
+      place = place_of(p, t, s);
+      if (turn) {
+        cs = load4(p.rope.cos + (int64_t)place.pos * half + 4 * c);
+        sn = load4(p.rope.sin + (int64_t)place.pos * half + 4 * c);
+      }
+    }
+    cp_async_wait_group<kStages - 1>();
+    __syncwarp();
+    const Heads h = heads_of(at.part);
+    const T* from = reinterpret_cast<const T*>(mine + (i % kStages) * kPiece);
+    const float* w = kNorm ? (h.of == 0 ? p.norm.q : h.of == 1 ? p.norm.k : nullptr) : nullptr;
+    const bool each = kNorm && (h.of == 0 ? p.norm.q_per_head : p.norm.k_per_head);
+    const bool keep = h.of == 0 || place.page >= 0;
+    uint16_t* to = h.of == 0 ? p.q_out + ((int64_t)t * p.q_heads + h.first) * p.dim
+                             : (h.of == 1 ? p.kp : p.vp) + (((int64_t)max(place.page, 0) * p.kv_heads + h.first) * p.page + place.at % p.page) * p.dim;
+    const int64_t ld = h.of == 0 ? p.dim : (int64_t)p.page * p.dim;
+    // kBatch heads of a thread at once, so that their chains of shuffles run side by side (whole warps)
+    constexpr int kBatch = 4;
+    const int mine_first = lane / lanes, step = 32 / lanes;
+    for (int g0 = 0; g0 < h.count; g0 += kBatch * step) {
+      float4 a[kBatch], b[kBatch];
+      float sq[kBatch];
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        const int k = min(g0 + mine_first + u * step, h.count - 1);
+        a[u] = shared4(from + k * p.dim + ea);
+        b[u] = shared4(from + k * p.dim + eb);
+        sq[u] = squares(a[u], b[u]);
+      }
+      if (kNorm && w) {
+        for (int d = 1; d < lanes; d <<= 1) {
+#pragma unroll
+          for (int u = 0; u < kBatch; ++u) sq[u] += __shfl_xor_sync(0xffffffffu, sq[u], d);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        const int k = g0 + mine_first + u * step;
+        if (k >= h.count || !keep) continue;
+        if (kNorm && w) {
+          float4 wa = h.of == 0 ? wqa : wka, wb = h.of == 0 ? wqb : wkb;
+          if (each) wa = load4(w + (h.first + k) * p.dim + ea), wb = load4(w + (h.first + k) * p.dim + eb);
+          normalise(a[u], b[u], sq[u], p.dim, p.norm.eps, wa, wb);
+        }
+        if (turn && h.of < 2) rotate(a[u], b[u], cs, sn, split);
+        store4(to + k * ld + ea, a[u]);
+        store4(to + k * ld + eb, b[u]);
+      }
+    }
+    __syncwarp();   // (the piece is read)
+  }
+  cp_async_wait_all();
 }
 
 bool valid_desc(const sdq_cache_desc* d) {
@@ -234,15 +412,28 @@ static int append(sdq_cache c, const sdq_batch* b, int32_t q_heads, const void* 
   p.ldq = ldq; p.ldk = ldk; p.ldv = ldv;
   p.kp = c->k; p.vp = c->v; p.q_out = q_out;
   p.q_heads = q_heads; p.kv_heads = c->desc.kv_heads; p.dim = d; p.page = c->desc.page_tokens; p.n_pages = c->desc.n_pages;
-  const int units = (q_heads + 2 * c->desc.kv_heads) * (d / 8);
-  const int parts = std::max(1, std::min((units + kThreads - 1) / kThreads, 2 * c->sm_count / b->n_tokens));
-  p.per_part = ((units + parts - 1) / parts + kThreads - 1) / kThreads * kThreads;
-  const dim3 grid((unsigned)b->n_tokens, (unsigned)((units + p.per_part - 1) / p.per_part));
+  const int heads = q_heads + 2 * c->desc.kv_heads, step = kThreads / (d / 8);   // heads that a block has in hand at once
+  const int parts = std::max(1, std::min((heads + step - 1) / step, 2 * c->sm_count / b->n_tokens));
+  p.per_part = ((heads + parts - 1) / parts + step - 1) / step * step;
+  const dim3 grid((unsigned)b->n_tokens, (unsigned)((heads + p.per_part - 1) / p.per_part));
   cudaStream_t cs = (cudaStream_t)stream;
-  auto run = [&](auto kernel) { return launch_pdl(kernel, grid, dim3(kThreads), 0, cs, p); };
-  const cudaError_t e = type == SDQ_F32 ? norm ? run(append_kernel<float, true>) : run(append_kernel<float, false>)
-                        : norm          ? run(append_kernel<uint16_t, true>)
-                                        : run(append_kernel<uint16_t, false>);
+  cudaError_t e;
+  if ((norm || type == SDQ_BF16) && (int64_t)b->n_tokens * heads >= kStreamHeads) {
+    static std::atomic<int> smem_set[3][64];
+    auto run = [&](auto kernel, int which) {
+      const cudaError_t set = smem_limit_once(kernel, kStreamSmem, c->device, smem_set[which]);
+      if (set != cudaSuccess) return set;
+      return launch_pdl(kernel, dim3((unsigned)c->sm_count), dim3(32 * kStreamWarps), (size_t)kStreamSmem, cs, p);
+    };
+    e = type == SDQ_F32 ? run(append_stream_kernel<float, true>, 0)
+        : norm          ? run(append_stream_kernel<uint16_t, true>, 1)
+                        : run(append_stream_kernel<uint16_t, false>, 2);
+  } else {
+    auto run = [&](auto kernel) { return launch_pdl(kernel, grid, dim3(kThreads), 0, cs, p); };
+    e = type == SDQ_F32 ? norm ? run(append_kernel<float, true>) : run(append_kernel<float, false>)
+        : norm          ? run(append_kernel<uint16_t, true>)
+                        : run(append_kernel<uint16_t, false>);
+  }
   return e == cudaSuccess ? SDQ_OK : SDQ_ERR_CUDA;
 }
 

@@ -38,7 +38,7 @@ __device__ __forceinline__ void scan(uint32_t (&v)[N], uint32_t (&total)[N], uin
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < N; ++k) {
-    uint32_t w = sums[k][lane];   // (every warp on its own)
+    uint32_t w = lane < (int)(blockDim.x >> 5) ? sums[k][lane] : 0;   // (every warp on its own)
     for (int d = 1; d < 32; d <<= 1) {
       const uint32_t o = __shfl_up_sync(0xffffffffu, w, d);
       if (lane >= d) w = add(w, o);
@@ -87,48 +87,58 @@ struct Before {
 };
 
 // One cluster: every thread block sums up all sequences (a thread `per`
-// neighbours of them), so that each can place any token by itself, and takes
-// its share of the pages that come back and of the tokens.  A few thousand
-// integers move; a chain of latencies bounds it.
-__global__ void __launch_bounds__(kThreads) pages_kernel(const PagesParams p) {
+// neighbours of them, kOne: one, kept in registers), so that each can place
+// any token by itself, and takes its share of the pages that come back and of
+// the tokens.  A few thousand integers move; a chain of latencies bounds it.
+template <bool kOne>
+__global__ void __launch_bounds__(kThreads, 1) pages_kernel(const PagesParams p) {
   __shared__ uint32_t sums[3][kWarps];
   __shared__ Before before[kThreads];            // a thread's first sequence
+  __shared__ Ask asks[kOne ? kThreads : 1];
   __shared__ uint32_t starts[kThreads + 1], backs[kThreads + 1];
   const sdq_pages& a = p.a;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, warps = blockDim.x >> 5;
   const int size = 1 << p.shift, blocks = gridDim.x;
   pdl_wait();
   pdl_launch_dependents();
   const int s0 = min(tid * p.per, a.n_seqs), s1 = min(s0 + p.per, a.n_seqs);
   const uint32_t had = (uint32_t)min(max(__ldcg(a.n_free), 0), a.n_pages);
   uint32_t asked[3] = {0, 0, 0}, all[3];         // pages back, tokens, pages
-  for (int s = s0; s < s1; ++s) {
-    const Ask q = ask_of(p, s);
-    asked[0] = add(asked[0], q.back);
-    asked[1] = add(asked[1], q.fresh);
-    asked[2] = add(asked[2], q.need);
+  Ask mine{};
+  if (kOne && s0 < s1) {
+    mine = ask_of(p, s0);
+    asks[tid] = mine;
+    asked[0] = mine.back;
+    asked[1] = mine.fresh;
+    asked[2] = mine.need;
   }
+  if (!kOne)
+    for (int s = s0; s < s1; ++s) {
+      const Ask q = ask_of(p, s);
+      asked[0] = add(asked[0], q.back);
+      asked[1] = add(asked[1], q.fresh);
+      asked[2] = add(asked[2], q.need);
+    }
   scan(asked, all, sums);
   const uint32_t available = min(had + all[0], (uint32_t)a.n_pages);
   Before b{asked[1], asked[2], 0, 0};
-  for (int s = s0; s < s1; ++s) b.take(ask_of(p, s), (uint32_t)a.n_tokens, available);
+  if (kOne) b.take(mine, (uint32_t)a.n_tokens, available);   // (one without a sequence asks for nothing)
+  else
+    for (int s = s0; s < s1; ++s) b.take(ask_of(p, s), (uint32_t)a.n_tokens, available);
   uint32_t given[2] = {b.tokens, b.pages}, taken[2];
   scan(given, taken, sums);
   before[tid] = Before{asked[1], asked[2], given[0], given[1]};
   starts[tid] = given[0];
   backs[tid] = asked[0];
-  if (tid == 0) {
-    starts[kThreads] = taken[0];
-    backs[kThreads] = all[0];
-  }
+  if (tid == 0) backs[blockDim.x] = all[0];
   __syncthreads();
   // pages that come back, on top of the free ones: a warp takes a thread's sequences
   if (all[0] > 0) {
-    for (int c = blockIdx.x * kWarps + warp; c < kThreads; c += blocks * kWarps) {
+    for (int c = blockIdx.x * warps + warp; c < (int)blockDim.x; c += blocks * warps) {
       if (backs[c + 1] == backs[c]) continue;
       uint32_t at = had + backs[c];
       for (int s = c * p.per; s < min((c + 1) * p.per, a.n_seqs); ++s) {
-        const int n = (int)ask_of(p, s).back;
+        const int n = (int)(kOne ? asks[c] : ask_of(p, s)).back;
         const int32_t* row = a.pages + (int64_t)s * a.page_stride;
 #pragma unroll 4
         for (int i = lane; i < n; i += 32)
@@ -136,25 +146,32 @@ __global__ void __launch_bounds__(kThreads) pages_kernel(const PagesParams p) {
         at = add(at, (uint32_t)n);
       }
     }
+    // (the pages go out again below; and nobody writes a table that is read here)
+    if (blocks > 1) cluster_sync();
+    else __syncthreads();
   }
-  cluster_sync();
-  for (int t = blockIdx.x * kThreads + tid; t < a.n_tokens; t += blocks * kThreads) {
+  for (int t = blockIdx.x * blockDim.x + tid; t < a.n_tokens; t += blocks * blockDim.x) {
     int slot = -1, position = 0;
     if ((uint32_t)t < taken[0]) {
       int c = 0;   // the last thread whose first sequence starts at t or before it
-      for (int d = kThreads / 2; d; d >>= 1)
+      for (int d = blockDim.x / 2; d; d >>= 1)
         if (starts[c + d] <= (uint32_t)t) c += d;
       Before x = before[c];
       int s = c * p.per;
       Ask q;
-      uint32_t first_page, got, first;
-      do {
-        q = ask_of(p, s++);
-        first = x.tokens;
-        first_page = x.pages;
-        got = x.take(q, (uint32_t)a.n_tokens, available);
-      } while ((uint32_t)t >= first + got && s < a.n_seqs);
-      --s;
+      uint32_t first = x.tokens, first_page = x.pages;
+      if (kOne) {
+        q = asks[c];
+      } else {
+        uint32_t got;
+        do {
+          q = ask_of(p, s++);
+          first = x.tokens;
+          first_page = x.pages;
+          got = x.take(q, (uint32_t)a.n_tokens, available);
+        } while ((uint32_t)t >= first + got && s < a.n_seqs);
+        --s;
+      }
       const int place = q.at + (int)((uint32_t)t - first), column = place >> p.shift, held = (q.at + size - 1) >> p.shift;
       int32_t* entry = a.pages + (int64_t)s * a.page_stride + column;
       int page;
@@ -170,13 +187,15 @@ __global__ void __launch_bounds__(kThreads) pages_kernel(const PagesParams p) {
     if (a.slots) a.slots[t] = slot;
     if (a.positions) a.positions[t] = position;
   }
-  // lengths last: they may stand where they were read
+  // lengths last: they may stand where they were read (by every thread block, and,
+  // where a thread has several sequences, for the tokens too)
+  if (blocks > 1) cluster_sync();
+  else if (!kOne) __syncthreads();
+  if (blockIdx.x != 0) return;
   uint32_t first = given[0];
   b = before[tid];
-  cluster_sync();
-  if (blockIdx.x != 0) return;
   for (int s = s0; s < s1; ++s) {
-    const Ask q = ask_of(p, s);
+    const Ask q = kOne ? mine : ask_of(p, s);
     a.token_start[s] = (int32_t)first;
     const uint32_t got = b.take(q, (uint32_t)a.n_tokens, available);
     first += got;
@@ -212,12 +231,16 @@ extern "C" int sdq_pages_step(const sdq_pages* a, void* stream) {
   p.a = *a;
   p.shift = 4;
   while ((1 << p.shift) < a->page_tokens) ++p.shift;
-  p.per = (a->n_seqs + kThreads - 1) / kThreads;
+  // Threads for the sequences, a power of 2, and for the tokens; one thread block
+  // for every 4096 tokens, or entries that may come back, up to 8.
+  int threads = 128;
+  while (threads < kThreads && threads < std::max(a->n_seqs, std::min(a->n_tokens, kThreads))) threads *= 2;
+  p.per = (a->n_seqs + threads - 1) / threads;
   cudaLaunchConfig_t cfg = {};
   const int64_t moved = std::max<int64_t>(a->n_tokens, a->done ? std::min<int64_t>(a->n_pages, (int64_t)a->n_seqs * a->page_columns) : 0);
   const unsigned blocks = (unsigned)std::min<int64_t>(8, (moved + 4095) / 4096);
   cfg.gridDim = dim3(blocks);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3((unsigned)threads);
   cfg.stream = (cudaStream_t)stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -226,6 +249,7 @@ extern "C" int sdq_pages_step(const sdq_pages* a, void* stream) {
   attr[1].val.clusterDim.x = blocks;
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, pages_kernel, p) == cudaSuccess ? SDQ_OK : SDQ_ERR_CUDA;
+  cfg.numAttrs = blocks > 1 ? 2 : 1;
+  const cudaError_t e = p.per == 1 ? cudaLaunchKernelEx(&cfg, pages_kernel<true>, p) : cudaLaunchKernelEx(&cfg, pages_kernel<false>, p);
+  return e == cudaSuccess ? SDQ_OK : SDQ_ERR_CUDA;
 }

@@ -1,12 +1,13 @@
 """Serving with the quantized layer: a decoder whose linears are Sigma-Delta
-plans, a paged cache behind a prefix that all requests share, attention over
-it, and sampling.
+plans, a paged cache behind a prefix that all requests share, whose pages come
+from a pool, attention over it (all of it, or a window and first tokens),
+penalties and sampling.
 
     python -m paper_2510_03275_gb300.serve --batch 32 --prefix 2000 --new 64
 
 builds one of random weights, answers a batch of random requests and prints a
-JSON line.  Decoding steps replay one CUDA graph: its batch's lengths and last
-tokens live on the GPU and move on inside the graph.
+JSON line.  Decoding steps replay one CUDA graph: its batch's lengths, block
+tables, histories and last tokens live on the GPU and move on inside the graph.
 """
 from __future__ import annotations
 
@@ -16,7 +17,7 @@ import time
 from dataclasses import dataclass
 from fractions import Fraction
 
-from . import Batch, CacheDesc, KVCache, LayerDesc, Plan, Rope, sample, workloads as W
+from . import Batch, CacheDesc, HeadNorm, KVCache, LayerDesc, PagePool, Plan, Rope, adjust_logits, sample, workloads as W
 
 
 @dataclass(frozen=True)
@@ -30,6 +31,9 @@ class Shape:
     vocab: int = 32000
     block: int = 128
     osr: Fraction = Fraction(2)
+    qk_norm: bool = False        # norms of the heads of queries and keys
+    window: int = 0              # positions that a token sees (0: all), beside the first `sinks`
+    sinks: int = 0
 
     def linears(self):
         """(name, n_out, k_in) of every linear; those that read the same input are one."""
@@ -48,6 +52,10 @@ def random_weights(shape: Shape, seed=0, device="cuda"):
     g = torch.Generator(device).manual_seed(seed)
     w = {name: torch.randn((n, k), generator=g, device=device) * k ** -0.5 for name, n, k in shape.linears()}
     w["embedding"] = torch.randn((shape.vocab, shape.hidden), generator=g, device=device)
+    if shape.qk_norm:
+        for i in range(shape.layers):
+            for name in ("q_norm", "k_norm"):
+                w[f"{i}.{name}"] = 1 + 0.2 * torch.randn(shape.head_dim, generator=g, device=device)
     return w
 
 
@@ -58,7 +66,7 @@ def _norm(x):
 
 
 class Decoder:
-    """The plans and codes of a decoder, and a cache per layer."""
+    """The plans and codes of a decoder, a cache per layer, and the pool of their pages."""
 
     def __init__(self, shape: Shape, weights, n_pages: int, page_tokens=16, n_pos=8192, signs=None):
         self.shape, self.page_tokens, self.n_pages = shape, page_tokens, n_pages
@@ -70,7 +78,11 @@ class Decoder:
             self.layers[name] = plan, plan.pack(codes), alpha
         desc = CacheDesc(shape.kv_heads, shape.head_dim, page_tokens, n_pages)
         self.caches = [KVCache(desc, device=self.embedding.device) for _ in range(shape.layers)]
+        self.pool = PagePool(page_tokens, n_pages=n_pages, device=self.embedding.device)
         self.rope = Rope.table(n_pos, shape.head_dim, device=self.embedding.device)
+        self.norms = [HeadNorm(weights[f"{i}.q_norm"], weights[f"{i}.k_norm"], 1e-5) if shape.qk_norm else None
+                      for i in range(shape.layers)]
+        self.seen = dict(window=shape.window, sinks=shape.sinks) if shape.window else {}
 
     def linear(self, name, x):
         plan, codes, alpha = self.layers[name]
@@ -81,12 +93,12 @@ class Decoder:
         import torch
         s = self.shape
         q_width, kv_width = s.q_heads * s.head_dim, s.kv_heads * s.head_dim
-        ws = self.caches[0].alloc_workspace(batch, s.q_heads)   # (the layers take turns on it)
+        ws = self.caches[0].alloc_workspace(batch, s.q_heads, **self.seen)   # (the layers take turns on it)
         h = self.embedding[tokens.long()]
         for i, cache in enumerate(self.caches):
             q, k, v = self.linear(f"{i}.qkv", _norm(h)).split([q_width, kv_width, kv_width], dim=1)
-            q = cache.append(batch, q, k, v, self.rope)
-            a = cache.attend(batch, q, ws=ws)
+            q = cache.append(batch, q, k, v, self.rope, norm=self.norms[i])
+            a = cache.attend(batch, q, ws=ws, **self.seen)
             h = h + self.linear(f"{i}.o", a.flatten(1))
             gate, up = self.linear(f"{i}.gate_up", _norm(h)).chunk(2, dim=1)
             h = h + self.linear(f"{i}.down", (gate * torch.sigmoid(gate) * up).to(torch.bfloat16))
@@ -94,12 +106,14 @@ class Decoder:
 
 
 def generate(dec: Decoder, prefix, prompts, n_new, u, temperature=None, top_k=None, top_p=None, min_p=None, graph=True,
-             keep_logits=False):
+             keep_logits=False, repetition=None, frequency=None, presence=None, **adjust):
     """Answer requests that all begin with the tokens `prefix` (a list, may be
     empty) and go on with their own `prompts` (lists of at least one token):
     n_new tokens each, from random numbers u (n_new x requests, on the GPU), as
     an int32 tensor (n_new x requests); with keep_logits also the logits that
-    they were drawn from.  Settings as in `sample`."""
+    they were drawn from.  Settings as in `sample`; penalties for tokens that
+    repeat, biases and allowed tokens (bias_ids, bias, allowed, allowed_row) as
+    in `adjust_logits`."""
     import torch
     dev, page, n = dec.embedding.device, dec.page_tokens, len(prompts)
     ints = lambda x: torch.tensor(x, dtype=torch.int32, device=dev)
@@ -108,32 +122,42 @@ def generate(dec: Decoder, prefix, prompts, n_new, u, temperature=None, top_k=No
     n_prefix = -(-len(prefix) // page)
     if min(lens) < 1 or n_prefix + sum(per) > dec.n_pages:
         raise ValueError("generate: an empty prompt, or more tokens than the cache has pages for")
-    prefix_pages = list(range(n_prefix))
-    at, table = n_prefix, []
-    for m in per:
-        table.append(list(range(at, at + m)) + [-1] * (max(per) - m))
-        at += m
-    shared = dict(prefix_pages=ints(prefix_pages) if prefix else None, prefix_len=len(prefix))
+    own, front_own = ints([0] * n), ints([0])
+    pages, front = (torch.full(size, -1, dtype=torch.int32, device=dev) for size in ((n, max(per)), (1, max(1, n_prefix))))
+    shared = dict(prefix_pages=front[0] if prefix else None, prefix_len=len(prefix))
     if prefix:   # its keys and values, once for everybody
-        dec.forward(ints(prefix), Batch(ints([0, len(prefix)]), ints([len(prefix)]), ints([prefix_pages]), len(prefix),
-                                        len(prefix), len(prefix)), rows=slice(-1, None))
-    ends = torch.tensor(lens).cumsum(0).tolist()
-    pages = ints(table)
-    prompt = Batch(ints([0] + ends), ints(lens), pages, ends[-1], max(lens), max(lens), **shared)
-    own = ints(lens)
-    step = Batch(torch.arange(n + 1, dtype=torch.int32, device=dev), own, pages, n, 1, max(lens) + n_new, **shared)
+        at = dec.pool.step(front_own, ints([len(prefix)]), front, len(prefix))
+        dec.forward(ints(prefix), Batch(at.token_start, at.own_len, front, len(prefix), len(prefix), len(prefix)), rows=slice(-1, None))
+    ends, ones = torch.tensor(lens).cumsum(0).tolist(), ints([1] * n)
+
+    def batch_of(new, tokens, max_new, max_own):
+        at = dec.pool.step(own, new, pages, tokens, prefix_len=len(prefix))
+        return Batch(at.token_start, own, pages, tokens, max_new, max_own, **shared)
+
     last = ints([e - 1 for e in ends]).long()
     u_now, tokens, out, logits = u[0].clone(), torch.empty(n, dtype=torch.int32, device=dev), [], []
+    adjust.update(repetition=repetition, frequency=frequency, presence=presence)
+    if any(x is not None for x in (repetition, frequency, presence)):
+        # each request's tokens so far, the answer's behind the prompt's
+        width = len(prefix) + max(lens) + n_new
+        adjust["history"] = ints([list(prefix) + p + [-1] * (width - len(prefix) - len(p)) for p in prompts])
+        adjust["prompt_len"] = ints([len(prefix) + m for m in lens])
+        adjust["history_len"] = adjust["prompt_len"].clone()
 
     def choose(z):
+        if any(x is not None for x in adjust.values()):
+            adjust_logits(z, **adjust, out=z)
         tokens.copy_(sample(z, u_now, temperature, top_k, top_p, min_p))
+        if "history" in adjust:
+            adjust["history"].scatter_(1, adjust["history_len"].long()[:, None], tokens[:, None])
+            adjust["history_len"].add_(1)
         return z
 
     def decode():
-        own.add_(1)
-        return choose(dec.forward(tokens, step))
+        return choose(dec.forward(tokens, batch_of(ones, n, 1, max(lens) + n_new)))
 
-    z, replay = choose(dec.forward(ints([t for p in prompts for t in p]), prompt, rows=last)), None
+    z = dec.forward(ints([t for p in prompts for t in p]), batch_of(ints(lens), ends[-1], max(lens), max(lens)), rows=last)
+    z, replay = choose(z), None
     for i in range(n_new):
         if i > 0:
             u_now.copy_(u[i])
@@ -148,6 +172,10 @@ def generate(dec: Decoder, prefix, prompts, n_new, u, temperature=None, top_k=No
             replay = torch.cuda.CUDAGraph()
             with torch.cuda.graph(replay):
                 z = decode()
+    # the pages go back
+    dec.pool.step(own, ones - 1, pages, 1, done=ones)
+    if prefix:
+        dec.pool.step(front_own, ones[:1] - 1, front, 1, done=ones[:1])
     return (torch.stack(out), torch.stack(logits)) if keep_logits else torch.stack(out)
 
 
@@ -159,8 +187,12 @@ def main(argv=None):
     ap.add_argument("--prompt", type=int, default=100, help="the longest prompt")
     ap.add_argument("--new", type=int, default=64, help="tokens to generate per request")
     ap.add_argument("--layers", type=int, default=4)
+    ap.add_argument("--qk-norm", action="store_true", help="norms of the heads of queries and keys")
+    ap.add_argument("--window", type=int, default=0, help="positions that a token sees (0: all)")
+    ap.add_argument("--sinks", type=int, default=0, help="first positions that stay visible beside a window")
+    ap.add_argument("--repetition", type=float, default=None, help="penalty for tokens that repeat")
     a = ap.parse_args(argv)
-    shape = Shape(layers=a.layers)
+    shape = Shape(layers=a.layers, qk_norm=a.qk_norm, window=a.window, sinks=a.sinks)
     g = torch.Generator().manual_seed(1)
     draw = lambda m: torch.randint(shape.vocab, (m,), generator=g).tolist()
     prefix = draw(a.prefix)
@@ -170,6 +202,8 @@ def main(argv=None):
     u = torch.rand((a.new, a.batch), generator=g).cuda()
     col = lambda x, dtype=torch.float32: torch.full((a.batch,), x, dtype=dtype, device="cuda")
     settings = dict(temperature=col(0.8), top_k=col(50, torch.int32), top_p=col(0.95))
+    if a.repetition is not None:
+        settings["repetition"] = col(a.repetition)
     seconds = []
     for _ in range(2):   # (the first run also loads the kernels)
         torch.cuda.synchronize()
