@@ -54,7 +54,7 @@ struct AttendParams {
 // to the last key.  They are tiles 0 .. a - 1 and those from a + skip on.
 struct Line {
   int a, skip, tiles;
-  __device__ int tile(int i) const { return i < a ? i : i + skip; }
+  __device__ int tile(int i) const volatile { return i < a ? i : i + skip; }
 };
 template <int K>
 __device__ __forceinline__ Line line_of(const AttendParams& p, int keys, int base, int first) {

@@ -2,7 +2,7 @@
 // (prompts, and a batch's rows against the shared prefix).
 #include <algorithm>
 
-#include "attention.cuh"
+#include "attention_wide.cuh"
 
 namespace sdq {
 
@@ -38,72 +38,6 @@ namespace {
 // us.
 // Registers: 384 threads hold 168 each at launch; the first two warpgroups go
 // to 224 once the third has gone down to 56 (224 + 224 + 56 = 3 x 168).
-constexpr int kWideThreads = 384;
-constexpr int kKeys = 128;             // of a tile
-constexpr int kSub = 64;               // keys of one P
-constexpr int kHalf = kKeys * 128;     // bytes: 128 rows x 64 elements
-
-template <int D> struct WideShape {
-  static constexpr int kMat = (D / 64) * kHalf;              // 128 rows of Q, K or V
-  static constexpr int kRing = D == 128 ? 5 : 8;
-  static constexpr int kSmem = 1024 + (2 + kRing) * kMat;
-  static_assert(256 * D * 4 <= (2 + kRing) * kMat, "256 fp32 rows fit over the operands");
-};
-
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-      : "r"(taddr));
-}
-
-// Two fp32 in a 64-bit register, and arithmetic on both at once.
-__device__ __forceinline__ uint64_t pair_of(float a, float b) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};\n" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ void unpair(uint64_t p, float& a, float& b) {
-  asm("mov.b64 {%0, %1}, %2;\n" : "=f"(a), "=f"(b) : "l"(p));
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;\n" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("mul.rn.f32x2 %0, %1, %2;\n" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("max.f32 %0, %1, %2, %3;\n" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-  return r;
-}
-
-// Operand with its second dimension contiguous (V: keys x 64 elements per
-// 128-byte row, 128-byte swizzle): 8-key groups 1024 bytes apart, the next 64
-// elements kHalf bytes on.
-__device__ __forceinline__ uint64_t sw128_mn_desc(uint32_t saddr) {
-  uint64_t d = 0;
-  d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
-  d |= (uint64_t)(kHalf >> 4) << 16;
-  d |= (uint64_t)(1024 >> 4) << 32;
-  d |= (uint64_t)1 << 46;
-  d |= (uint64_t)2 << 61;
-  return d;
-}
-
 // What a thread block works on.
 struct WideItem {
   int first, rows, r0;       // first token, rows of the (sequence, head) or of the batch, first row of the block
@@ -113,17 +47,8 @@ struct WideItem {
   int prefix_tiles, t0, t1;  // of the line: the prefix's tiles, this block's [t0, t1)
 };
 
-// With a window the line is of 64-key pieces, two to a tile, so that what is
-// left out, first keys apart from the window, and the ends cost half a tile
-// at most: which of the prefix's and of the own pieces, and how many.
-struct WideLine {
-  Line prefix, own;
-  int pieces;
-};
-
 // (a whole warp; false: nothing to do)
-template <bool kWindow>
-__device__ __forceinline__ bool wide_item(const AttendParams& p, int part, WideItem* w, WideLine* line) {
+__device__ __forceinline__ bool wide_item(const AttendParams& p, int part, WideItem* w) {
   const int splits = p.splits[part];
   const int id = blockIdx.x / (p.kv_heads * splits), rest = blockIdx.x % (p.kv_heads * splits);
   w->h = rest / splits;
@@ -171,16 +96,7 @@ __device__ __forceinline__ bool wide_item(const AttendParams& p, int part, WideI
     w->r0 = rb * 256;
     w->prefix_tiles = p.chained ? ptiles : 0;
     const int last = min(w->rows, w->r0 + 256) - 1;   // its last row sees the most
-    const int keys = max(0, q.own - q.count + last / p.group + 1);
-    if (kWindow) {
-      const int first = position_of(p, q.own - q.count + w->r0 / p.group);
-      line->prefix = line_of<kSub>(p, p.b.prefix_len, 0, first);
-      line->own = line_of<kSub>(p, keys, p.b.prefix_len, first);
-      line->pieces = line->prefix.tiles + line->own.tiles;
-      tiles = (line->pieces + 1) / 2;
-    } else {
-      tiles = w->prefix_tiles + (keys + kKeys - 1) / kKeys;
-    }
+    tiles = w->prefix_tiles + (max(0, q.own - q.count + last / p.group + 1) + kKeys - 1) / kKeys;
   }
   const int per = (tiles + splits - 1) / splits;
   w->t0 = min(tiles, w->split * per);
@@ -188,7 +104,7 @@ __device__ __forceinline__ bool wide_item(const AttendParams& p, int part, WideI
   return true;
 }
 
-template <int D, bool kWindow>
+template <int D>
 __global__ void __launch_bounds__(kWideThreads, 1)
     wide_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const AttendParams p,
                 const int part) {
@@ -197,7 +113,6 @@ __global__ void __launch_bounds__(kWideThreads, 1)
   __shared__ __align__(8) uint64_t full[S::kRing], empty[S::kRing], q_full, s_full[2], p_full[2][2], pv_done[2], mma_done;
   __shared__ uint32_t tmem_base;
   __shared__ volatile int tainted;   // a value that is not finite was taken out
-  __shared__ WideLine line_s;        // (read where it is needed: the softmax has no registers to spare)
   const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
   const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t ring = sbase + 2 * S::kMat;
@@ -228,8 +143,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
   pdl_launch_dependents();
   call_record_start(p.rec, p.call, blockIdx.x == 0 && tid == 0);
   WideItem w;
-  WideLine line_r;
-  if (!wide_item<kWindow>(p, part, &w, &line_r)) {   // (all warps alike)
+  if (!wide_item(p, part, &w)) {   // (all warps alike)
     if (warp == 8) tmem_dealloc(tmem_base, 512);
     return;
   }
@@ -238,28 +152,6 @@ __global__ void __launch_bounds__(kWideThreads, 1)
   const bool joins = p.splits[part] > 1 || p.parts > 1;
   const uint32_t tmem = tmem_base;
   bool ok = true;
-  if (kWindow) {
-    if (tid == 0) line_s = line_r;
-    __syncthreads();
-  }
-  const volatile WideLine& line = line_s;
-  // pieces of 64 keys that this thread block takes; of piece q: is it the prefix's, its first key
-  const int n_pieces = kWindow ? min(2 * n, line_r.pieces - 2 * w.t0) : 2 * n;
-  struct Piece {
-    bool pre;
-    int k0;
-  };
-  auto piece_at = [&](int q) {
-    const int c = 2 * w.t0 + q;
-    if (kWindow) {
-      const int np = line.prefix.tiles, i = c - np;
-      if (i < 0) return Piece{true, (c < line.prefix.a ? c : c + line.prefix.skip) * kSub};
-      return Piece{false, (i < line.own.a ? i : i + line.own.skip) * kSub};
-    }
-    const int t = c >> 1;
-    const bool pre = t < w.prefix_tiles;
-    return Piece{pre, (pre ? t : t - w.prefix_tiles) * kKeys + kSub * (c & 1)};
-  };
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;\n");
     if (warp == 9) {
@@ -277,24 +169,10 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         // (a page outside the cache: rows outside the arrays, which read as zeros)
         return pg >= 0 && pg < p.n_pages ? ((pg * p.kv_heads + w.h) << p.page_shift) + ((at & (per_page - 1)) << p.box_shift) : -box;
       };
-      // with a window, of the lane's box in its piece: is it one (not past the last key), its rows
-      auto window_row = [&](int t, bool* is) {
-        const int q = 2 * (t - w.t0) + lane / (per_tile / 2);
-        *is = false;
-        if (lane >= per_tile || q >= n_pieces) return -box;
-        const Piece c = piece_at(q);
-        const int at = (c.k0 >> p.box_shift) + lane % (per_tile / 2);
-        *is = at < (((c.pre ? p.b.prefix_len : w.own) + box - 1) >> p.box_shift);
-        const int pg = *is ? __ldg((c.pre ? p.b.prefix_pages : own_table) + at / per_page) : -1;
-        return pg >= 0 && pg < p.n_pages ? ((pg * p.kv_heads + w.h) << p.page_shift) + ((at & (per_page - 1)) << p.box_shift) : -box;
-      };
-      bool is_next = false;
-      int y_next = kWindow ? window_row(w.t0, &is_next) : row_of(w.t0), slot = 0;
+      int y_next = row_of(w.t0), slot = 0;
       for (int t = w.t0; t < w.t1 && ok; ++t) {
-        const int y = y_next;
-        const uint32_t boxes = kWindow ? __ballot_sync(0xffffffffu, is_next) : 0;
-        const int nb = kWindow ? __popc(boxes) : boxes_of(t);
-        y_next = kWindow ? window_row(t + 1, &is_next) : row_of(t + 1);
+        const int y = y_next, nb = boxes_of(t);
+        y_next = row_of(t + 1);
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv, ++slot) {
           const int st = slot % S::kRing, r = slot / S::kRing;
@@ -303,10 +181,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
             break;
           }
           mbar_expect_tx_warp(&full[st], (uint32_t)((nb << p.box_shift) * 128 * (D / 64)));
-          uint32_t left = boxes;
-          for (int k = 0; k < nb; ++k) {
-            const int i = kWindow ? __ffs(left) - 1 : k;
-            left &= left - 1;
+          for (int i = 0; i < nb; ++i) {
             const int yi = __shfl_sync(0xffffffffu, y, i);
 #pragma unroll
             for (int half = 0; half < D / 64; ++half)
@@ -344,7 +219,6 @@ __global__ void __launch_bounds__(kWideThreads, 1)
           for (int half = 0; half < halves && ok; ++half) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-              if (kWindow && 2 * i + j >= n_pieces) break;   // (the last tile may have one piece)
               if (ok) ok = mbar_wait_warp(&p_full[half][j], i & 1);
               if (ok && j + half == 0) ok = mbar_wait_warp(&full[vs], ((2 * i + 1) / S::kRing) & 1);
               if (!ok) break;
@@ -401,34 +275,13 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       // finite are taken out of the tile, as zero times them is not zero, and added
       // at the end to the rows that see them
       const int all_rows = max(0, w.own - w.count + w.r0 / p.group + 1);
-      // with a window: the first position of this row's, and of the window of the
-      // last row of its half and of the block (the latest ones)
-      const int last = min(w.rows, w.r0 + 256) - 1;
-      auto low_of = [&](int r) { return position_of(p, w.own - w.count + r / p.group) - p.window + 1; };
-      const int low = kWindow && live ? position_of(p, w.own - w.count + tok) - p.window + 1 : 0;
-      const int low_half = kWindow ? low_of(min(last, w.r0 + 128 * half + 127)) : 0, low_rows = kWindow ? low_of(last) : 0;
-      // do 64 keys from k0 of the prefix's or own ones hold some that not all rows of the block see?
-      auto partial = [&](bool pre, int k0) {
-        const int keys = pre ? p.b.prefix_len : w.own, base = pre ? 0 : p.b.prefix_len;
-        return k0 + kSub > (pre ? keys : min(keys, all_rows)) || (kWindow && k0 < low_rows - base && k0 + kSub > p.sinks - base);
-      };
       const uint32_t ts = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + 128 * half;
       const uint32_t to = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + 256 + D * half;
-      // does piece q need a look at what its keys are?  (Of both pieces of a tile before its scores are waited for:
-      // between the scores and the weights every instruction counts)
-      auto edge_of = [&](int q) {
-        const Piece c = piece_at(q);
-        const int base = c.pre ? 0 : p.b.prefix_len;
-        return c.k0 + kSub > (c.pre ? p.b.prefix_len : all) || (c.k0 < low_half - base && c.k0 + kSub > p.sinks - base) ||
-               (half == 0 && partial(c.pre, c.k0));
-      };
-      int edge = 3;
       float m = -INFINITY;        // reference maximum (log2 units)
       uint64_t l2 = 0;            // two sums
       const uint64_t scale2 = pair_of(p.scale, p.scale);
-      for (int q = 0; q < n_pieces; ++q) {
+      for (int q = 0; q < 2 * n; ++q) {
         const int i = q >> 1, j = q & 1;
-        if (kWindow && j == 0) edge = (int)edge_of(q) | (int)edge_of(q + 1) << 1;
         if (j == 0 && !mbar_wait_warp(&s_full[half], i & 1)) {
           ok = false;
           break;
@@ -438,60 +291,49 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         tmem_ld32(ts + kSub * j, x);
         tmem_ld32(ts + kSub * j + 32, x + 32);
         tmem_ld_wait();
-        if (!kWindow || (edge >> j & 1)) {
-          const Piece piece = piece_at(q);
-          const bool pre = piece.pre;
-          const int k0 = piece.k0, keys = pre ? p.b.prefix_len : w.own;
-          if (k0 + kSub > (pre ? keys : all)) {
-            const int see = (pre ? keys : lim) - k0;   // of these 64
+        const int t = w.t0 + i;
+        const bool pre = t < w.prefix_tiles;
+        const int k0 = (pre ? t : t - w.prefix_tiles) * kKeys + kSub * j, keys = pre ? p.b.prefix_len : w.own;
+        if (k0 + kSub > (pre ? keys : all)) {
+          const int see = (pre ? keys : lim) - k0;   // of these 64
 #pragma unroll
-            for (int c = 0; c < kSub; ++c)
-              if (c >= see) x[c] = 0xFF800000u;
+          for (int c = 0; c < kSub; ++c)
+            if (c >= see) x[c] = 0xFF800000u;
+        }
+        if (half == 0 && k0 + kSub > (pre ? keys : min(keys, all_rows))) {
+          // (for both halves: the second's product is issued after the first's)
+          // values past the last key are leftovers (perhaps NaN): zero times them has to be zero too
+          const int vs = (2 * i + 1) % S::kRing, from = 8 * max(0, (pre ? keys : min(keys, all_rows)) - k0);
+          if (!mbar_wait_warp(&full[vs], ((2 * i + 1) / S::kRing) & 1)) {
+            ok = false;
+            break;
           }
-          if (kWindow) {
-            const int base = pre ? 0 : p.b.prefix_len;
-            if (k0 < low_half - base && k0 + kSub > p.sinks - base) {
-              const int from = p.sinks - base - k0, to = low - base - k0;   // of these 64
-#pragma unroll
-              for (int c = 0; c < kSub; ++c)
-                if (c >= from && c < to) x[c] = 0xFF800000u;
-            }
-          }
-          if (half == 0 && partial(pre, k0)) {
-            // (for both halves: the second's product is issued after the first's)
-            // values past the last key are leftovers (perhaps NaN): zero times them has to be zero too
-            const int vs = (2 * i + 1) % S::kRing, from = kWindow ? 0 : 8 * max(0, (pre ? keys : min(keys, all_rows)) - k0);
-            if (!mbar_wait_warp(&full[vs], ((2 * i + 1) / S::kRing) & 1)) {
-              ok = false;
-              break;
-            }
-            const uint32_t at = ring + vs * S::kMat + (kSub * j) * 128;   // 16-byte pieces c of the rows
+          const uint32_t at = ring + vs * S::kMat + (kSub * j) * 128;   // 16-byte pieces c of the rows
 #pragma unroll 1
-            for (int c = from + wtid; c < 8 * kSub; c += 256) {
-              uint4 v[2][D / 64];
+          for (int c = from + wtid; c < 8 * kSub; c += 256) {
+            uint4 v[2][D / 64];
 #pragma unroll
-              for (int k = 0; k < 2; ++k)
+            for (int k = 0; k < 2; ++k)
 #pragma unroll
-                for (int d = 0; d < D / 64; ++d) v[k][d] = ld_shared16(at + d * kHalf + 16 * min(c + 128 * k, 8 * kSub - 1));
-              bool any = false;
+              for (int d = 0; d < D / 64; ++d) v[k][d] = ld_shared16(at + d * kHalf + 16 * min(c + 128 * k, 8 * kSub - 1));
+            bool any = false;
 #pragma unroll
-              for (int k = 0; k < 2; ++k)
+            for (int k = 0; k < 2; ++k)
 #pragma unroll
-                for (int d = 0; d < D / 64; ++d) any |= some_not_finite(v[k][d]);
-              if (!any) continue;
+              for (int d = 0; d < D / 64; ++d) any |= some_not_finite(v[k][d]);
+            if (!any) continue;
 #pragma unroll
-              for (int k = 0; k < 2; ++k)
+            for (int k = 0; k < 2; ++k)
 #pragma unroll
-                for (int d = 0; d < D / 64; ++d) {
-                  const uint4 x = v[k][d];
-                  if (c + 128 * k >= 8 * kSub || !some_not_finite(x)) continue;
-                  if (k0 + ((c + 128 * k) >> 3) < keys) tainted = 1;
-                  st_shared16(at + d * kHalf + 16 * (c + 128 * k), x.x & ~not_finite(x.x), x.y & ~not_finite(x.y), x.z & ~not_finite(x.z),
-                              x.w & ~not_finite(x.w));
-                }
-            }
-            fence_proxy_async_smem();
+              for (int d = 0; d < D / 64; ++d) {
+                const uint4 x = v[k][d];
+                if (c + 128 * k >= 8 * kSub || !some_not_finite(x)) continue;
+                if (k0 + ((c + 128 * k) >> 3) < keys) tainted = 1;
+                st_shared16(at + d * kHalf + 16 * (c + 128 * k), x.x & ~not_finite(x.x), x.y & ~not_finite(x.y), x.z & ~not_finite(x.z),
+                            x.w & ~not_finite(x.w));
+              }
           }
+          fence_proxy_async_smem();
         }
         float mx[4];
 #pragma unroll
@@ -552,10 +394,10 @@ __global__ void __launch_bounds__(kWideThreads, 1)
           uint32_t o[32];
           tmem_ld32(to + 32 * c, o);
           tmem_ld_wait();
-          // element 2 j and 2 j + 1 of these 32 of a key's value
-          auto add_value = [&](const int32_t* table, int key) {
-            const int pg = __ldg(table + (key >> p.page_shift));
-            if (pg < 0 || pg >= p.n_pages) return;
+#pragma unroll 1
+          for (int key = all_rows; live && key < lim; ++key) {
+            const int pg = __ldg(p.b.pages + (int64_t)w.s * p.b.page_stride + (key >> p.page_shift));
+            if (pg < 0 || pg >= p.n_pages) continue;
             const uint32_t* v = reinterpret_cast<const uint32_t*>(
                 p.v + ((((int64_t)pg * p.kv_heads + w.h) << p.page_shift) + (key & ((1 << p.page_shift) - 1))) * D + 32 * c);
 #pragma unroll
@@ -564,23 +406,6 @@ __global__ void __launch_bounds__(kWideThreads, 1)
               if (bad & 0xFFFFu) o[2 * j] = __float_as_uint(__uint_as_float(o[2 * j]) + __uint_as_float(x << 16));
               if (bad >> 16) o[2 * j + 1] = __float_as_uint(__uint_as_float(o[2 * j + 1]) + __uint_as_float(x & 0xFFFF0000u));
             }
-          };
-          const int32_t* own_table = p.b.pages + (int64_t)w.s * p.b.page_stride;
-          if (kWindow) {
-#pragma unroll 1
-            for (int q = 0; live && q < n_pieces; ++q) {
-              const Piece piece = piece_at(q);
-              const bool pre = piece.pre;
-              const int k0 = piece.k0, base = pre ? 0 : p.b.prefix_len;
-              if (!partial(pre, k0)) continue;
-              const int end = min(k0 + kSub, pre ? p.b.prefix_len : lim);
-#pragma unroll 1
-              for (int key = k0; key < end; ++key)
-                if (key >= low - base || key < p.sinks - base) add_value(pre ? p.b.prefix_pages : own_table, key);
-            }
-          } else {
-#pragma unroll 1
-            for (int key = all_rows; live && key < lim; ++key) add_value(own_table, key);
           }
           __syncwarp();
           tmem_st32(to + 32 * c, o);
@@ -682,12 +507,12 @@ int64_t wide_blocks(const sdq_batch* b, int group, int part) {
   return part == kPrefix ? (rows + 255) / 256 : rows / 256 + std::min(b->n_seqs, b->n_tokens);
 }
 
-template <int D, bool kWindow>
+template <int D>
 cudaError_t launch(const sdq_cache_s* c, const AttendParams& p, int part, cudaStream_t st) {
   static std::atomic<int> smem_set[64];
-  const cudaError_t e = smem_limit_once(wide_kernel<D, kWindow>, WideShape<D>::kSmem, c->device, smem_set);
+  const cudaError_t e = smem_limit_once(wide_kernel<D>, WideShape<D>::kSmem, c->device, smem_set);
   if (e != cudaSuccess) return e;
-  return launch_pdl(wide_kernel<D, kWindow>, dim3((unsigned)wide_grid(c, p, part)), dim3(kWideThreads), (size_t)WideShape<D>::kSmem, st, c->kmap,
+  return launch_pdl(wide_kernel<D>, dim3((unsigned)wide_grid(c, p, part)), dim3(kWideThreads), (size_t)WideShape<D>::kSmem, st, c->kmap,
                     c->vmap, p, part);
 }
 
@@ -737,8 +562,8 @@ int wide_splits(const sdq_cache_s* c, const AttendParams& p, int q_heads, int pa
 }
 
 cudaError_t launch_wide(const sdq_cache_s* c, const AttendParams& p, int part, cudaStream_t st) {
-  if (p.window > 0) return c->desc.head_dim == 128 ? launch<128, true>(c, p, part, st) : launch<64, true>(c, p, part, st);
-  return c->desc.head_dim == 128 ? launch<128, false>(c, p, part, st) : launch<64, false>(c, p, part, st);
+  if (p.window > 0) return launch_window(c, p, wide_grid(c, p, part), st);
+  return c->desc.head_dim == 128 ? launch<128>(c, p, part, st) : launch<64>(c, p, part, st);
 }
 
 }  // namespace sdq
