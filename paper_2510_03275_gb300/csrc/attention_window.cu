@@ -17,13 +17,22 @@ namespace {
 // ends run beside each other:
 //   warp 10         looks the next item up, into one of two places
 //   warp 9          streams the keys and values of item after item
-//   warps 0-3, 4-7  copy the next item's queries over the last ones' as soon as
-//                   the last scores are there, ahead of their softmax
+//   warp 11         looks at the values of keys that not all rows see, and passes
+//                   every tile of values on
 //   warp 8          starts the next scores behind the last product of an item,
 //                   while its output is still being written
+//   warps 0-3, 4-7  rows 0-127, 128-255: softmax and output; they copy the next
+//                   item's queries over the last ones' as soon as the last scores are
+//                   there, ahead of their softmax (by one warp beside them: 2.5 us an
+//                   item more)
 // An item's line is of 64-key pieces, two to a tile, so that what is left out,
 // first keys apart from the window, and the ends cost half a tile at most.
 constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;   // 2 x 216 + 72 = 3 x 168, the registers at launch
+
+// Stages of keys and of values (apart, so that whoever waits for the values has
+// waited for every use of a stage before).
+template <int D> constexpr int kStagesK = WideShape<D>::kRing / 2;
+template <int D> constexpr int kStagesV = WideShape<D>::kRing - kStagesK<D>;
 
 struct Item {
   int valid;                 // 0: there are no more
@@ -31,6 +40,7 @@ struct Item {
   int h, split, s;           // key head, share, sequence
   int own, count;            // its own tokens and new tokens
   int piece, n, n_pieces;    // first piece of the line, tiles and pieces from there on
+  int all_rows, low_rows;    // own keys that every row of the block sees, the first position that all of their windows have
   Line prefix, mine;         // which pieces of the prefix's and of the own keys the line holds
 };
 // Piece q of an item: is it the prefix's, its first key.
@@ -42,6 +52,14 @@ __device__ __forceinline__ Piece piece_at(const volatile Item& w, int q) {
   const int c = w.piece + q, i = c - w.prefix.tiles;
   if (i < 0) return Piece{true, w.prefix.tile(c) * kSub};
   return Piece{false, w.mine.tile(i) * kSub};
+}
+
+// Does a piece hold keys that not all rows of the block see?  Values there that
+// are not finite are taken out of the tile, as zero times them is not zero, and
+// added at the end to the rows that see them.
+__device__ __forceinline__ bool partial(const AttendParams& p, const volatile Item& w, const Piece& c) {
+  const int keys = c.pre ? p.b.prefix_len : min(w.own, w.all_rows), base = c.pre ? 0 : p.b.prefix_len;
+  return c.k0 + kSub > keys || (c.k0 < w.low_rows - base && c.k0 + kSub > p.sinks - base);
 }
 
 // Item `id` (a whole warp; lane 0's is written).  at, before: the 32 sequences
@@ -86,6 +104,8 @@ __device__ __forceinline__ bool find_item(const AttendParams& p, int64_t id, int
     w.piece = 2 * t0;
     w.n = t1 - t0;
     w.n_pieces = max(0, min(2 * w.n, pieces - 2 * t0));
+    w.all_rows = max(0, x.own - x.count + w.r0 / p.group + 1);
+    w.low_rows = position_of(p, x.own - x.count + last / p.group) - p.window + 1;
     *out = w;
     return true;
   }
@@ -98,19 +118,25 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                   const int64_t items) {
   using S = WideShape<D>;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t full[S::kRing], empty[S::kRing], q_full[2], s_full[2], p_full[2][2], pv_done[2], o_full[2], o_free[2],
+  constexpr int NK = kStagesK<D>, NV = kStagesV<D>;
+  __shared__ __align__(8) uint64_t full_k[NK], empty_k[NK], full_v[NV], clean[NV], empty_v[NV], q_full[2], s_full[2], p_full[2][2], pv_done[2], o_full[2], o_free[2],
       item_full[2], item_empty[2], mma_done;
   __shared__ uint32_t tmem_base;
   __shared__ Item item_s[2];
   __shared__ volatile int tainted[2];   // 1 + the item that a value that is not finite was taken out of
   const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
   const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const uint32_t ring = sbase + 2 * S::kMat;
-  uint8_t* ring_ptr = smem_raw + (ring - smem_u32(smem_raw));
+  const uint32_t k_ring = sbase + 2 * S::kMat, v_ring = k_ring + NK * S::kMat;
+  uint8_t* ring_ptr = smem_raw + (k_ring - smem_u32(smem_raw));
   if (tid == 0) {
-    for (int i = 0; i < S::kRing; ++i) {
-      mbar_init(&full[i], 1);
-      mbar_init(&empty[i], 1);
+    for (int i = 0; i < NK; ++i) {
+      mbar_init(&full_k[i], 1);
+      mbar_init(&empty_k[i], 1);
+    }
+    for (int i = 0; i < NV; ++i) {
+      mbar_init(&full_v[i], 1);
+      mbar_init(&clean[i], 1);
+      mbar_init(&empty_v[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&q_full[i], 128);
@@ -120,7 +146,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       mbar_init(&o_full[i], 1);
       mbar_init(&o_free[i], 128);
       mbar_init(&item_full[i], 1);
-      mbar_init(&item_empty[i], 10);
+      mbar_init(&item_empty[i], 11);
       tainted[i] = 0;
     }
     mbar_init(&mma_done, 1);
@@ -161,10 +187,60 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         if (lane == 0) mbar_arrive(&item_full[it & 1]);
         if (!is) break;
       }
+    } else if (warp == 11) {
+      // ------------------------------------------------------------ values
+      for (int it = 0, tile = 0; ok; ++it) {   // tile: of all items so far
+        if (!item_ready(it)) {
+          ok = false;
+          break;
+        }
+        const volatile Item& w = item_s[it & 1];
+        if (!w.valid) break;
+        const int n = w.n, n_pieces = w.n_pieces;
+        for (int i = 0; i < n && ok; ++i, ++tile) {
+          const int vs = tile % NV;
+          int look = 0;
+          for (int j = 0; j < 2; ++j)
+            if (2 * i + j < n_pieces && partial(p, w, piece_at(w, 2 * i + j))) look |= 1 << j;
+          ok = mbar_wait_warp(&full_v[vs], (tile / NV) & 1);
+          if (!ok) break;
+          for (int j = 0; j < 2; ++j) {
+            if (!(look >> j & 1)) continue;
+            const Piece c = piece_at(w, 2 * i + j);
+            const int keys = c.pre ? p.b.prefix_len : w.own;
+            const uint32_t at = v_ring + vs * S::kMat + (kSub * j) * 128;   // 16-byte pieces of the rows
+            constexpr int kAhead = 8;
+#pragma unroll 1
+            for (int b = lane; b < 8 * kSub * (D / 64); b += 32 * kAhead) {
+              uint4 v[kAhead];
+              bool any = false;
+#pragma unroll
+              for (int k = 0; k < kAhead; ++k) {
+                const int e = b + 32 * k;
+                v[k] = ld_shared16(at + (e / (8 * kSub)) * kHalf + 16 * (e % (8 * kSub)));
+                any |= some_not_finite(v[k]);
+              }
+              if (!any) continue;
+#pragma unroll
+              for (int k = 0; k < kAhead; ++k) {
+                if (!some_not_finite(v[k])) continue;
+                const int e = b + 32 * k;
+                if (c.k0 + ((e % (8 * kSub)) >> 3) < keys) tainted[it & 1] = it + 1;
+                st_shared16(at + (e / (8 * kSub)) * kHalf + 16 * (e % (8 * kSub)), v[k].x & ~not_finite(v[k].x), v[k].y & ~not_finite(v[k].y),
+                            v[k].z & ~not_finite(v[k].z), v[k].w & ~not_finite(v[k].w));
+              }
+            }
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&clean[vs]);
+        }
+        item_done(it);
+      }
     } else if (warp == 9) {
       // ------------------------------------------------------------ loads
       const int box = 1 << p.box_shift, per_page = 1 << (p.page_shift - p.box_shift), per_piece = kSub >> p.box_shift;
-      int slot = 0;
+      int tile = 0, issued_k = 0, issued_v = 0;   // of all items so far
       for (int it = 0; ok; ++it) {
         if (!item_ready(it)) {
           ok = false;
@@ -188,38 +264,42 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         };
         bool is_next = false;
         int y_next = row_of(0, &is_next);
-        for (int t = 0; t < n && ok; ++t) {
+        for (int t = 0; t < n && ok; ++t, ++tile) {
           const int y = y_next;
           const uint32_t boxes = __ballot_sync(0xffffffffu, is_next);
           y_next = row_of(t + 1, &is_next);
 #pragma unroll
-          for (int kv = 0; kv < 2; ++kv, ++slot) {
-            const int st = slot % S::kRing, r = slot / S::kRing;
-            if (r > 0 && !mbar_wait_warp(&empty[st], (r - 1) & 1)) {
+          for (int kv = 0; kv < 2; ++kv) {
+            const int stages = kv ? NV : NK, st = tile % stages, r = tile / stages;
+            uint64_t* bar = (kv ? full_v : full_k) + st;
+            if (r > 0 && !mbar_wait_warp((kv ? empty_v : empty_k) + st, (r - 1) & 1)) {
               ok = false;
               break;
             }
-            mbar_expect_tx_warp(&full[st], (uint32_t)((__popc(boxes) << p.box_shift) * 128 * (D / 64)));
+            mbar_expect_tx_warp(bar, (uint32_t)((__popc(boxes) << p.box_shift) * 128 * (D / 64)));
+            (kv ? issued_v : issued_k) = tile + 1;
             for (uint32_t left = boxes; left; left &= left - 1) {
               const int i = __ffs(left) - 1, yi = __shfl_sync(0xffffffffu, y, i);
 #pragma unroll
               for (int half = 0; half < D / 64; ++half)
-                tma_load_2d_warp(ring_ptr + st * S::kMat + half * kHalf + ((i * box) << 7), kv ? &vmap : &kmap, 64 * half, yi, &full[st]);
+                tma_load_2d_warp(ring_ptr + ((kv ? NK : 0) + st) * S::kMat + half * kHalf + ((i * box) << 7), kv ? &vmap : &kmap, 64 * half, yi, bar);
             }
           }
         }
         item_done(it);
       }
       // the copies in flight have landed before the thread block ends
-      for (int j = max(0, slot - S::kRing); j < slot; ++j)
-        if (!mbar_wait_warp(&full[j % S::kRing], (j / S::kRing) & 1)) ok = false;
+      for (int j = max(0, issued_k - NK); j < issued_k; ++j)
+        if (!mbar_wait_warp(&full_k[j % NK], (j / NK) & 1)) ok = false;
+      for (int j = max(0, issued_v - NV); j < issued_v; ++j)
+        if (!mbar_wait_warp(&full_v[j % NV], (j / NV) & 1)) ok = false;
     } else if (warp == 8) {
       // --------------------------------------------------------- products
       constexpr uint32_t kF32Bf16 = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(128 >> 4) << 24);   // M = 128
       constexpr uint32_t qk_idesc = kF32Bf16 | ((uint32_t)(kKeys >> 3) << 17);
       constexpr uint32_t pv_idesc = kF32Bf16 | ((uint32_t)(D >> 3) << 17) | (1u << 16);   // B with its N contiguous
       auto scores = [&](int half, int st) {
-        const uint64_t a = sw128_desc(sbase + half * S::kMat), b = sw128_desc(ring + st * S::kMat);
+        const uint64_t a = sw128_desc(sbase + half * S::kMat), b = sw128_desc(k_ring + st * S::kMat);
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
           const uint64_t off = (uint64_t)((k >> 2) * (kHalf >> 4) + 2 * (k & 3));
@@ -227,8 +307,8 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         }
         umma_commit_warp(&s_full[half]);
       };
-      auto ready = [&](int slot) { return mbar_wait_warp(&full[slot % S::kRing], (slot / S::kRing) & 1); };
-      int slot = 0, tiles[2] = {0, 0}, blocks[2] = {0, 0};   // of all items so far; of a half: tiles, items with tiles
+      auto keys_there = [&](int t) { return mbar_wait_warp(&full_k[t % NK], (t / NK) & 1); };
+      int tile = 0, tiles[2] = {0, 0}, blocks[2] = {0, 0};   // of all items so far; of a half: tiles, items with tiles
       for (int it = 0; ok; ++it) {
         if (!item_ready(it)) {
           ok = false;
@@ -239,23 +319,23 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         const int n = w.n, n_pieces = w.n_pieces, halves = w.rows - w.r0 > 128 ? 2 : 1;
         if (n > 0) {
           for (int half = 0; half < halves && ok; ++half) ok = mbar_wait_warp(&q_full[half], blocks[half] & 1);
-          if (ok) ok = ready(slot);
+          if (ok) ok = keys_there(tile);
           if (!ok) break;
           tc_fence_after();
-          for (int half = 0; half < halves; ++half) scores(half, slot % S::kRing);
-          umma_commit_warp(&empty[slot % S::kRing]);
+          for (int half = 0; half < halves; ++half) scores(half, tile % NK);
+          umma_commit_warp(&empty_k[tile % NK]);
           for (int i = 0; i < n && ok; ++i) {
-            const int kn = slot + 2 * i + 2, vn = slot + 2 * i + 1, vs = vn % S::kRing, ks = kn % S::kRing;
+            const int t = tile + i, vs = t % NV, ks = (t + 1) % NK;
             for (int half = 0; half < halves && ok; ++half) {
               // (the output of the item before has been read)
               if (i == 0 && blocks[half] > 0) ok = mbar_wait_warp(&o_free[half], (blocks[half] - 1) & 1);
 #pragma unroll
               for (int j = 0; j < 2; ++j) {
                 if (ok) ok = mbar_wait_warp(&p_full[half][j], (tiles[half] + i) & 1);
-                if (ok && j + half == 0) ok = ready(vn);
+                if (ok && j + half == 0) ok = mbar_wait_warp(&clean[vs], (t / NV) & 1);
                 if (!ok) break;
                 tc_fence_after();
-                const uint64_t b = sw128_mn_desc(ring + vs * S::kMat + j * (kSub * 128));
+                const uint64_t b = sw128_mn_desc(v_ring + vs * S::kMat + j * (kSub * 128));
                 if (2 * i + j < n_pieces)   // (the last tile may have one piece)
 #pragma unroll
                   for (int k = 0; k < kSub / 16; ++k)
@@ -264,19 +344,19 @@ __global__ void __launch_bounds__(kWideThreads, 1)
                 if (j == 0) umma_commit_warp(&pv_done[half]);
               }
               if (!ok) break;
-              if (half == halves - 1) umma_commit_warp(&empty[vs]);
+              if (half == halves - 1) umma_commit_warp(&empty_v[vs]);
               if (i + 1 < n) {
-                if (half == 0) ok = ready(kn);
+                if (half == 0) ok = keys_there(t + 1);
                 if (!ok) break;
                 tc_fence_after();
                 scores(half, ks);
-                if (half == halves - 1) umma_commit_warp(&empty[ks]);
+                if (half == halves - 1) umma_commit_warp(&empty_k[ks]);
               } else {
                 umma_commit_warp(&o_full[half]);
               }
             }
           }
-          slot += 2 * n;
+          tile += n;
           for (int half = 0; half < halves; ++half) {
             tiles[half] += n;
             ++blocks[half];
@@ -328,7 +408,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
     };
     ok = load_queries(0);
     queries_there();
-    int slot = 0, tiles = 0, blocks = 0;   // as the products'
+    int tiles = 0, blocks = 0;   // as the products'
     for (int it = 0; ok; ++it) {
       const volatile Item& w = item_s[it & 1];   // (load_queries has waited for it)
       if (!w.valid) break;
@@ -336,35 +416,24 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       if (rows - r0 <= 128 * half) {   // (the second half of a short row block)
         ok = load_queries(it + 1);
         queries_there();
-        slot += 2 * n;
         item_done(it);
         continue;
       }
       const int row = r0 + 128 * half + wtid, tok = row / p.group, g = row - tok * p.group;
       const bool live = row < rows;
       const int own = w.own, behind = own - w.count;   // the place of token 0 of the item's
-      // own keys that this row sees, that every row of its half does, of the block
-      const int lim = live ? behind + tok + 1 : own;
-      const int all = behind + (r0 + 128 * half) / p.group + 1, all_rows = max(0, behind + r0 / p.group + 1);
-      // the first position of this row's window, and of that of the last row of its half and of the block (the latest ones)
-      const int last = min(rows, r0 + 256) - 1;
+      // own keys that this row sees, that every row of its half does
+      const int lim = live ? behind + tok + 1 : own, all = behind + (r0 + 128 * half) / p.group + 1;
+      // the first position of this row's window, and of that of the last row of its half (the latest one)
+      const int last = min(rows, r0 + 128 * half + 128) - 1;
       auto low_of = [&](int t) { return position_of(p, behind + t) - p.window + 1; };
-      const int low = live ? low_of(tok) : 0;
-      const int low_half = low_of(min(last, r0 + 128 * half + 127) / p.group), low_rows = low_of(last / p.group);
-      // does a piece hold keys that not all rows of the block see?  Values there that
-      // are not finite are taken out of the tile, as zero times them is not zero,
-      // and added at the end to the rows that see them
-      auto partial = [&](const Piece& c) {
-        const int keys = c.pre ? p.b.prefix_len : own, base = c.pre ? 0 : p.b.prefix_len;
-        return c.k0 + kSub > (c.pre ? keys : min(keys, all_rows)) || (c.k0 < low_rows - base && c.k0 + kSub > p.sinks - base);
-      };
+      const int low = live ? low_of(tok) : 0, low_half = low_of(last / p.group);
       // does piece q need a look at what its keys are?  (Of both pieces of a tile before its scores are waited for:
       // between the scores and the weights every instruction counts)
       auto edge_of = [&](int q) {
         const Piece c = piece_at(w, q);
         const int base = c.pre ? 0 : p.b.prefix_len;
-        return c.k0 + kSub > (c.pre ? p.b.prefix_len : all) || (c.k0 < low_half - base && c.k0 + kSub > p.sinks - base) ||
-               (half == 0 && partial(c));
+        return c.k0 + kSub > (c.pre ? p.b.prefix_len : all) || (c.k0 < low_half - base && c.k0 + kSub > p.sinks - base);
       };
       int edge = 0;
       float m = -INFINITY;        // reference maximum (log2 units)
@@ -402,38 +471,6 @@ __global__ void __launch_bounds__(kWideThreads, 1)
 #pragma unroll
             for (int k = 0; k < kSub; ++k)
               if (k >= from && k < to_key) x[k] = 0xFF800000u;
-          }
-          if (half == 0 && partial(c)) {
-            // (for both halves: the second's product is issued after the first's)
-            const int vn = slot + 2 * i + 1, vs = vn % S::kRing;
-            ok = mbar_wait_warp(&full[vs], (vn / S::kRing) & 1);
-            if (!ok) break;
-            const uint32_t at = ring + vs * S::kMat + (kSub * j) * 128;   // 16-byte pieces of the rows
-#pragma unroll 1
-            for (int b = wtid; b < 8 * kSub; b += 256) {
-              uint4 v[2][D / 64];
-#pragma unroll
-              for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int d = 0; d < D / 64; ++d) v[k][d] = ld_shared16(at + d * kHalf + 16 * (b + 128 * k));
-              bool any = false;
-#pragma unroll
-              for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int d = 0; d < D / 64; ++d) any |= some_not_finite(v[k][d]);
-              if (!any) continue;
-#pragma unroll
-              for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int d = 0; d < D / 64; ++d) {
-                  const uint4 y = v[k][d];
-                  if (!some_not_finite(y)) continue;
-                  if (k0 + ((b + 128 * k) >> 3) < keys) tainted[it & 1] = it + 1;
-                  st_shared16(at + d * kHalf + 16 * (b + 128 * k), y.x & ~not_finite(y.x), y.y & ~not_finite(y.y), y.z & ~not_finite(y.z),
-                              y.w & ~not_finite(y.w));
-                }
-            }
-            fence_proxy_async_smem();
           }
         }
         float mx[4];
@@ -515,7 +552,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
 #pragma unroll 1
           for (int q = 0; q < n_pieces; ++q) {
             const Piece pc = piece_at(w, q);
-            if (!partial(pc)) continue;
+            if (!partial(p, w, pc)) continue;
             const int base = pc.pre ? 0 : p.b.prefix_len, end = min(pc.k0 + kSub, pc.pre ? p.b.prefix_len : lim);
             const int32_t* table = pc.pre ? p.b.prefix_pages : p.b.pages + (int64_t)w.s * p.b.page_stride;
 #pragma unroll 1
@@ -556,7 +593,6 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       }
       if (live && split) p.split_ml[kOwn][place] = make_float2(l == l ? m : l, l);   // (NaN scores leave no maximum)
       if (live && !split && p.lse) p.lse[at] = natural_lse(m, l);
-      slot += 2 * n;
       if (n > 0) {
         tiles += n;
         ++blocks;
