@@ -479,10 +479,15 @@ __global__ void __launch_bounds__(kWideThreads, 1)
 #pragma unroll
         for (int c = 12; c < kSub; c += 2) mx[(c >> 1) & 3] = max3(mx[(c >> 1) & 3], __uint_as_float(x[c]), __uint_as_float(x[c + 1]));
         const float top = max3(mx[0], mx[1], fmaxf(mx[2], mx[3])) * p.scale;
+        // The reference is raised where a row's maximum passes it by more than 2^8,
+        // and then set kAhead above the maximum: the first keys of a window are few
+        // for many rows, and later ones larger.  (Weights and sums are floating:
+        // nothing is lost by a reference that lies higher.)
         const bool grow = top > m + 8.f;   // (also from -inf)
         if (__any_sync(0xffffffffu, grow)) {
-          const float f = grow ? exp2_approx(m - top) : 1.f;
-          if (grow) m = top;
+          constexpr float kAhead = 12.f;
+          const float f = grow ? exp2_approx(m - (top + kAhead)) : 1.f;
+          if (grow) m = top + kAhead;
           l2 = mul2(l2, pair_of(f, f));
           if (q > 0) {   // once the products so far are in O (those of the tiles before are, with this one's S)
             if (j == 1) ok = mbar_wait_warp(&pv_done[half], (tiles + i) & 1);
