@@ -43,13 +43,16 @@ struct Row {
 // e of the row, whose first logit is at place `lead` behind a 16-byte
 // boundary).  Each logit is read and written once: HBM bounds it.  What the
 // history says of the block's tokens is counted in shared memory first (a word
-// per token; whole numbers, so that no order of atomics shows), beside the
-// first loads of the logits, which are under way meanwhile; every block of a
+// per token; whole numbers, so that no order of atomics shows); every block of a
 // row looks through all of its history, 4 tokens a load.  The few tokens
 // with a bias are worked out one by a thread, the list's entries for one token
-// added up in their order, and written behind the others.
+// added up in their order, and written behind the others.  96 x 128255 fp32
+// logits (a copy: 17 us): 34 us, 11 of them for histories of 100 to 32768 tokens
+// (their length, their tokens, the logits: chains of latencies that two thread
+// blocks per SM hide in part; 16-bit counters, for three, gain nothing), 4 for
+// 300 biases, 2 for the grammar; one row of 32000: 3.4.
 template <class T, int kV, bool kInPlace>
-__global__ void __launch_bounds__(kThreads) adjust_kernel(const AdjustParams p) {
+__global__ void __launch_bounds__(kThreads, 2) adjust_kernel(const AdjustParams p) {
   constexpr int kVec = 16 / sizeof(T), kChunk = kThreads * kV * kVec;
   extern __shared__ __align__(16) uint32_t smem[];
   uint32_t* seen = smem;                                    // [kChunk]
@@ -67,54 +70,61 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(const AdjustParams p) 
   pdl_wait();
   pdl_launch_dependents();
   auto whole = [&](int t) { return even && t >= 0 && t + kVec <= p.vocab; };
-  uint4 x[kV];
-  if (!kInPlace) {
-#pragma unroll
-    for (int v = 0; v < kV; ++v) {
-      const int t = t0 + (v * kThreads + tid) * kVec;
-      if (whole(t)) x[v] = __ldg(reinterpret_cast<const uint4*>(in + t));
-    }
-  }
+  // what the block waits for first, all of it under way at once
+  const int set = p.a.allowed ? (p.a.allowed_row ? __ldg(p.a.allowed_row + row) : row) : -1;
+  const int len = !p.a.history || t0 >= t1 ? 0 : p.a.history_len ? min(max(__ldg(p.a.history_len + row), 0), p.a.history_max) : p.a.history_max;
+  const int prompt = p.a.prompt_len ? __ldg(p.a.prompt_len + row) : 0;
   Row r;
   r.repetition = p.a.repetition ? __ldg(p.a.repetition + row) : 1.f;
   r.frequency = p.a.frequency ? __ldg(p.a.frequency + row) : 0.f;
   r.presence = p.a.presence ? __ldg(p.a.presence + row) : 0.f;
-  const int set = p.a.allowed ? (p.a.allowed_row ? __ldg(p.a.allowed_row + row) : row) : -1;
   r.allowed = set >= 0 && set < p.a.n_allowed ? p.a.allowed + set * p.a.allowed_stride : nullptr;
+  // the history: places 0 .. head - 1 lie before a 16-byte boundary, the last ones behind whole pieces
+  const int32_t* h = p.a.history + row * p.a.history_stride;
+  const int head = min(len, (int)(-(reinterpret_cast<uintptr_t>(h) >> 2) & 3u)), pieces = (len - head) / 4;
+  const int4* h4 = reinterpret_cast<const int4*>(h + head);
+  constexpr int kAhead = 4;
+  int4 ids[kAhead];
+  auto load_ids = [&](int i0) {
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) ids[k] = i0 + k * kThreads < pieces ? __ldg(h4 + i0 + k * kThreads) : make_int4(-1, -1, -1, -1);
+  };
+  load_ids(tid);
+  // of this thread's logits, which the grammar allows: kVec bits for each piece
+  uint32_t open = ~0u;
+  static_assert(kV * kVec <= 32, "a word per thread");
+  if (r.allowed) {
+    open = 0;
+    const int last = (p.vocab - 1) >> 5;
+#pragma unroll
+    for (int v = 0; v < kV; ++v) {
+      const int t = t0 + (v * kThreads + tid) * kVec, b = min(max(t, 0) >> 5, last);
+      const uint32_t lo = __ldg(r.allowed + b), hi = __ldg(r.allowed + min(b + 1, last));
+      open |= ((t >= 0 ? __funnelshift_r(lo, hi, t & 31) : lo << (-t & 31)) & ((1u << kVec) - 1)) << (kVec * v);
+    }
+  }
   if (p.a.history) {
     for (int i = tid; i < kChunk / 4; i += kThreads) reinterpret_cast<uint4*>(seen)[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
-    const int len = p.a.history_len ? min(max(__ldg(p.a.history_len + row), 0), p.a.history_max) : p.a.history_max;
-    const int prompt = p.a.prompt_len ? __ldg(p.a.prompt_len + row) : 0;
-    const int32_t* h = p.a.history + row * p.a.history_stride;
-    const uint32_t width = (uint32_t)(t1 - max(t0, 0)), low = (uint32_t)max(t0, 0);
+    const uint32_t width = (uint32_t)max(t1 - max(t0, 0), 0), low = (uint32_t)max(t0, 0);
     auto count = [&](int i, int t) {
       if ((uint32_t)t - low >= width) return;   // (also below 0)
       if (i < prompt) atomicOr(seen + (t - t0), ~kCount);
       else atomicAdd(seen + (t - t0), 1u);
     };
-    // places 0 .. head - 1 lie before a 16-byte boundary, the last ones behind whole pieces
-    const int head = min(len, (int)(-(reinterpret_cast<uintptr_t>(h) >> 2) & 3u)), pieces = (len - head) / 4;
-    if (t0 < t1) {
-      const int4* h4 = reinterpret_cast<const int4*>(h + head);
-      constexpr int kAhead = 4;
-      for (int i0 = tid; i0 < pieces; i0 += kAhead * kThreads) {
-        int4 q[kAhead];
+    for (int i0 = tid; i0 < pieces; i0 += kAhead * kThreads, load_ids(i0)) {
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) q[k] = i0 + k * kThreads < pieces ? __ldg(h4 + i0 + k * kThreads) : make_int4(-1, -1, -1, -1);
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-          const int i = head + 4 * (i0 + k * kThreads);
-          count(i, q[k].x);
-          count(i + 1, q[k].y);
-          count(i + 2, q[k].z);
-          count(i + 3, q[k].w);
-        }
+      for (int k = 0; k < kAhead; ++k) {
+        const int i = head + 4 * (i0 + k * kThreads);
+        count(i, ids[k].x);
+        count(i + 1, ids[k].y);
+        count(i + 2, ids[k].z);
+        count(i + 3, ids[k].w);
       }
-      if (tid < head) count(tid, __ldg(h + tid));
-      const int i = head + 4 * pieces + tid - 4;
-      if (tid >= 4 && i < len) count(i, __ldg(h + i));
     }
+    if (tid < head) count(tid, __ldg(h + tid));
+    const int i = head + 4 * pieces + tid - 4;
+    if (tid >= 4 && i < len) count(i, __ldg(h + i));
   }
   // biases of tokens in this block's range, in the list's order
   int n = 0;
@@ -148,49 +158,58 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(const AdjustParams p) 
     res[e] = r.may(t) ? r.penalized(z, p.a.history ? seen[t - t0] : 0) + sum : -INFINITY;   // (entries of one token: the same)
   }
   if (n > 0) __syncthreads();
+  // (4 pieces of the logits under way at once: held from the kernel's start they
+  // cost registers, and with them thread blocks of an SM)
+  constexpr int kAtOnce = kV < 4 ? kV : 4;
+#pragma unroll 1
+  for (int v0 = 0; v0 < kV; v0 += kAtOnce) {
+    uint4 x[kAtOnce];
+    if (!kInPlace) {
 #pragma unroll
-  for (int v = 0; v < kV; ++v) {
-    const int at = (v * kThreads + tid) * kVec, t = t0 + at;
-    if (t >= t1 || t + kVec <= 0) continue;
-    uint32_t w[kVec], any = 0;
+      for (int v = 0; v < kAtOnce; ++v) {
+        const int t = t0 + ((v0 + v) * kThreads + tid) * kVec;
+        if (whole(t)) x[v] = __ldg(reinterpret_cast<const uint4*>(in + t));
+      }
+    }
 #pragma unroll
-    for (int j = 0; j < kVec; j += 4) {
-      const uint4 q = p.a.history ? *reinterpret_cast<const uint4*>(seen + at + j) : make_uint4(0, 0, 0, 0);
-      w[j] = q.x;
-      w[j + 1] = q.y;
-      w[j + 2] = q.z;
-      w[j + 3] = q.w;
-      any |= q.x | q.y | q.z | q.w;
-    }
-    uint32_t bits = ~0u;
-    if (r.allowed) {
-      const int b = max(t, 0) >> 5, last = (p.vocab - 1) >> 5;
-      const uint32_t lo = __ldg(r.allowed + b), hi = __ldg(r.allowed + min(b + 1, last));
-      bits = t >= 0 ? __funnelshift_r(lo, hi, t & 31) : lo << -t;
-    }
-    const bool all = (~bits & ((1u << kVec) - 1)) == 0;
-    if (kInPlace && any == 0 && all) continue;
-    if (whole(t)) {
-      if (kInPlace) x[v] = *reinterpret_cast<const uint4*>(in + t);
-      if (any != 0 || !all) {
-        T z[kVec];
-        memcpy(z, &x[v], 16);
+    for (int v = 0; v < kAtOnce; ++v) {
+      const int at = ((v0 + v) * kThreads + tid) * kVec, t = t0 + at;
+      if (t >= t1 || t + kVec <= 0) continue;
+      uint32_t w[kVec], any = 0;
+#pragma unroll
+      for (int j = 0; j < kVec; j += 4) {
+        const uint4 q = p.a.history ? *reinterpret_cast<const uint4*>(seen + at + j) : make_uint4(0, 0, 0, 0);
+        w[j] = q.x;
+        w[j + 1] = q.y;
+        w[j + 2] = q.z;
+        w[j + 3] = q.w;
+        any |= q.x | q.y | q.z | q.w;
+      }
+      const uint32_t bits = open >> (kVec * (v0 + v));
+      const bool all = (~bits & ((1u << kVec) - 1)) == 0;
+      if (kInPlace && any == 0 && all) continue;
+      if (whole(t)) {
+        if (kInPlace) x[v] = *reinterpret_cast<const uint4*>(in + t);
+        if (any != 0 || !all) {
+          T z[kVec];
+          memcpy(z, &x[v], 16);
+#pragma unroll
+          for (int j = 0; j < kVec; ++j) {
+            if (w[j]) z[j] = from_float<T>(r.penalized(to_float(z[j]), w[j]));
+            if (!(bits >> j & 1u)) z[j] = from_float<T>(-INFINITY);
+          }
+          memcpy(&x[v], z, 16);
+        }
+        *reinterpret_cast<uint4*>(out + t) = x[v];
+      } else {
 #pragma unroll
         for (int j = 0; j < kVec; ++j) {
-          if (w[j]) z[j] = from_float<T>(r.penalized(to_float(z[j]), w[j]));
-          if (!(bits >> j & 1u)) z[j] = from_float<T>(-INFINITY);
+          if (t + j < 0 || t + j >= p.vocab) continue;
+          T z = in[t + j];
+          if (w[j]) z = from_float<T>(r.penalized(to_float(z), w[j]));
+          if (!(bits >> j & 1u)) z = from_float<T>(-INFINITY);
+          out[t + j] = z;
         }
-        memcpy(&x[v], z, 16);
-      }
-      *reinterpret_cast<uint4*>(out + t) = x[v];
-    } else {
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) {
-        if (t + j < 0 || t + j >= p.vocab) continue;
-        T z = in[t + j];
-        if (w[j]) z = from_float<T>(r.penalized(to_float(z), w[j]));
-        if (!(bits >> j & 1u)) z = from_float<T>(-INFINITY);
-        out[t + j] = z;
       }
     }
   }
