@@ -45,25 +45,35 @@ __device__ __forceinline__ void store4(uint16_t* p, float4 a) {
 }
 
 // A head's elements in a thread's hands (a: 4, b: 4 more), normalised and rotated.
+// Every rounding is written down, so that a token's values do not depend on the
+// kernel, and so on the batch, that it comes with.
+__device__ __forceinline__ float squares(const float4& a, const float4& b) {
+  const float x = __fmaf_rn(a.w, a.w, __fmaf_rn(a.z, a.z, __fmaf_rn(a.y, a.y, __fmul_rn(a.x, a.x))));
+  const float y = __fmaf_rn(b.w, b.w, __fmaf_rn(b.z, b.z, __fmaf_rn(b.y, b.y, __fmul_rn(b.x, b.x))));
+  return __fadd_rn(x, y);
+}
 // (dim: a power of 2, so that its inverse is exact)
 __device__ __forceinline__ void normalise(float4& a, float4& b, float sum_of_squares, int dim, float eps, const float4& wa, const float4& wb) {
-  const float r = rsqrtf(sum_of_squares * (dim == 128 ? 1.f / 128 : 1.f / 64) + eps);
-  a = make_float4(a.x * r * wa.x, a.y * r * wa.y, a.z * r * wa.z, a.w * r * wa.w);
-  b = make_float4(b.x * r * wb.x, b.y * r * wb.y, b.z * r * wb.z, b.w * r * wb.w);
+  const float r = rsqrtf(__fmaf_rn(sum_of_squares, dim == 128 ? 1.f / 128 : 1.f / 64, eps));
+  auto times = [&](const float4& x, const float4& w) {
+    return make_float4(__fmul_rn(__fmul_rn(x.x, r), w.x), __fmul_rn(__fmul_rn(x.y, r), w.y), __fmul_rn(__fmul_rn(x.z, r), w.z),
+                       __fmul_rn(__fmul_rn(x.w, r), w.w));
+  };
+  a = times(a, wa);
+  b = times(b, wb);
 }
 // split: a and b are the pairs' first and second elements; else neighbours are.
 __device__ __forceinline__ void rotate(float4& a, float4& b, const float4& cs, const float4& sn, bool split) {
+  auto first = [](float u, float w, float c, float s) { return __fmaf_rn(u, c, -__fmul_rn(w, s)); };
+  auto second = [](float u, float w, float c, float s) { return __fmaf_rn(w, c, __fmul_rn(u, s)); };
   const float4 x = a, y = b;
   if (split) {
-    a = make_float4(x.x * cs.x - y.x * sn.x, x.y * cs.y - y.y * sn.y, x.z * cs.z - y.z * sn.z, x.w * cs.w - y.w * sn.w);
-    b = make_float4(y.x * cs.x + x.x * sn.x, y.y * cs.y + x.y * sn.y, y.z * cs.z + x.z * sn.z, y.w * cs.w + x.w * sn.w);
+    a = make_float4(first(x.x, y.x, cs.x, sn.x), first(x.y, y.y, cs.y, sn.y), first(x.z, y.z, cs.z, sn.z), first(x.w, y.w, cs.w, sn.w));
+    b = make_float4(second(x.x, y.x, cs.x, sn.x), second(x.y, y.y, cs.y, sn.y), second(x.z, y.z, cs.z, sn.z), second(x.w, y.w, cs.w, sn.w));
   } else {
-    a = make_float4(x.x * cs.x - x.y * sn.x, x.y * cs.x + x.x * sn.x, x.z * cs.y - x.w * sn.y, x.w * cs.y + x.z * sn.y);
-    b = make_float4(y.x * cs.z - y.y * sn.z, y.y * cs.z + y.x * sn.z, y.z * cs.w - y.w * sn.w, y.w * cs.w + y.z * sn.w);
+    a = make_float4(first(x.x, x.y, cs.x, sn.x), second(x.x, x.y, cs.x, sn.x), first(x.z, x.w, cs.y, sn.y), second(x.z, x.w, cs.y, sn.y));
+    b = make_float4(first(y.x, y.y, cs.z, sn.z), second(y.x, y.y, cs.z, sn.z), first(y.z, y.w, cs.w, sn.w), second(y.z, y.w, cs.w, sn.w));
   }
-}
-__device__ __forceinline__ float squares(const float4& a, const float4& b) {
-  return a.x * a.x + a.y * a.y + (a.z * a.z + a.w * a.w) + (b.x * b.x + b.y * b.y + (b.z * b.z + b.w * b.w));
 }
 // Where a token stands: its page (-1: its key and value are not kept), its place
 // among its sequence's tokens, its position.

@@ -70,6 +70,50 @@ def test_append_norm_matches_the_definition(sdq, heads, new, own, prefix, page, 
         assert torch.equal(a.view(torch.int16) * keep, b.view(torch.int16) * keep)
 
 
+@pytest.mark.parametrize("heads", [(64, 8, 128), (12, 12, 64), (20, 1, 128), (5, 1, 64)])
+@pytest.mark.parametrize("kind,norm", [("f32", True), ("bf16", True), ("bf16", False)])
+def test_many_tokens_are_those_of_small_calls(sdq, heads, kind, norm):
+    """The calls of many tokens (pieces streamed through shared memory) give what the calls of few give, bit by bit:
+    several sequences, an empty slot, tokens of nobody between and behind them, a page outside the cache."""
+    import torch
+    hq, hk, dim = heads
+    rng = np.random.default_rng(9)
+    total = -(-26000 // (hq + 2 * hk))
+    cuts = np.sort(rng.choice(np.arange(1, total), 9, replace=False))
+    new = np.diff(np.concatenate([[0], cuts, [total]])).tolist()
+    own = [n + int(rng.integers(0, 40)) for n in new]
+    own[3] = 0
+    c = Case((hq, hk, dim), new, own, 11, 16, seed=2)
+    c.pages[1, 0] = -1
+    x = [torch.from_numpy((10.0 ** rng.uniform(-2, 1, (total, 1)) * rng.standard_normal((total, h * dim))).astype(np.float32)).cuda()
+         for h in (hq, hk, hk)]
+    x = [t if kind == "f32" else t.to(torch.bfloat16) for t in x]
+    weights = sdq.HeadNorm(torch.randn((hq, dim), device="cuda"), torch.randn(dim, device="cuda")) if norm else None
+    rope = sdq.Rope.table(11 + max(own) + 1, dim // 2, interleaved=dim == 64)
+    a, b = c.cache(sdq, torch), c.cache(sdq, torch)
+    got = a.append(c.batch(sdq, torch, max_new=max(new) - 1), *x, rope, norm=weights)
+    i = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    want = torch.empty_like(got)
+    for s, n in enumerate(new):                               # (the bound cuts a sequence's last token off)
+        rows = slice(int(c.start[s]), int(c.start[s + 1]))
+        few = max(1, 20000 // (hq + 2 * hk))
+        for t in range(0, n, few):
+            m = min(few, n - t)
+            part = slice(rows.start + t, rows.start + t + m)
+            kept = min(n, max(new) - 1)
+            # the same places: own tokens up to the part's last one
+            last = own[s] - kept + t + m if own[s] else 0
+            start, keep = [0, m], m
+            if t + m > kept:
+                keep, last = kept - t, own[s]
+                start = [0, keep]
+            batch = sdq.Batch(i(start), i([last]), i(c.pages[s:s + 1].tolist()), m, max(1, keep), max(own), i(c.prefix_pages.tolist()), 11)
+            want[part] = b.append(batch, *(v[part] for v in x), rope, norm=weights)
+    assert torch.equal(a.k_pages.view(torch.int16), b.k_pages.view(torch.int16))
+    assert torch.equal(a.v_pages.view(torch.int16), b.v_pages.view(torch.int16))
+    assert torch.equal(got.view(torch.int16), want.view(torch.int16))
+
+
 def test_without_weights_nothing_changes(sdq):
     import torch
     c = Case((4, 2, 64), [3, 20], [40, 20], 7, 16, seed=3)
