@@ -236,6 +236,17 @@ def _empty(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+def _check_devices(where, first, *others):
+    """Raise unless the tensors (None: left out) are all on the current device, on which the kernels run."""
+    import torch
+    device = first.device
+    for t in others:
+        if t is not None and t.device != device:
+            raise ValueError(f"{where}: tensors on different devices")
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"{where}: the tensors are not on the current device")
+
+
 # ------------------------------------------------------------- C-ABI names
 def sdq_plan_create(desc: LayerDesc, had_signs=None) -> int:
     import numpy as np
@@ -651,6 +662,7 @@ class PagePool:
         (rows, columns), (stride, adjacent) = (pages.shape, pages.stride()) if pages.dim() == 2 else ((-1, 0), (0, 0))
         if rows != n_seqs or pages.dtype is not i32 or not pages.is_cuda or (columns > 1 and adjacent != 1):
             raise ValueError("PagePool.step: pages must be an int32 CUDA tensor (sequences, columns), adjacent in a row")
+        _check_devices("PagePool.step", own_len, new_len, done, pages, self.free, self.n_free)
         if done is not None:
             at_done = done.data_ptr()
         if in_place and n_seqs > 0 and at_own in (at_new, at_done):
@@ -710,14 +722,16 @@ class HeadNorm:
         self.ref = ctypes.addressof(self._c)
         self._checked = None
 
-    def check(self, q_heads: int, kv_heads: int, head_dim: int):
-        """Raise where a weight is not of these heads."""
-        if self._checked == (q_heads, kv_heads, head_dim):
+    def check(self, q_heads: int, kv_heads: int, head_dim: int, device):
+        """Raise where a weight is not of these heads, or not on this device."""
+        if self._checked == (q_heads, kv_heads, head_dim, device):
             return
         for t, heads in zip(self.tensors, (q_heads, kv_heads)):
             if t is not None and tuple(t.shape) not in ((head_dim,), (heads, head_dim)):
                 raise ValueError("HeadNorm: weights are not of head_dim, or heads x head_dim, elements")
-        self._checked = q_heads, kv_heads, head_dim
+            if t is not None and t.device != device:
+                raise ValueError("HeadNorm: weights on another device than the cache")
+        self._checked = q_heads, kv_heads, head_dim, device
 
 
 class KVCache:
@@ -774,7 +788,7 @@ class KVCache:
             _check(lib().sdq_cache_append(self.handle, batch.ref, q_heads, q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
                                           kind, rope.ref, out.data_ptr(), _stream(stream)), "sdq_cache_append")
         else:
-            norm.check(q_heads, d.kv_heads, dim)
+            norm.check(q_heads, d.kv_heads, dim, self.k_pages.device)
             _check(lib().sdq_cache_append_norm(self.handle, batch.ref, q_heads, q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(),
                                                ldv, kind, rope.ref, norm.ref, out.data_ptr(), _stream(stream)),
                    "sdq_cache_append_norm")
@@ -888,6 +902,8 @@ def adjust_logits(logits, history=None, history_len=None, prompt_len=None, repet
         raise ValueError("adjust_logits: allowed_row belongs to allowed")
     if allowed is not None and words < (vocab + 31) // 32:
         raise ValueError("adjust_logits: the sets of allowed have too few words")
+    _check_devices("adjust_logits", logits, history, history_len, prompt_len, repetition, frequency, presence, bias_ids, bias,
+                   allowed, allowed_row, out)
     if out is None:
         out = _empty(shape, logits.dtype, logits.device, stream)
     elif out.shape != shape or out.dtype is not logits.dtype or out.stride()[1] != 1 or not out.is_cuda:

@@ -261,3 +261,49 @@ def test_window_refusals(sdq):
         cache.attend(batch, q, ws=small, window=9)
     assert e.value.status not in (0, -1)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("prefix", [0, 70])
+@pytest.mark.parametrize("bad", [None, np.nan, np.inf])
+def test_many_row_blocks_one_after_another(sdq, prefix, bad):
+    """More row blocks than thread blocks, of all kinds in turn: short and long, one half and two, an odd number of
+    pieces, without a key; a value that is not finite stays in the rows of its sequence that see it."""
+    import torch
+    rng = np.random.default_rng(prefix)
+    new = [int(n) for n in rng.choice([33, 40, 64, 128, 129, 150], 64)]
+    own = [0 if s % 13 == 5 else int(n + rng.choice([0, 0, 1, 30, 200, 400])) for s, n in enumerate(new)]
+    c = Case((8, 8, 64), new, own, prefix, 16, seed=31)
+    assert sum(-(-n // 256) for n in new) * 8 > 3 * 152
+    window, sinks = 90, 3
+    marked = [s for s in range(64) if own[s] > 250][:3] if bad is not None else []
+    seen = np.zeros(c.tokens, bool)
+    for s in marked:
+        at = prefix + own[s] - new[s] // 2
+        _mark(c, s, at, bad)
+        pos = prefix + own[s] - new[s] + np.arange(new[s])
+        seen[c.start[s]:c.start[s + 1]] = (pos >= at) & (pos - window < at)
+    out, lse = _run(sdq, torch, c, window, sinks)
+    if bad is None:
+        _check(c, out, lse, window, sinks)
+        return
+    assert len(marked) == 3 and seen.any()
+    got = out.float()
+    hit = got[torch.from_numpy(seen).cuda()][..., 3::7]
+    assert torch.all(hit.isnan() if np.isnan(bad) else hit == bad)
+    clean = Case((8, 8, 64), new, own, prefix, 16, seed=31)
+    assert np.all(np.isfinite(np.delete(got.cpu().numpy(), np.s_[3::7], axis=-1)))
+    _check(clean, got.nan_to_num(0, 0, 0), lse, window, sinks, ~seen)
+
+
+def test_outputs_off_32_bytes_and_shares_of_few_row_blocks(sdq):
+    import torch
+    for heads, new, own in ((H7, [40], [3000]), ((4, 4, 64), [300], [301])):
+        c = Case(heads, new, own, 0, 16, seed=33)
+        cache, batch, q = c.cache(sdq, torch), c.batch(sdq, torch), to_bf16(torch, c.q)
+        want = cache.attend(batch, q, window=70, sinks=1)
+        flat = torch.full((q.numel() + 16,), 5.0, dtype=torch.bfloat16, device="cuda")
+        out = flat[8:8 + q.numel()].reshape(q.shape)                         # 16 bytes behind a boundary
+        ws = cache.alloc_workspace(batch, c.q_heads, window=70, sinks=1)
+        sdq.sdq_attention_window(cache.handle, batch, c.q_heads, q, c.q_heads * c.dim, c.dim ** -0.5, 70, 1, out, None, ws)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.all(flat[:8] == 5.0) and torch.all(flat[8 + q.numel():] == 5.0)
