@@ -239,11 +239,11 @@ def _empty(shape, dtype, device, stream):
 def _check_devices(where, first, *others):
     """Raise unless the tensors (None: left out) are all on the current device, on which the kernels run."""
     import torch
-    device = first.device
+    device = first.get_device()
     for t in others:
-        if t is not None and t.device != device:
+        if t is not None and t.get_device() != device:
             raise ValueError(f"{where}: tensors on different devices")
-    if device.index != torch.cuda.current_device():
+    if device != torch.cuda.current_device():
         raise ValueError(f"{where}: the tensors are not on the current device")
 
 

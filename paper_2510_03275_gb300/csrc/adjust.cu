@@ -247,13 +247,9 @@ extern "C" int sdq_adjust_logits(const void* logits, int32_t type, int32_t rows,
   if ((a->history && a->history_max < 0) || a->n_bias < 0 || a->n_bias > kMaxBiases) return SDQ_ERR_INVALID_ARG;
   if (a->n_bias > 0 && (!a->bias_ids || !a->bias)) return SDQ_ERR_INVALID_ARG;
   if (a->allowed && a->n_allowed < (a->allowed_row ? 1 : rows)) return SDQ_ERR_INVALID_ARG;
-  int dev = -1, major = 0, minor = 0, sms = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-    return SDQ_ERR_CUDA;
-  if (major != 10 || minor != 3) return SDQ_ERR_UNSUPPORTED;
+  int dev = -1, sms = 0;
+  const int supported = supported_device(&dev, &sms);
+  if (supported != SDQ_OK) return supported;
   AdjustParams p;
   p.a = *a;
   p.in = logits; p.out = out;

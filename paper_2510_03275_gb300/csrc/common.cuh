@@ -90,6 +90,27 @@ cudaError_t launch_prefill(const sdq_plan_s* p, const uint32_t* codes, const flo
 cudaError_t prefill_occupancy(sdq_plan_s* p);
 cudaError_t launch_read_prep(const sdq_plan_s* p, int M, const void* ws, float* out, cudaStream_t st);
 
+// The current device, and how many SMs it has: SDQ_OK, SDQ_ERR_UNSUPPORTED
+// where it is not of compute capability 10.3, or SDQ_ERR_CUDA.  What is asked of
+// the driver once per device does not change while the process lives.
+inline int supported_device(int* device, int* sms) {
+  static std::atomic<int> known[64];   // 0: not asked yet; -1: another capability; the number of SMs
+  if (cudaGetDevice(device) != cudaSuccess) return SDQ_ERR_CUDA;
+  const bool cached = *device >= 0 && *device < 64;
+  int n = cached ? known[*device].load(std::memory_order_acquire) : 0;
+  if (n == 0) {
+    int major = 0, minor = 0;
+    if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, *device) != cudaSuccess ||
+        cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, *device) != cudaSuccess ||
+        cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, *device) != cudaSuccess)
+      return SDQ_ERR_CUDA;
+    if (major != 10 || minor != 3) n = -1;
+    if (cached) known[*device].store(n, std::memory_order_release);
+  }
+  *sms = n;
+  return n > 0 ? SDQ_OK : SDQ_ERR_UNSUPPORTED;
+}
+
 // Raise `kernel`'s dynamic shared-memory limit to `bytes` once per device:
 // the setting is per function and device, and a constant value makes later
 // launches (and concurrent callers) skip the driver call.

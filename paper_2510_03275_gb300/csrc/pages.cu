@@ -221,12 +221,9 @@ extern "C" int sdq_pages_step(const sdq_pages* a, void* stream) {
   if (a->n_seqs < 1 || a->n_seqs > 65535 || a->n_tokens < 1 || a->n_tokens > (1 << 20)) return SDQ_ERR_INVALID_ARG;
   if (a->page_columns < 1 || a->page_stride < a->page_columns || (int64_t)a->page_columns * a->page_tokens >= (1ll << 30)) return SDQ_ERR_INVALID_ARG;
   if (a->prefix_len < 0 || a->prefix_len >= (1 << 30)) return SDQ_ERR_INVALID_ARG;
-  int dev = -1, major = 0, minor = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev) != cudaSuccess)
-    return SDQ_ERR_CUDA;
-  if (major != 10 || minor != 3) return SDQ_ERR_UNSUPPORTED;
+  int dev = -1, sms = 0;
+  const int supported = supported_device(&dev, &sms);
+  if (supported != SDQ_OK) return supported;
   PagesParams p;
   p.a = *a;
   p.shift = 4;

@@ -92,6 +92,9 @@ class _Elsewhere:
 
     is_cuda = True
 
+    def get_device(self):
+        return self.device.index
+
     def __getattr__(self, name):
         return getattr(self.t, name)
 
