@@ -23,6 +23,7 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendParams p) {
   const int tok = (int)(row / p.q_heads);
   const SeqSpan q = seq_span(p.b, seq_of_token(p.b.token_start, p.b.n_seqs, tok));
   const bool own = tok < q.first + q.count;
+  if (p.window > 0 && !own) return;   // (with a window a row that no sequence has stays as it was)
   const int np = p.narrow[kPrefix] + max(p.wide[kPrefix], p.splits[kPrefix]);
   const int n = np + (own ? p.narrow[kOwn] + max(p.wide[kOwn], p.splits[kOwn]) : 0);
   float acc[V], sum = 0.f, top = -INFINITY;
@@ -72,17 +73,32 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendParams p) {
 // one line, on the kernel of their number.
 constexpr int kPrefixNarrowRows = 8;
 
+// With a window, few rows a sequence: is it quicker to read what the sequences
+// see of the prefix once for all of them (the wide kernel and the join) than by
+// each for itself (40 bytes a ns and SM)?  As in wide_splits the mean own length
+// is taken as a sixth of its bound.
+bool prefix_apart(const sdq_cache_s* c, const AttendParams& p, int q_heads) {
+  const sdq_batch& b = p.b;
+  if (b.prefix_len == 0) return false;
+  const double seen = std::min<double>(b.prefix_len, std::max<double>(p.window - b.max_own / 6.0, p.sinks));
+  const double each = (double)b.n_seqs * c->desc.kv_heads * seen * c->desc.head_dim * 4 / (40e3 * c->sm_count);
+  const int s = wide_splits(c, p, q_heads, kPrefix, true);
+  const double join = 3.0 + (double)b.n_tokens * q_heads * c->desc.head_dim * 4.0 * (s + 1) / 4e6;
+  return each > wide_time(c, p, q_heads, kPrefix, s) + join;
+}
+
 void set_route(const sdq_cache_s* c, const sdq_batch* b, int q_heads, AttendParams* p) {
   const int group = q_heads / c->desc.kv_heads;
   // (a window, or first tokens, that cover every position leave nothing out)
   if ((int64_t)std::max(p->window, p->sinks) >= (int64_t)b->prefix_len + b->max_own) p->window = p->sinks = 0;
   const bool window = p->window > 0;
   const int64_t own_rows = b->max_own > 0 || (window && b->prefix_len > 0) ? (int64_t)b->max_new * group : 0;
-  const int64_t prefix_rows = b->prefix_len > 0 && !window ? (int64_t)b->n_tokens * group : 0;
   const bool own_wide = own_rows > kNarrowRows;
   p->b = *b;
   p->group = group;
   p->group_inverse = 65536u / (uint32_t)group + 1;
+  p->apart = window && !own_wide && b->max_own > 0 && (int64_t)b->n_tokens * group > kPrefixNarrowRows && prefix_apart(c, *p, q_heads);
+  const int64_t prefix_rows = b->prefix_len > 0 && (!window || p->apart) ? (int64_t)b->n_tokens * group : 0;
   p->chained = own_wide && prefix_rows > 0 && prefix_rows >= 128ll * b->n_seqs;
   p->wide[kOwn] = own_wide;
   // (a call without any keys goes through the narrow kernel too: it writes the zeros)

@@ -36,6 +36,7 @@ struct AttendParams {
   int q_heads, kv_heads, group, page_shift, box_shift, n_pages;
   uint32_t group_inverse;   // 2^16 / group + 1
   int window, sinks;        // a token sees its last `window` positions and the first `sinks` (window 0: all)
+  int apart;                // with a window: the prefix is a part of its own, for all sequences together
   int narrow[2], wide[2];   // which kernel takes a part (neither: it has no keys)
   int parts;                // parts that are computed apart (1, 2)
   int chained;              // the wide kernel's rows of kOwn run over the prefix first (no kPrefix part)

@@ -92,7 +92,7 @@ struct UnitLine {
 };
 __device__ __forceinline__ UnitLine unit_line(const AttendParams& p, int count, int own) {
   const int first = position_of(p, own - count);
-  return UnitLine{line_of<kTile>(p, p.b.prefix_len, 0, first), line_of<kTile>(p, own, p.b.prefix_len, first)};
+  return UnitLine{p.apart ? Line{0, 0, 0} : line_of<kTile>(p, p.b.prefix_len, 0, first), line_of<kTile>(p, own, p.b.prefix_len, first)};
 }
 
 // The line of units that have tiles.  All of it by whole warps: a lane holds
@@ -753,7 +753,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (part == kOwn)
       for (int s = blockIdx.x; s < p.b.n_seqs; s += gridDim.x) {
         const SeqSpan q = seq_span(p.b, s);
-        if (q.own > 0 || (kWindow && p.b.prefix_len > 0)) continue;
+        if (q.own > 0 || (kWindow && p.b.prefix_len > 0 && !p.apart)) continue;
         const int64_t r1 = (int64_t)(q.first + q.count) * p.q_heads;
         for (int64_t row = (int64_t)q.first * p.q_heads + warp; row < r1; row += kWarps) {
           const float none[D / 32] = {};

@@ -562,7 +562,7 @@ int wide_splits(const sdq_cache_s* c, const AttendParams& p, int q_heads, int pa
 }
 
 cudaError_t launch_wide(const sdq_cache_s* c, const AttendParams& p, int part, cudaStream_t st) {
-  if (p.window > 0) return launch_window(c, p, wide_grid(c, p, part), st);
+  if (p.window > 0) return launch_window(c, p, part, wide_grid(c, p, part), st);
   return c->desc.head_dim == 128 ? launch<128>(c, p, part, st) : launch<64>(c, p, part, st);
 }
 

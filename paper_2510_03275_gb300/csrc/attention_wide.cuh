@@ -71,7 +71,7 @@ __device__ __forceinline__ uint64_t sw128_mn_desc(uint32_t saddr) {
   return d;
 }
 
-// The wide kernel with a window: `items` row blocks, key heads and shares.
-cudaError_t launch_window(const sdq_cache_s* c, const AttendParams& p, int64_t items, cudaStream_t st);
+// The wide kernel with a window on `part`: `items` row blocks, key heads and shares.
+cudaError_t launch_window(const sdq_cache_s* c, const AttendParams& p, int part, int64_t items, cudaStream_t st);
 
 }  // namespace sdq

@@ -25,9 +25,12 @@ namespace {
 //                   item's queries over the last ones' as soon as the last scores are
 //                   there, ahead of their softmax (by one warp beside them: 2.5 us an
 //                   item more)
+// The other kind of items: all of the batch's rows against what the sequences see
+// of the prefix (part kPrefix), each row from where its own window begins.
 // An item's line is of 64-key pieces, two to a tile, so that what is left out,
 // first keys apart from the window, and the ends cost half a tile at most.
-constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;   // 2 x 216 + 72 = 3 x 168, the registers at launch
+// Registers: 384 threads hold 168 each at launch; the third warpgroup goes down to
+// 72, the first two up to 216 (2 x 216 + 72 = 3 x 168).
 
 // Stages of keys and of values (apart, so that whoever waits for the values has
 // waited for every use of a stage before).
@@ -37,7 +40,7 @@ template <int D> constexpr int kStagesV = WideShape<D>::kRing - kStagesK<D>;
 struct Item {
   int valid;                 // 0: there are no more
   int first, rows, r0;       // first token, rows of the (sequence, head), first row of the block
-  int h, split, s;           // key head, share, sequence
+  int h, split, s;           // key head, share, sequence (-1: the whole batch)
   int own, count;            // its own tokens and new tokens
   int piece, n, n_pieces;    // first piece of the line, tiles and pieces from there on
   int all_rows, low_rows;    // own keys that every row of the block sees, the first position that all of their windows have
@@ -62,12 +65,50 @@ __device__ __forceinline__ bool partial(const AttendParams& p, const volatile It
   return c.k0 + kSub > keys || (c.k0 < w.low_rows - base && c.k0 + kSub > p.sinks - base);
 }
 
+// What depends on the part that a call's kernel takes: picked on the host.
+// (Indexed by the part in the kernel, the parameters would be copied to local
+// memory; read through an address of theirs instead, as __grid_constant__ allows,
+// an early build faulted.)
+struct WindowPart {
+  int prefix;    // all of the batch's rows against the prefix
+  int splits;
+  int joins;     // fp32 sums for the join, or rows of the output
+  float* o;
+  float2* ml;
+};
+
 // Item `id` (a whole warp; lane 0's is written).  at, before: the 32 sequences
 // of the last search and the row blocks before them.
-__device__ __forceinline__ bool find_item(const AttendParams& p, int64_t id, int& at, int& before, Item* out) {
-  const int splits = p.splits[kOwn], lane = threadIdx.x & 31;
+__device__ __forceinline__ bool find_item(const AttendParams& p, const WindowPart& part, int64_t id, int& at, int& before, Item* out) {
+  const int splits = part.splits, lane = threadIdx.x & 31;
   const int64_t block = id / (p.kv_heads * splits);
   const int rest = (int)(id % (p.kv_heads * splits));
+  // the line's shares: which of its pieces the item takes
+  auto share = [&](Item& w) {
+    const int pieces = w.prefix.tiles + w.mine.tiles, tiles = (pieces + 1) / 2, per = (tiles + splits - 1) / splits;
+    const int t0 = min(tiles, w.split * per), t1 = min(tiles, t0 + per);
+    w.piece = 2 * t0;
+    w.n = t1 - t0;
+    w.n_pieces = max(0, min(2 * w.n, pieces - 2 * t0));
+  };
+  if (part.prefix) {
+    if (lane == 0) {
+      Item w;
+      w.valid = 1;
+      w.s = -1;
+      w.first = w.count = w.own = w.all_rows = 0;
+      w.rows = p.b.n_tokens * p.group;
+      w.r0 = (int)block * 256;
+      w.h = rest / splits;
+      w.split = rest % splits;
+      w.prefix = line_of<kSub>(p, p.b.prefix_len, 0, position_of(p, -1));   // (no token stands before that)
+      w.mine = Line{0, 0, 0};
+      w.low_rows = p.b.prefix_len;   // (some may see nothing of a piece but first keys)
+      share(w);
+      *out = w;
+    }
+    return true;
+  }
   for (; at < p.b.n_seqs; at += 32) {
     SeqSpan x{0, 0, 0};
     if (at + lane < p.b.n_seqs) x = seq_span(p.b, at + lane);
@@ -99,11 +140,7 @@ __device__ __forceinline__ bool find_item(const AttendParams& p, int64_t id, int
     const int keys = max(0, x.own - x.count + last / p.group + 1), first = position_of(p, x.own - x.count + w.r0 / p.group);
     w.prefix = line_of<kSub>(p, p.b.prefix_len, 0, first);
     w.mine = line_of<kSub>(p, keys, p.b.prefix_len, first);
-    const int pieces = w.prefix.tiles + w.mine.tiles, tiles = (pieces + 1) / 2, per = (tiles + splits - 1) / splits;
-    const int t0 = min(tiles, w.split * per), t1 = min(tiles, t0 + per);
-    w.piece = 2 * t0;
-    w.n = t1 - t0;
-    w.n_pieces = max(0, min(2 * w.n, pieces - 2 * t0));
+    share(w);
     w.all_rows = max(0, x.own - x.count + w.r0 / p.group + 1);
     w.low_rows = position_of(p, x.own - x.count + last / p.group) - p.window + 1;
     *out = w;
@@ -115,7 +152,7 @@ __device__ __forceinline__ bool find_item(const AttendParams& p, int64_t id, int
 template <int D>
 __global__ void __launch_bounds__(kWideThreads, 1)
     window_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const AttendParams p,
-                  const int64_t items) {
+                  const WindowPart part, const int64_t items) {
   using S = WideShape<D>;
   extern __shared__ uint8_t smem_raw[];
   constexpr int NK = kStagesK<D>, NV = kStagesV<D>;
@@ -181,7 +218,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
           break;
         }
         const int64_t id = blockIdx.x + (int64_t)it * gridDim.x;
-        const bool is = id < items && find_item(p, id, at, before, &item_s[it & 1]);
+        const bool is = id < items && find_item(p, part, id, at, before, &item_s[it & 1]);
         if (!is && lane == 0) item_s[it & 1].valid = 0;
         __syncwarp();
         if (lane == 0) mbar_arrive(&item_full[it & 1]);
@@ -249,7 +286,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
         const volatile Item& w = item_s[it & 1];
         if (!w.valid) break;
         const int n = w.n, n_pieces = w.n_pieces, own = w.own, h = w.h;
-        const int32_t* own_table = p.b.pages + (int64_t)w.s * p.b.page_stride;
+        const int32_t* own_table = p.b.pages + (int64_t)max(w.s, 0) * p.b.page_stride;
         // of the lane's box of tile t: is it one (not past the last key), its rows
         auto row_of = [&](int t, bool* is) {
           const int q = 2 * t + lane / per_piece;
@@ -424,10 +461,21 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       const int own = w.own, behind = own - w.count;   // the place of token 0 of the item's
       // own keys that this row sees, that every row of its half does
       const int lim = live ? behind + tok + 1 : own, all = behind + (r0 + 128 * half) / p.group + 1;
-      // the first position of this row's window, and of that of the last row of its half (the latest one)
+      // the first position of this row's window, and of that of the last row of its half (the latest one); where the
+      // rows are several sequences', of its warp's latest
       const int last = min(rows, r0 + 128 * half + 128) - 1;
       auto low_of = [&](int t) { return position_of(p, behind + t) - p.window + 1; };
-      const int low = live ? low_of(tok) : 0, low_half = low_of(last / p.group);
+      int low = 0, low_half;
+      if (part.prefix) {
+        if (live) {
+          const SeqSpan x = seq_span(p.b, seq_of_token(p.b.token_start, p.b.n_seqs, tok));
+          low = position_of(p, x.own - x.count + (tok - x.first)) - p.window + 1;
+        }
+        low_half = __reduce_max_sync(0xffffffffu, low);
+      } else {
+        if (live) low = low_of(tok);
+        low_half = low_of(last / p.group);
+      }
       // does piece q need a look at what its keys are?  (Of both pieces of a tile before its scores are waited for:
       // between the scores and the weights every instruction counts)
       auto edge_of = [&](int q) {
@@ -533,9 +581,8 @@ __global__ void __launch_bounds__(kWideThreads, 1)
       if (!ok) break;
       tc_fence_after();
       const bool taint = n > 0 && tainted[it & 1] == it + 1;
-      const bool split = p.splits[kOwn] > 1;
       const int64_t at = (int64_t)(w.first + tok) * p.q_heads + w.h * p.group + g;
-      const int64_t place = (split ? (int64_t)w.split * p.b.n_tokens * p.q_heads : 0) + at;
+      const int64_t place = (int64_t)w.split * p.b.n_tokens * p.q_heads + at;
       const float k = l > 0.f ? 1.f / l : l;       // (0 where nothing is seen; NaN stays)
       // (written straight from registers, 32 bytes a store: the place of the
       // queries, through which rows could go, holds the next ones by now)
@@ -559,7 +606,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
             const Piece pc = piece_at(w, q);
             if (!partial(p, w, pc)) continue;
             const int base = pc.pre ? 0 : p.b.prefix_len, end = min(pc.k0 + kSub, pc.pre ? p.b.prefix_len : lim);
-            const int32_t* table = pc.pre ? p.b.prefix_pages : p.b.pages + (int64_t)w.s * p.b.page_stride;
+            const int32_t* table = pc.pre ? p.b.prefix_pages : p.b.pages + (int64_t)max(w.s, 0) * p.b.page_stride;
 #pragma unroll 1
             for (int key = pc.k0; key < end; ++key) {
               if (key < low - base && key >= p.sinks - base) continue;
@@ -578,8 +625,8 @@ __global__ void __launch_bounds__(kWideThreads, 1)
           }
         __syncwarp();
         if (!live) continue;
-        if (split) {
-          float* dst = p.split_o[kOwn] + place * D + 32 * c;
+        if (part.joins) {
+          float* dst = part.o + place * D + 32 * c;
 #pragma unroll
           for (int j = 0; j < 4; ++j) st_global32(dst + 8 * j, o + 8 * j);
         } else {
@@ -596,8 +643,8 @@ __global__ void __launch_bounds__(kWideThreads, 1)
           }
         }
       }
-      if (live && split) p.split_ml[kOwn][place] = make_float2(l == l ? m : l, l);   // (NaN scores leave no maximum)
-      if (live && !split && p.lse) p.lse[at] = natural_lse(m, l);
+      if (live && part.joins) part.ml[place] = make_float2(l == l ? m : l, l);   // (NaN scores leave no maximum)
+      if (live && !part.joins && p.lse) p.lse[at] = natural_lse(m, l);
       if (n > 0) {
         tiles += n;
         ++blocks;
@@ -616,18 +663,21 @@ __global__ void __launch_bounds__(kWideThreads, 1)
 }
 
 template <int D>
-cudaError_t launch(const sdq_cache_s* c, const AttendParams& p, int64_t items, cudaStream_t st) {
+cudaError_t launch(const sdq_cache_s* c, const AttendParams& p, int part, int64_t items, cudaStream_t st) {
+  const bool split = p.splits[part] > 1;
+  const WindowPart w{part == kPrefix, p.splits[part], split || p.parts > 1, split ? p.split_o[part] : p.o[part],
+                     split ? p.split_ml[part] : p.ml[part]};
   static std::atomic<int> smem_set[64];
   const cudaError_t e = smem_limit_once(window_kernel<D>, WideShape<D>::kSmem, c->device, smem_set);
   if (e != cudaSuccess) return e;
   return launch_pdl(window_kernel<D>, dim3((unsigned)std::min<int64_t>(items, c->sm_count)), dim3(kWideThreads),
-                    (size_t)WideShape<D>::kSmem, st, c->kmap, c->vmap, p, items);
+                    (size_t)WideShape<D>::kSmem, st, c->kmap, c->vmap, p, w, items);
 }
 
 }  // namespace
 
-cudaError_t launch_window(const sdq_cache_s* c, const AttendParams& p, int64_t items, cudaStream_t st) {
-  return c->desc.head_dim == 128 ? launch<128>(c, p, items, st) : launch<64>(c, p, items, st);
+cudaError_t launch_window(const sdq_cache_s* c, const AttendParams& p, int part, int64_t items, cudaStream_t st) {
+  return c->desc.head_dim == 128 ? launch<128>(c, p, part, items, st) : launch<64>(c, p, part, items, st);
 }
 
 }  // namespace sdq

@@ -307,3 +307,98 @@ def test_outputs_off_32_bytes_and_shares_of_few_row_blocks(sdq):
         sdq.sdq_attention_window(cache.handle, batch, c.q_heads, q, c.q_heads * c.dim, c.dim ** -0.5, 70, 1, out, None, ws)
         torch.cuda.synchronize()
         assert torch.equal(out, want) and torch.all(flat[:8] == 5.0) and torch.all(flat[8 + q.numel():] == 5.0)
+
+
+# A prefix that is long against the own lengths, and many sequences: what they see of it is read once for all of
+# them and joined with each sequence's own part.
+APART = {
+    # heads, new tokens, own tokens, prefix, page, window, sinks
+    "decode": (H7, [1] * 100, [(7 * i) % 90 for i in range(100)], 1900, 64, 1500, 5),
+    "decode-70b": (H70, [1] * 128, [1 + (5 * i) % 60 for i in range(128)], 3001, 16, 2900, 0),
+    "window-over-the-prefix": (H7, [1] * 90, [1 + (37 * i) % 900 for i in range(90)], 1200, 32, 2000, 3),
+    "sinks-over-the-prefix": (H7, [1] * 90, [1 + (11 * i) % 300 for i in range(90)], 1300, 16, 200, 1350),
+    "draft": (ODD, [1 + i % 4 for i in range(128)], [4 + (13 * i) % 70 for i in range(128)], 2500, 128, 2300, 9),
+    "draft-short": (ODD, [1 + i % 4 for i in range(128)], [(3 * i) % 5 for i in range(128)], 2500, 16, 2300, 0),
+    "64": ((12, 12, 64), [1] * 70, [(5 * i) % 97 for i in range(70)], 1501, 16, 1400, 1),
+    "shares": ((8, 1, 128), [1] * 128, [1 + i % 50 for i in range(128)], 16000, 128, 15000, 20),
+}
+
+
+def _apart(sdq, torch, c, window, sinks):
+    """Does the call keep two parts' sums (fp32, for a row each)?"""
+    cache, batch = c.cache(sdq, torch), c.batch(sdq, torch)
+    return sdq.sdq_attention_window_workspace_bytes(cache.handle, batch, c.q_heads, window, sinks) >= 8 * c.tokens * c.q_heads * c.dim
+
+
+@pytest.mark.parametrize("name", APART)
+def test_a_prefix_shared_by_many_sequences(sdq, name):
+    import torch
+    heads, new, own, prefix, page, window, sinks = APART[name]
+    c = Case(heads, new, own, prefix, page, seed=len(name))
+    assert _apart(sdq, torch, c, window, sinks)
+    out, lse = _run(sdq, torch, c, window, sinks)
+    _check(c, out, lse, window, sinks)
+    again, lse2 = _run(sdq, torch, c, window, sinks)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("bad", [np.nan, np.inf])
+@pytest.mark.parametrize("name", ["decode", "draft", "64"])
+def test_values_of_a_shared_prefix_reach_the_rows_that_see_them(sdq, name, bad):
+    import torch
+    heads, new, own, prefix, page, window, sinks = APART[name]
+    c = Case(heads, new, own, prefix, page, seed=1)
+    marked = Case(heads, new, own, prefix, page, seed=1)
+    at = prefix - window + 45
+    _mark(marked, 0, at, bad)
+    for j in range(sinks, prefix - window):                  # and what no row sees may hold anything
+        _mark(marked, 0, j, np.nan)
+        _mark(marked, 0, j, np.nan, keys=True)
+    out, lse = _run(sdq, torch, marked, window, sinks)
+    pos = np.concatenate([prefix + np.maximum(-1, m - n + np.arange(n)) for n, m in zip(new, own)])
+    sees = at > pos - window
+    assert sees.any() and not sees.all()
+    got = out.float()
+    hit = got[torch.from_numpy(sees).cuda()][..., 3::7]
+    assert torch.all(hit.isnan() if np.isnan(bad) else hit == bad)
+    assert np.all(np.isfinite(np.delete(got.cpu().numpy(), np.s_[3::7], axis=-1)))
+    _check(c, got.nan_to_num(0, 0, 0), lse, window, sinks, ~sees)
+
+
+def test_rows_of_nobody_stay_beside_a_shared_prefix(sdq):
+    import torch
+    heads, new, own, prefix, page, window, sinks = APART["decode"]
+    c = Case(heads, new, own, prefix, page, seed=3)
+    cache = c.cache(sdq, torch)
+    i = lambda a: torch.from_numpy(np.ascontiguousarray(a, np.int32)).cuda()
+    batch = sdq.Batch(i(c.start), i(c.own), i(c.pages), 107, 1, max(own), i(c.prefix_pages), prefix)
+    q = torch.randn((107, 4, 128), device="cuda").to(torch.bfloat16)
+    c.q = q[:100].float().cpu().numpy()
+    ws = cache.alloc_workspace(batch, 4, window=window, sinks=sinks)
+    out = torch.full((107, 4, 128), 3.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((107, 4), 3.0, device="cuda")
+    sdq.sdq_attention_window(cache.handle, batch, 4, q, 512, 128 ** -0.5, window, sinks, out, lse, ws)
+    assert sdq.sdq_attention_status(ws) == 0
+    assert torch.all(out[100:] == 3.0) and torch.all(lse[100:] == 3.0)
+    _check(c, out[:100], lse[:100], window, sinks)
+
+
+def test_a_shared_prefix_in_a_graph(sdq):
+    """Lengths move on under a captured call, rows that saw much of the prefix see less."""
+    import torch
+    own = [(7 * i) % 90 for i in range(100)]
+    c = Case(H7, [1] * 100, [m + 40 for m in own], 1900, 64, seed=4)
+    cache, q = c.cache(sdq, torch), to_bf16(torch, c.q)
+    batch = c.batch(sdq, torch)
+    ws = cache.alloc_workspace(batch, 4, window=1500, sinks=2)
+    out, graph = torch.empty((100, 4, 128), dtype=torch.bfloat16, device="cuda"), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        sdq.sdq_attention_window(cache.handle, batch, 4, q, 512, 128 ** -0.5, 1500, 2, out, None, ws)
+    for step in (0, 1, 40):
+        now = Case(H7, [1] * 100, [m + 40 for m in own], 1900, 64, seed=4)
+        now.own = [m + step for m in own]
+        batch.tensors[1].copy_(torch.tensor(now.own, dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        _check(now, out, None, 1500, 2)
