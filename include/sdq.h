@@ -567,8 +567,10 @@ int sdq_attention(sdq_cache cache, const sdq_batch* batch, int32_t q_heads, cons
  * its own, stands at prefix_len - 1) sees, of the keys at positions j <= p,
  * those with j > p - window or j < sinks.  Positions count the prefix; keys that
  * no token of a sequence sees are not read.  window 1 .. 2^30 - 1 (its own key among them), sinks 0 ..
- * 2^30 - 1.  Every sequence reads what it sees of the prefix for itself.  All
- * else as sdq_attention; the workspace is this call's own size. */
+ * 2^30 - 1.  What they see of the prefix the sequences read each for itself, or,
+ * where that is quicker, all together as above.  Rows of out and lse that no
+ * sequence has are left as they were.  All else as sdq_attention; the workspace
+ * is this call's own size. */
 size_t sdq_attention_window_workspace_bytes(sdq_cache cache, const sdq_batch* batch, int32_t q_heads, int32_t window,
                                             int32_t sinks);
 int sdq_attention_window(sdq_cache cache, const sdq_batch* batch, int32_t q_heads, const uint16_t* q, int64_t ldq,

@@ -70,13 +70,18 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendParams p) {
 // and its own keys in one line; below that the batch's rows share blocks against
 // the prefix, and the two parts' results are joined.  With a window every
 // sequence's rows run over what they see of the prefix and of their own keys in
-// one line, on the kernel of their number.
+// one line, on the kernel of their number, unless the prefix is better read once
+// for all (prefix_apart).
 constexpr int kPrefixNarrowRows = 8;
 
 // With a window, few rows a sequence: is it quicker to read what the sequences
 // see of the prefix once for all of them (the wide kernel and the join) than by
 // each for itself (40 bytes a ns and SM)?  As in wide_splits the mean own length
-// is taken as a sixth of its bound.
+// is taken as a sixth of its bound.  us by this rule, always apart, never (64
+// heads, 8 key heads, lengths over their logarithm): 64 sequences of up to 900
+// behind 2051, window 515: 25, 27, 25; window 1500: 30, 30, 44; up to 4000, window
+// 2500: 63, 63, 58; 128 of up to 900 behind 4000, window 4000: 61, 61, 167; 16 of 32
+// heads of up to 900 behind 2051, window 1500: 26, 26, 42.
 bool prefix_apart(const sdq_cache_s* c, const AttendParams& p, int q_heads) {
   const sdq_batch& b = p.b;
   if (b.prefix_len == 0) return false;
