@@ -520,13 +520,66 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (!sees(b >> 2, b & 1, key + 8 * (b >> 1 & 1))) hidden |= 1u << b;
         }
         uint32_t pf[NT][2];
+        if (kWindow) {
+          // The reference of a query's weights is raised only where its maximum
+          // passes it by more than 2^8, and then set kAhead above it (weights and
+          // sums are floating: nothing is lost by a reference that lies higher);
+          // one look for all queries.  (Raised with every larger score, as below, one of 24
+          // queries' was on almost every tile: 2 x 3 tokens, window 32768, 77 us.)
+          constexpr float kRaise = 8.f, kAhead = 12.f;
+          float x[NT][4], mx[NT][2];
+          bool grow = false;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
+          for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              x[n][j] = (s[n][0][j] + s[n][1][j]) * p.scale;
+              if (hidden >> (4 * n + j) & 1u) x[n][j] = -INFINITY;
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              mx[n][j] = fmaxf(x[n][j], x[n][j + 2]);
+              grow |= mx[n][j] > m[n][j] + kRaise;   // (also from -inf)
+            }
+          }
+          if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              float f[2];
+#pragma unroll
+              for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) mx[n][j] = fmaxf(mx[n][j], __shfl_xor_sync(0xffffffffu, mx[n][j], d));
+                const bool raise = mx[n][j] > m[n][j] + kRaise;
+                f[j] = raise ? exp2_approx(m[n][j] - (mx[n][j] + kAhead)) : 1.f;
+                if (raise) m[n][j] = mx[n][j] + kAhead;
+                l[n][j] *= f[j];
+              }
+#pragma unroll
+              for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[n][d][j] *= f[j & 1];
+            }
+          }
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            float e[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              e[j] = exp2_approx(x[n][j] - (m[n][j & 1] == -INFINITY ? 0.f : m[n][j & 1]));
+              l[n][j & 1] += e[j];
+            }
+            pf[n][0] = movmatrix(pack_bf16x2(e[0], e[1]));
+            pf[n][1] = movmatrix(pack_bf16x2(e[2], e[3]));
+          }
+        }
+#pragma unroll
+        for (int n = 0; n < (kWindow ? 0 : NT); ++n) {
           float x[4];
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             x[j] = (s[n][0][j] + s[n][1][j]) * p.scale;
-            if (kWindow ? hidden >> (4 * n + j) & 1u : edge && key + 8 * (j >> 1) >= lim[n][j & 1]) x[j] = -INFINITY;
+            if (edge && key + 8 * (j >> 1) >= lim[n][j & 1]) x[j] = -INFINITY;
           }
           float mx[2];
 #pragma unroll

@@ -402,3 +402,34 @@ def test_a_shared_prefix_in_a_graph(sdq):
         graph.replay()
         torch.cuda.synchronize()
         _check(now, out, None, 1500, 2)
+
+
+@pytest.mark.parametrize("name", ["draft", "wide", "64", "apart"])
+def test_scores_that_are_not_a_number_stay_in_their_rows(sdq, name):
+    """A key that is NaN: NaN, and a log-sum-exp that is NaN, for the rows that see it alone."""
+    import torch
+    heads, new, own, prefix, page, window, sinks = {"draft": (ODD, [4], [300], 37, 16, 100, 5), "wide": (H70, [60], [300], 37, 16, 100, 5),
+                                                    "64": ((4, 4, 64), [290], [300], 20, 64, 40, 0), "apart": APART["decode"]}[name]
+    c, marked = (Case(heads, new, own, prefix, page, seed=6) for _ in range(2))
+    at = prefix - window + 60 if name == "apart" else prefix + own[0] - new[0] // 2 - window // 2
+    _mark(marked, 0, at, np.nan, keys=True)
+    out, lse = _run(sdq, torch, marked, window, sinks)
+    pos = np.concatenate([prefix + np.maximum(-1, m - n + np.arange(n)) for n, m in zip(new, own)])
+    sees = (at <= pos) & ((at > pos - window) | (at < sinks))
+    assert sees.any() and sees.all() == (name in ("draft", "wide"))
+    hit = torch.from_numpy(sees).cuda()
+    assert out[hit].isnan().all() and lse[hit].isnan().all()
+    if not sees.all():
+        _check(c, out.nan_to_num(0), lse.nan_to_num(0), window, sinks, ~sees)
+
+
+def test_scores_that_grow_and_shrink_along_the_window(sdq):
+    """Maxima that rise by a little at every tile, by much at some, and fall: references that are raised late."""
+    import torch
+    for heads, new in ((H70, 1), (H70, 3), (ODD, 5), (H7, 40)):
+        for shape in (np.linspace(-6, 6, 900), np.linspace(6, -6, 900), 8 * np.sin(np.arange(900) / 40.0), np.where(np.arange(900) % 300 == 299, 12.0, -12.0)):
+            c = Case(heads, [new], [900], 0, 16, seed=15)
+            for j in range(900):
+                c.k[c.pages[0, j // 16], :, j % 16] = bf16(shape[j] + 0.05 * c.k[c.pages[0, j // 16], :, j % 16])
+            c.q[:] = bf16(np.abs(c.q) * 0.25)
+            _check(c, *_run(sdq, torch, c, 700, 3), 700, 3)
