@@ -26,8 +26,8 @@ namespace {
 // window's, then of the sequence's own the same.  What the tokens of a unit see is then not nested, so a
 // value that is not finite and not every token's goes to those that see it by an
 // addition.  64 sequences of 1 to 16384 tokens, 64 heads, window 1024 and 4 first: 28.8
-// us (3.6 TB/s: the ends as above); 2 x 3 tokens, window 32768: 77 us, of which the
-// keys' reading 40: three groups of 8 rows keep a warp 4700 cycles on a tile.  (A third
+// us (3.6 TB/s: the ends as above); 2 x 3 tokens, window 32768: 72 us, of which the
+// keys' reading 40: three groups of 8 rows keep a warp 4000 cycles on a tile.  (A third
 // stage in the scratch's place gains nothing.)
 // P is rounded to bf16 for its product (relative 2^-8 at most per weight, as
 // the values themselves carry); sums, maxima and outputs are fp32.
@@ -95,8 +95,8 @@ __device__ __forceinline__ int token_of(const AttendParams& p, int r) { return (
 struct UnitLine {
   Line prefix, own;
   __device__ int tiles() const { return prefix.tiles + own.tiles; }
-  __device__ bool in_prefix(int i) const { return i < prefix.tiles; }
-  __device__ int tile(int i) const { return i < prefix.tiles ? prefix.tile(i) : own.tile(i - prefix.tiles); }
+  __device__ bool in_prefix(int i) const volatile { return i < prefix.tiles; }
+  __device__ int tile(int i) const volatile { return i < prefix.tiles ? prefix.tile(i) : own.tile(i - prefix.tiles); }
 };
 __device__ __forceinline__ UnitLine unit_line(const AttendParams& p, int count, int own) {
   const int first = position_of(p, own - count);
@@ -361,6 +361,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   __shared__ Pieces<NT> pc;
   __shared__ uint32_t arrived[2];
   __shared__ AttendParams sp;
+  constexpr bool kShared = kWindow && NT >= 3;   // (the accumulators leave no registers for the lines: 74 us with them there, not 72)
+  __shared__ UnitLine lines[kShared ? kWarps : 1][2];
   const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31;
   const uint32_t sbase = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem = smem_raw + (sbase - smem_u32(smem_raw));
@@ -395,15 +397,25 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (warp == 0 && lane == 0 && u.a < ct0) ticket_install(p.tickets[part] + (part == kPrefix ? u.h : (int64_t)u.s * p.kv_heads + u.h), p.call);
     // ---- copies: tile ti of unit ui is the next, if it is one of this share's; `page` of tile pb + lane of sequence ps
     int ti = (int)(t0 - u.a), ki = 0, pb = 0, ps = -2, page = -1;
-    UnitLine line, line_i;   // with a window: of u, of ui
-    if (kWindow) line = line_i = unit_line(p, u.count, u.keys);
+    UnitLine line_r[2];      // with a window: of u, of ui
+    const volatile UnitLine &line = kShared ? lines[warp][0] : line_r[0], &line_i = kShared ? lines[warp][1] : line_r[1];
+    auto set_line = [&](int which, const Unit& unit) {
+      if (!kShared) {
+        line_r[which] = unit_line(p, unit.count, unit.keys);
+        return;
+      }
+      __syncwarp();
+      if (lane == 0) lines[warp][which] = unit_line(p, unit.count, unit.keys);
+      __syncwarp();
+    };
+    if (kWindow) set_line(1, ui);
     const int per_page = p.page_shift - 4;   // log2 of tiles per page
     auto issue = [&]() {
       if (ti >= ui.tiles) {
         if (ui.a + walk.places_of(ui.tiles) >= t1) return;
         walk.next(ui);
         ti = 0;
-        if (kWindow) line_i = unit_line(p, ui.count, ui.keys);
+        if (kWindow) set_line(1, ui);
       }
       if (ui.a + ti >= t1) return;
       if (ui.s != ps || ti < pb || ti >= pb + 32) {
@@ -434,7 +446,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       // query rows as the products' B operand; rows past the last are zero
       uint32_t qf[NT][D / 16][2];
       int lim[NT][2];   // keys that this lane's two queries of each 8 see
-      if (kWindow) line = unit_line(p, u.count, u.keys);
+      if (kWindow) set_line(0, u);
       float o[NT][D / 16][4], m[NT][2], l[NT][2];
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
@@ -525,7 +537,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           // passes it by more than 2^8, and then set kAhead above it (weights and
           // sums are floating: nothing is lost by a reference that lies higher);
           // one look for all queries.  (Raised with every larger score, as below, one of 24
-          // queries' was on almost every tile: 2 x 3 tokens, window 32768, 77 us.)
+          // queries' was on almost every tile: 2 x 3 tokens, window 32768, 77 us, not 74.)
           constexpr float kRaise = 8.f, kAhead = 12.f;
           float x[NT][4], mx[NT][2];
           bool grow = false;

@@ -91,8 +91,8 @@ cudaError_t prefill_occupancy(sdq_plan_s* p);
 cudaError_t launch_read_prep(const sdq_plan_s* p, int M, const void* ws, float* out, cudaStream_t st);
 
 // The current device, and how many SMs it has: SDQ_OK, SDQ_ERR_UNSUPPORTED
-// where it is not of compute capability 10.3, or SDQ_ERR_CUDA.  What is asked of
-// the driver once per device does not change while the process lives.
+// where it is not of compute capability 10.3, or SDQ_ERR_CUDA.  (Asked once per
+// device: it does not change while the process lives.)
 inline int supported_device(int* device, int* sms) {
   static std::atomic<int> known[64];   // 0: not asked yet; -1: another capability; the number of SMs
   if (cudaGetDevice(device) != cudaSuccess) return SDQ_ERR_CUDA;
