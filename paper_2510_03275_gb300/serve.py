@@ -113,29 +113,21 @@ def generate(dec: Decoder, prefix, prompts, n_new, u, temperature=None, top_k=No
     an int32 tensor (n_new x requests); with keep_logits also the logits that
     they were drawn from.  Settings as in `sample`; penalties for tokens that
     repeat, biases and allowed tokens (bias_ids, bias, allowed, allowed_row) as
-    in `adjust_logits`."""
+    in `adjust_logits`.  The decoder's pool has as many free pages behind the
+    call as ahead of it, also where it raises; ValueError where they are too few,
+    RuntimeError where somebody else took them meanwhile."""
     import torch
     dev, page, n = dec.embedding.device, dec.page_tokens, len(prompts)
     ints = lambda x: torch.tensor(x, dtype=torch.int32, device=dev)
     lens = [len(p) for p in prompts]
     per = [-(-(m + n_new) // page) for m in lens]
     n_prefix = -(-len(prefix) // page)
-    if min(lens) < 1 or n_prefix + sum(per) > dec.n_pages:
-        raise ValueError("generate: an empty prompt, or more tokens than the cache has pages for")
+    if min(lens) < 1 or n_new < 1 or n_prefix + sum(per) > min(dec.n_pages, int(dec.pool.n_free)):
+        raise ValueError("generate: an empty prompt, no token to answer with, or more tokens than the cache has free pages for")
     own, front_own = ints([0] * n), ints([0])
     pages, front = (torch.full(size, -1, dtype=torch.int32, device=dev) for size in ((n, max(per)), (1, max(1, n_prefix))))
     shared = dict(prefix_pages=front[0] if prefix else None, prefix_len=len(prefix))
-    if prefix:   # its keys and values, once for everybody
-        at = dec.pool.step(front_own, ints([len(prefix)]), front, len(prefix))
-        dec.forward(ints(prefix), Batch(at.token_start, at.own_len, front, len(prefix), len(prefix), len(prefix)), rows=slice(-1, None))
     ends, ones = torch.tensor(lens).cumsum(0).tolist(), ints([1] * n)
-
-    def batch_of(new, tokens, max_new, max_own):
-        at = dec.pool.step(own, new, pages, tokens, prefix_len=len(prefix))
-        return Batch(at.token_start, own, pages, tokens, max_new, max_own, **shared)
-
-    last = ints([e - 1 for e in ends]).long()
-    u_now, tokens, out, logits = u[0].clone(), torch.empty(n, dtype=torch.int32, device=dev), [], []
     adjust.update(repetition=repetition, frequency=frequency, presence=presence)
     if any(x is not None for x in (repetition, frequency, presence)):
         # each request's tokens so far, the answer's behind the prompt's
@@ -143,6 +135,10 @@ def generate(dec: Decoder, prefix, prompts, n_new, u, temperature=None, top_k=No
         adjust["history"] = ints([list(prefix) + p + [-1] * (width - len(prefix) - len(p)) for p in prompts])
         adjust["prompt_len"] = ints([len(prefix) + m for m in lens])
         adjust["history_len"] = adjust["prompt_len"].clone()
+
+    def batch_of(new, tokens, max_new, max_own):
+        at = dec.pool.step(own, new, pages, tokens, prefix_len=len(prefix))
+        return Batch(at.token_start, own, pages, tokens, max_new, max_own, **shared)
 
     def choose(z):
         if any(x is not None for x in adjust.values()):
@@ -156,27 +152,37 @@ def generate(dec: Decoder, prefix, prompts, n_new, u, temperature=None, top_k=No
     def decode():
         return choose(dec.forward(tokens, batch_of(ones, n, 1, max(lens) + n_new)))
 
-    z = dec.forward(ints([t for p in prompts for t in p]), batch_of(ints(lens), ends[-1], max(lens), max(lens)), rows=last)
-    z, replay = choose(z), None
-    for i in range(n_new):
-        if i > 0:
-            u_now.copy_(u[i])
-            if replay is not None:
-                replay.replay()
-            else:
-                z = decode()
-        out.append(tokens.clone())
-        if keep_logits:
-            logits.append(z.clone())
-        if graph and i == 1 and n_new > 2:   # (after a step of the same sizes has run)
-            replay = torch.cuda.CUDAGraph()
-            with torch.cuda.graph(replay):
-                z = decode()
-    # the pages go back
-    dec.pool.step(own, ones - 1, pages, 1, done=ones)
-    if prefix:
-        dec.pool.step(front_own, ones[:1] - 1, front, 1, done=ones[:1])
-    return (torch.stack(out), torch.stack(logits)) if keep_logits else torch.stack(out)
+    try:
+        if prefix:   # its keys and values, once for everybody
+            at = dec.pool.step(front_own, ints([len(prefix)]), front, len(prefix))
+            dec.forward(ints(prefix), Batch(at.token_start, at.own_len, front, len(prefix), len(prefix), len(prefix)),
+                        rows=slice(-1, None))
+        last = ints([e - 1 for e in ends]).long()
+        u_now, tokens, out, logits = u[0].clone(), torch.empty(n, dtype=torch.int32, device=dev), [], []
+        z = dec.forward(ints([t for p in prompts for t in p]), batch_of(ints(lens), ends[-1], max(lens), max(lens)), rows=last)
+        z, replay = choose(z), None
+        for i in range(n_new):
+            if i > 0:
+                u_now.copy_(u[i])
+                if replay is not None:
+                    replay.replay()
+                else:
+                    z = decode()
+            out.append(tokens.clone())
+            if keep_logits:
+                logits.append(z.clone())
+            if graph and i == 1 and n_new > 2:   # (after a step of the same sizes has run)
+                replay = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(replay):
+                    z = decode()
+        # (a step that does not get its pages leaves a request's tokens out, and shifts the rows of those behind it)
+        if own.tolist() + front_own.tolist() != [m + n_new - 1 for m in lens] + [len(prefix)]:
+            raise RuntimeError("generate: the pool ran out of pages on the way (other calls take from it meanwhile)")
+        return (torch.stack(out), torch.stack(logits)) if keep_logits else torch.stack(out)
+    finally:   # the pages go back, whatever has become of the call
+        dec.pool.step(own, ones - 1, pages, 1, done=ones)
+        if prefix:
+            dec.pool.step(front_own, ones[:1] - 1, front, 1, done=ones[:1])
 
 
 def main(argv=None):
