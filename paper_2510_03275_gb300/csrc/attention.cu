@@ -23,7 +23,7 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendParams p) {
   const int tok = (int)(row / p.q_heads);
   const SeqSpan q = seq_span(p.b, seq_of_token(p.b.token_start, p.b.n_seqs, tok));
   const bool own = tok < q.first + q.count;
-  if (p.window > 0 && !own) return;   // (with a window a row that no sequence has stays as it was)
+  if (p.keep && !own) return;
   const int np = p.narrow[kPrefix] + max(p.wide[kPrefix], p.splits[kPrefix]);
   const int n = np + (own ? p.narrow[kOwn] + max(p.wide[kOwn], p.splits[kOwn]) : 0);
   float acc[V], sum = 0.f, top = -INFINITY;
@@ -94,6 +94,7 @@ bool prefix_apart(const sdq_cache_s* c, const AttendParams& p, int q_heads) {
 
 void set_route(const sdq_cache_s* c, const sdq_batch* b, int q_heads, AttendParams* p) {
   const int group = q_heads / c->desc.kv_heads;
+  p->keep = p->window > 0;
   // (a window, or first tokens, that cover every position leave nothing out)
   if ((int64_t)std::max(p->window, p->sinks) >= (int64_t)b->prefix_len + b->max_own) p->window = p->sinks = 0;
   const bool window = p->window > 0;
@@ -111,6 +112,8 @@ void set_route(const sdq_cache_s* c, const sdq_batch* b, int q_heads, AttendPara
   p->wide[kPrefix] = prefix_rows > kPrefixNarrowRows && !p->chained;
   p->narrow[kPrefix] = prefix_rows > 0 && prefix_rows <= kPrefixNarrowRows;
   p->parts = p->wide[kOwn] + p->narrow[kOwn] + p->wide[kPrefix] + p->narrow[kPrefix];
+  // (a prefix alone takes all of the batch's rows: the join leaves out those that no sequence has)
+  if (p->keep && prefix_rows > 0 && !p->chained) p->parts = 2;
   for (int part = 0; part < 2; ++part) {
     p->splits[part] = p->wide[part] ? wide_splits(c, *p, q_heads, part, part == kPrefix && p->narrow[kOwn]) : 0;
   }

@@ -37,8 +37,9 @@ struct AttendParams {
   uint32_t group_inverse;   // 2^16 / group + 1
   int window, sinks;        // a token sees its last `window` positions and the first `sinks` (window 0: all)
   int apart;                // with a window: the prefix is a part of its own, for all sequences together
+  int keep;                 // rows of the output that no sequence has stay as they were (called with a window, whatever that covers)
   int narrow[2], wide[2];   // which kernel takes a part (neither: it has no keys)
-  int parts;                // parts that are computed apart (1, 2)
+  int parts;                // parts that are computed apart (1, 2; above 1 their rows go to the join)
   int chained;              // the wide kernel's rows of kOwn run over the prefix first (no kPrefix part)
   int splits[2];            // thread blocks that share a row block's keys in the wide kernel
   uint64_t* rec;
