@@ -597,6 +597,9 @@ class Batch:
         self.n_seqs, self.n_tokens, self.max_new, self.max_own = n_seqs, n_tokens, max_new, max_own
         self.prefix_len = prefix_len
         self.tensors = (token_start, own_len, pages, prefix_pages)
+        self.device_index = own_len.get_device()
+        if any(t is not None and t.get_device() != self.device_index for t in self.tensors):
+            raise ValueError("Batch: tensors on different devices")
         self.page_columns = pages.shape[1]
         self._c = _Batch(n_seqs, n_tokens, max_new, max_own, pages.stride(0) if n_seqs > 1 else pages.shape[1], prefix_len,
                          token_start.data_ptr(), own_len.data_ptr(), pages.data_ptr() or None,
@@ -694,7 +697,10 @@ class Rope:
             for t in (cos, sin):
                 if t.dtype != torch.float32 or t.dim() != 2 or not t.is_cuda or not t.is_contiguous() or t.shape != cos.shape:
                     raise ValueError("Rope: cos and sin must be contiguous 2-d float32 CUDA tensors of one shape")
+            if cos.get_device() != sin.get_device():
+                raise ValueError("Rope: cos and sin on different devices")
         self.tensors = (cos, sin)
+        self.device_index = None if cos is None else cos.get_device()
         self._c = _Rope(_ptr(cos), _ptr(sin), 0 if cos is None else cos.shape[0], 0 if cos is None else 2 * cos.shape[1],
                         int(interleaved))
         self.ref = ctypes.addressof(self._c)
@@ -736,7 +742,10 @@ class HeadNorm:
 
 class KVCache:
     """Owns an ``sdq_cache`` and holds its two arrays (allocated here, zeroed,
-    unless given: bf16, ``desc.shape``, contiguous)."""
+    unless given: bf16, ``desc.shape``, contiguous).  Everything that a call
+    works on is on the arrays' device, the current one."""
+
+    device_index = -1   # (of the arrays)
 
     def __init__(self, desc: CacheDesc, k_pages=None, v_pages=None, device="cuda"):
         import torch
@@ -747,7 +756,8 @@ class KVCache:
         for t in (k_pages, v_pages):
             if t is None or t.dtype != torch.bfloat16 or tuple(t.shape) != desc.shape or not t.is_contiguous() or not t.is_cuda:
                 raise ValueError("KVCache: both arrays must be contiguous bfloat16 CUDA tensors of desc.shape")
-        self.k_pages, self.v_pages = k_pages, v_pages
+        _check_devices("KVCache", k_pages, v_pages)
+        self.k_pages, self.v_pages, self.device_index = k_pages, v_pages, k_pages.get_device()
         self.handle = sdq_cache_create(desc, k_pages, v_pages)
 
     def close(self):
@@ -769,8 +779,7 @@ class KVCache:
         import torch
         d, tokens, shape, rows = self.desc, batch.n_tokens, q.shape, k.shape
         dim = d.head_dim
-        if (len(shape) != 2 or shape[0] != tokens or rows != (tokens, d.kv_heads * dim) or v.shape != rows
-                or not (q.is_cuda and k.is_cuda and v.is_cuda)):
+        if len(shape) != 2 or shape[0] != tokens or rows != (tokens, d.kv_heads * dim) or v.shape != rows:
             raise ValueError("KVCache.append: q, k and v need one row of heads x head_dim elements per token")
         (ldq, q1), (ldk, k1), (ldv, v1) = q.stride(), k.stride(), v.stride()
         if not q1 == k1 == v1 == 1:
@@ -781,6 +790,11 @@ class KVCache:
         if tokens == 1:   # (a single row has no stride of its own)
             ldq, ldk, ldv = shape[1], rows[1], rows[1]
         batch.check(d.page_tokens)
+        at = self.device_index
+        if not q.get_device() == k.get_device() == v.get_device() == batch.device_index == at or rope.device_index not in (None, at):
+            raise ValueError("KVCache.append: q, k, v, the batch and the rotation tables must be on the cache's device")
+        if norm is not None:
+            norm.check(q_heads, d.kv_heads, dim, self.k_pages.device)
         kind = q.dtype
         kind = -1 if k.dtype is not kind or v.dtype is not kind else SDQ_F32 if kind is torch.float32 else SDQ_BF16 if kind is torch.bfloat16 else -1
         out = _empty((tokens, q_heads, dim), torch.bfloat16, q.device, stream)
@@ -788,7 +802,6 @@ class KVCache:
             _check(lib().sdq_cache_append(self.handle, batch.ref, q_heads, q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
                                           kind, rope.ref, out.data_ptr(), _stream(stream)), "sdq_cache_append")
         else:
-            norm.check(q_heads, d.kv_heads, dim, self.k_pages.device)
             _check(lib().sdq_cache_append_norm(self.handle, batch.ref, q_heads, q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(),
                                                ldv, kind, rope.ref, norm.ref, out.data_ptr(), _stream(stream)),
                    "sdq_cache_append_norm")
@@ -824,10 +837,13 @@ class KVCache:
         if window is None and sinks != 0:
             raise ValueError("KVCache.attend: sinks belong to a window")
         batch.check(d.page_tokens)
+        at = self.device_index
+        if not q.get_device() == batch.device_index == at or (lse is not None and lse.get_device() != at):
+            raise ValueError("KVCache.attend: q, the batch and lse must be on the cache's device")
         if ws is None:
             ws = self.alloc_workspace(batch, heads, stream, window, sinks)
-        elif not ws.is_cuda or not ws.is_contiguous():
-            raise ValueError("KVCache.attend: ws must be a contiguous CUDA tensor")
+        elif not ws.is_cuda or not ws.is_contiguous() or ws.get_device() != at:
+            raise ValueError("KVCache.attend: ws must be a contiguous CUDA tensor on the cache's device")
         out = _empty((tokens, heads, dim), torch.bfloat16, q.device, stream)
         ldq, scale = stride[0] if tokens > 1 else heads * dim, dim ** -0.5 if scale is None else scale
         if window is None:
@@ -847,8 +863,9 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, stre
         raise ValueError("sample: logits must be a CUDA tensor (rows, vocab) with adjacent elements in a row")
     rows, f32 = shape[:1], torch.float32
     for t, dtype in ((u, f32), (temperature, f32), (top_k, torch.int32), (top_p, f32), (min_p, f32)):
-        if t is not None and (t.dtype is not dtype or t.shape != rows or not t.is_contiguous() or not t.is_cuda):
+        if t is not None and (t.dtype is not dtype or t.shape != rows or not t.is_contiguous()):
             raise ValueError("sample: u, temperature, top_p and min_p are float32, top_k int32, one per row, on the GPU")
+    _check_devices("sample", logits, u, temperature, top_k, top_p, min_p)
     tokens = _empty(rows, torch.int32, logits.device, stream)
     sdq_sample(logits, u, temperature, top_k, top_p, min_p, tokens, stream)
     return tokens
