@@ -236,14 +236,27 @@ def _empty(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+def _first_current_device() -> int:
+    """The current device; once CUDA is initialized straight from the binding that torch's own call ends in, where this
+    torch has it."""
+    global _current_device
+    import torch
+    device, raw = torch.cuda.current_device(), getattr(torch._C, "_cuda_getDevice", None)
+    if raw is not None and torch.cuda.is_initialized() and raw() == device:
+        _current_device = raw
+    return device
+
+
+_current_device = _first_current_device
+
+
 def _check_devices(where, first, *others):
     """Raise unless the tensors (None: left out) are all on the current device, on which the kernels run."""
-    import torch
     device = first.get_device()
     for t in others:
         if t is not None and t.get_device() != device:
             raise ValueError(f"{where}: tensors on different devices")
-    if device != torch.cuda.current_device():
+    if device != _current_device():
         raise ValueError(f"{where}: the tensors are not on the current device")
 
 
@@ -862,10 +875,11 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, stre
     if len(shape) != 2 or logits.stride()[1] != 1 or not logits.is_cuda:
         raise ValueError("sample: logits must be a CUDA tensor (rows, vocab) with adjacent elements in a row")
     rows, f32 = shape[:1], torch.float32
+    _check_devices("sample", logits)
+    at = logits.get_device()
     for t, dtype in ((u, f32), (temperature, f32), (top_k, torch.int32), (top_p, f32), (min_p, f32)):
-        if t is not None and (t.dtype is not dtype or t.shape != rows or not t.is_contiguous()):
-            raise ValueError("sample: u, temperature, top_p and min_p are float32, top_k int32, one per row, on the GPU")
-    _check_devices("sample", logits, u, temperature, top_k, top_p, min_p)
+        if t is not None and (t.dtype is not dtype or t.shape != rows or not t.is_contiguous() or t.get_device() != at):
+            raise ValueError("sample: u, temperature, top_p and min_p are float32, top_k int32, one per row, on the logits' GPU")
     tokens = _empty(rows, torch.int32, logits.device, stream)
     sdq_sample(logits, u, temperature, top_k, top_p, min_p, tokens, stream)
     return tokens
