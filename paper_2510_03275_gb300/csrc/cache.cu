@@ -98,13 +98,14 @@ __device__ __forceinline__ Place place_of(const AppendParams& p, int t, int s) {
 // ones of every head that it comes to, so that their cosines, sines and weights
 // are read once per token (a read for each head, from the L1, cost as much as
 // the data).  The next head's elements are under way while one is worked on.
-// grid.x: tokens, grid.y: parts of a token's heads.  2566 tokens of 64 + 2 x 8
-// heads of 128, fp32: 27.6 us (86 % of the measured copy bandwidth); one token:
-// 1.9 us, 2.2 with norms (a graph of 30 calls).
+// grid.x: tokens, grid.y: parts of a token's heads.  One token of 64 + 2 x 8 heads of
+// 128, fp32: 1.7 us, 2.2 with norms; 256 tokens without norms: 3.6 (a graph of 30 calls).
 // kNorm: a head's threads are neighbours in one warp (8 or 16 of them) and add up
 // its squares, all in fp32; whole warps stay in the loop for it.
+// (Registers: 56 without norms.  Held to 40, so that more thread blocks fit, they
+// spill: 1.9 us for the one token, 4.5 for the 256.)
 template <class T, bool kNorm>
-__global__ void __launch_bounds__(kThreads, kNorm ? 3 : 6) append_kernel(const AppendParams p) {
+__global__ void __launch_bounds__(kThreads, kNorm ? 3 : 1) append_kernel(const AppendParams p) {
   pdl_wait();
   pdl_launch_dependents();
   const int t = blockIdx.x, lanes = p.dim / 8, half = p.rope.dim / 2;   // threads of a head
@@ -165,16 +166,59 @@ __global__ void __launch_bounds__(kThreads, kNorm ? 3 : 6) append_kernel(const A
   }
 }
 
-// The same for many tokens.  Loads that wait in registers are too few bytes
-// under way here (the arithmetic needs the registers): a warp streams pieces of
-// kPiece bytes, some heads of one token's q, k or v, through a ring of its own in
-// shared memory, 192 KB of an SM under way at once.  The line of pieces, token
+// Without norms, many tokens: thread blocks enough for every SM to hold several, so
+// that what hides the loads is their number and not each one's own next load.  A
+// thread holds 8 elements and nothing from one head to the next (38 registers, 6
+// thread blocks of an SM against 4).  fp32, us here and by append_kernel: 64 + 2 x 8
+// heads of 128, 900 tokens 11.1, 12.8; 2400 25.7 (84 % of the measured copy
+// bandwidth), 27.8; 3 x 12 heads of 64, 400 tokens 2.4, 2.8; 2400 8.9, 10.9.
+// (append_kernel is ahead once more where its blocks just fill all places, 608 tokens:
+// 600 of 64 + 2 x 8 heads 9.0, 8.4; 400 of 8 + 2 heads 2.0, 2.6.  So it takes calls of up
+// to two tokens an SM, where it is ahead for all of these but the last: 256 2.0, 2.1.)
+template <class T>
+__global__ void __launch_bounds__(kThreads) append_many_kernel(const AppendParams p) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const int t = blockIdx.x, lanes = p.dim / 8, half = p.rope.dim / 2;
+  const Place at = place_of(p, t, seq_of_token(p.b.token_start, p.b.n_seqs, t));
+  const int units = (p.q_heads + 2 * p.kv_heads) * lanes;
+  for (int u = threadIdx.x; u < units; u += kThreads) {
+    const int h = u / lanes, c = u - h * lanes;
+    const bool is_q = h < p.q_heads, is_v = h >= p.q_heads + p.kv_heads;
+    const int kh = is_q ? h : is_v ? h - p.q_heads - p.kv_heads : h - p.q_heads;
+    const T* src = is_q   ? static_cast<const T*>(p.q) + t * p.ldq + kh * p.dim
+                   : is_v ? static_cast<const T*>(p.v) + t * p.ldv + kh * p.dim
+                          : static_cast<const T*>(p.k) + t * p.ldk + kh * p.dim;
+    const bool turn = !is_v && 8 * c < p.rope.dim, split = turn && !p.rope.interleaved;
+    const int ea = split ? 4 * c : 8 * c, eb = split ? 4 * c + half : 8 * c + 4;
+    float4 a = load4(src + ea), b = load4(src + eb);
+    if (turn) {
+      const float4 cs = load4(p.rope.cos + (int64_t)at.pos * half + 4 * c);
+      const float4 sn = load4(p.rope.sin + (int64_t)at.pos * half + 4 * c);
+      rotate(a, b, cs, sn, split);
+    }
+    uint16_t* dst;
+    if (is_q) {
+      dst = p.q_out + ((int64_t)t * p.q_heads + kh) * p.dim;
+    } else {
+      if (at.page < 0) continue;
+      dst = (is_v ? p.vp : p.kp) + (((int64_t)at.page * p.kv_heads + kh) * p.page + at.at % p.page) * p.dim;
+    }
+    store4(dst + ea, a);
+    store4(dst + eb, b);
+  }
+}
+
+// The same for many tokens with norms, or in bf16.  Loads that wait in registers are too
+// few bytes under way here (the arithmetic needs the registers): a warp streams
+// pieces of kPiece bytes, some heads of one token's q, k or v, through a ring of its
+// own in shared memory, 192 KB of an SM under way at once.  The line of pieces, token
 // by token, is cut into equal shares for all warps; what a token needs (its
 // place, its cosines and sines) is looked up when a share comes to it.
 // 3710 tokens of 64 + 2 x 8 heads of 128, normalised: fp32 42.5 us (79 % of the
 // measured copy bandwidth; append_kernel 52), bf16 38.3 (61.6: the sums'
-// shuffles, not the bytes); without norms fp32 40.0 (37.8, so these stay
-// there), bf16 28.8 (34.5).  256 tokens, normalised: fp32 7.5 (6.3), bf16 6.3
+// shuffles, not the bytes); without norms fp32 40.0 (append_many_kernel 37.8, so these
+// stay there), bf16 28.8 (34.5).  256 tokens, normalised: fp32 7.5 (6.3), bf16 6.3
 // (6.9); 512 of 3 x 12 heads of 64: 4.6 (5.4), 256 of them 4.5 (3.5).
 constexpr int kStreamWarps = 16, kPiece = 4096, kStages = 3;
 constexpr int64_t kStreamHeads = 24576;   // of q, k and v, from which this kernel takes a call
@@ -438,6 +482,10 @@ static int append(sdq_cache c, const sdq_batch* b, int32_t q_heads, const void* 
     e = type == SDQ_F32 ? run(append_stream_kernel<float, true>, 0)
         : norm          ? run(append_stream_kernel<uint16_t, true>, 1)
                         : run(append_stream_kernel<uint16_t, false>, 2);
+  } else if (!norm && b->n_tokens > 2 * c->sm_count) {   // (grid.y is 1 there)
+    const dim3 tokens((unsigned)b->n_tokens);
+    e = type == SDQ_F32 ? launch_pdl(append_many_kernel<float>, tokens, dim3(kThreads), 0, cs, p)
+                        : launch_pdl(append_many_kernel<uint16_t>, tokens, dim3(kThreads), 0, cs, p);
   } else {
     auto run = [&](auto kernel) { return launch_pdl(kernel, grid, dim3(kThreads), 0, cs, p); };
     e = type == SDQ_F32 ? norm ? run(append_kernel<float, true>) : run(append_kernel<float, false>)
