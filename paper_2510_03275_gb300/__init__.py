@@ -933,6 +933,8 @@ def adjust_logits(logits, history=None, history_len=None, prompt_len=None, repet
         raise ValueError("adjust_logits: allowed_row belongs to allowed")
     if allowed is not None and words < (vocab + 31) // 32:
         raise ValueError("adjust_logits: the sets of allowed have too few words")
+    if allowed is not None and at_allowed == 0 and allowed_row is None:   # (no memory: as if it were not given)
+        raise ValueError("adjust_logits: allowed needs a set for each row, or allowed_row")
     _check_devices("adjust_logits", logits, history, history_len, prompt_len, repetition, frequency, presence, bias_ids, bias,
                    allowed, allowed_row, out)
     if out is None:
