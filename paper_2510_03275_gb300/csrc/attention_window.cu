@@ -626,14 +626,12 @@ __global__ void __launch_bounds__(kWideThreads, 1)
               }
             }
           }
-          }
-        __syncwarp();
-        if (!live) continue;
-        if (part.joins) {
+        }
+        if (live && part.joins) {
           float* dst = part.o + place * D + 32 * c;
 #pragma unroll
           for (int j = 0; j < 4; ++j) st_global32(dst + 8 * j, o + 8 * j);
-        } else {
+        } else if (live) {
           uint32_t r[16];
 #pragma unroll
           for (int j = 0; j < 16; ++j) r[j] = pack_bf16x2(__uint_as_float(o[2 * j]) * k, __uint_as_float(o[2 * j + 1]) * k);
@@ -646,6 +644,7 @@ __global__ void __launch_bounds__(kWideThreads, 1)
             for (int j = 0; j < 4; ++j) reinterpret_cast<uint4*>(dst)[j] = make_uint4(r[4 * j], r[4 * j + 1], r[4 * j + 2], r[4 * j + 3]);
           }
         }
+        __syncwarp();   // (whole warps read tensor memory)
       }
       if (live && part.joins) part.ml[place] = make_float2(l == l ? m : l, l);   // (NaN scores leave no maximum)
       if (live && !part.joins && p.lse) p.lse[at] = natural_lse(m, l);

@@ -99,7 +99,7 @@ __device__ __forceinline__ Place place_of(const AppendParams& p, int t, int s) {
 // are read once per token (a read for each head, from the L1, cost as much as
 // the data).  The next head's elements are under way while one is worked on.
 // grid.x: tokens, grid.y: parts of a token's heads.  One token of 64 + 2 x 8 heads of
-// 128, fp32: 1.7 us, 2.2 with norms; 256 tokens without norms: 3.6 (a graph of 30 calls).
+// 128, fp32: 1.6 us, 2.2 with norms; 256 of four sequences, without norms: 3.9 (a graph of 30 calls).
 // kNorm: a head's threads are neighbours in one warp (8 or 16 of them) and add up
 // its squares, all in fp32; whole warps stay in the loop for it.
 // (Registers: 56 without norms.  Held to 40, so that more thread blocks fit, they
