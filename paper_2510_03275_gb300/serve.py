@@ -175,14 +175,16 @@ def generate(dec: Decoder, prefix, prompts, n_new, u, temperature=None, top_k=No
                 replay = torch.cuda.CUDAGraph()
                 with torch.cuda.graph(replay):
                     z = decode()
-        # (a step that does not get its pages leaves a request's tokens out, and shifts the rows of those behind it)
-        if own.tolist() + front_own.tolist() != [m + n_new - 1 for m in lens] + [len(prefix)]:
-            raise RuntimeError("generate: the pool ran out of pages on the way (other calls take from it meanwhile)")
-        return (torch.stack(out), torch.stack(logits)) if keep_logits else torch.stack(out)
+        got, lengths = torch.stack(out), torch.cat([own, front_own])
+        logits = torch.stack(logits) if keep_logits else None
     finally:   # the pages go back, whatever has become of the call
         dec.pool.step(own, ones - 1, pages, 1, done=ones)
         if prefix:
             dec.pool.step(front_own, ones[:1] - 1, front, 1, done=ones[:1])
+    # (a step that does not get its pages leaves a request's tokens out, and shifts the rows of those behind it)
+    if lengths.tolist() != [m + n_new - 1 for m in lens] + [len(prefix)]:
+        raise RuntimeError("generate: the pool ran out of pages on the way (other calls take from it meanwhile)")
+    return (got, logits) if keep_logits else got
 
 
 def main(argv=None):
