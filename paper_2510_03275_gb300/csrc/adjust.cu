@@ -50,7 +50,8 @@ struct Row {
 // logits (a copy: 17 us): 34 us, 11 of them for histories of 100 to 32768 tokens
 // (their length, their tokens, the logits: chains of latencies that two thread
 // blocks per SM hide in part; 16-bit counters, for three, gain nothing), 4 for
-// 300 biases, 2 for the grammar; one row of 32000: 3.4.
+// 300 biases, 2 for the grammar; in place 36 (less is written, but a block reads a piece only
+// once it knows that it changes); one row of 32000: 3.5.
 template <class T, int kV, bool kInPlace>
 __global__ void __launch_bounds__(kThreads, kV * 16 / (int)sizeof(T) >= 32 ? 2 : 3) adjust_kernel(const AdjustParams p) {
   constexpr int kVec = 16 / sizeof(T), kChunk = kThreads * kV * kVec;

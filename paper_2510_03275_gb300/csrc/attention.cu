@@ -81,7 +81,12 @@ constexpr int kPrefixNarrowRows = 8;
 // heads, 8 key heads, lengths over their logarithm): 64 sequences of up to 900
 // behind 2051, window 515: 25, 27, 25; window 1500: 30, 30, 44; up to 4000, window
 // 2500: 63, 63, 58; 128 of up to 900 behind 4000, window 4000: 61, 61, 167; 16 of 32
-// heads of up to 900 behind 2051, window 1500: 26, 26, 42.
+// heads of up to 900 behind 2051, window 1500: 26, 26, 42.  The same with all lengths at
+// their bound, where the sequences see less of the prefix than the rule takes them to: 33, 56,
+// 33; 60, 60, 52; 134, 133, 108; 106, 106, 166; 59, 59, 52; and with all of 1 but
+// one: 24, 27, 24; 27, 27, 42; 55, 55, 51; 57, 57, 163; 26, 26, 42.  (What it costs at
+// most, of 11 such batches: 128 of up to 300 behind 515, window 515, 61 and 42 at the
+// bound, 30 and 36 over their logarithm.)
 bool prefix_apart(const sdq_cache_s* c, const AttendParams& p, int q_heads) {
   const sdq_batch& b = p.b;
   if (b.prefix_len == 0) return false;

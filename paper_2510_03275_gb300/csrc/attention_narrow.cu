@@ -26,9 +26,10 @@ namespace {
 // window's, then of the sequence's own the same.  What the tokens of a unit see is then not nested, so a
 // value that is not finite and not every token's goes to those that see it by an
 // addition.  64 sequences of 1 to 16384 tokens, 64 heads, window 1024 and 4 first: 28.8
-// us (3.6 TB/s: the ends as above); 2 x 3 tokens, window 32768: 72 us, of which the
-// keys' reading 40: three groups of 8 rows keep a warp 4000 cycles on a tile.  (A third
-// stage in the scratch's place gains nothing.)
+// us (3.6 TB/s: the ends as above); 2 x 3 tokens, window 32768: 72 us.  Over windows of
+// 16352, 32768, 65600 and 131264 that is 33 us and the keys at 7.2 TB/s; as many keys
+// without a window 30 and the same rate, one token 13: 24 rows cost that much beside
+// their keys, a window 2 to 3.  (A third stage in the scratch's place gains nothing.)
 // P is rounded to bf16 for its product (relative 2^-8 at most per weight, as
 // the values themselves carry); sums, maxima and outputs are fp32.
 // 64 tokens of 64 heads (8 key heads of 128) on 1 to 4096 keys each: 43 us, 4.7

@@ -30,9 +30,13 @@ namespace {
 // An item's line is of 64-key pieces, two to a tile, so that what is left out,
 // first keys apart from the window, and the ends cost half a tile at most.
 // Prompts of 13757 tokens, 64 heads of 128, window 1024 and 4 first tokens, behind
-// 515: 421 us, 1070 TFLOP/s of what the rows see (58 % of the measured bf16 rate; the
-// tiles' edges that nobody sees are a fifth of the products, a tile takes 1.5 us
-// of 1.37 at that rate, an item's ends 4 us).
+// 515: 422 us, 1070 TFLOP/s of what the rows see (58 % of the measured bf16 rate).  An
+// item takes 18.5 us: 9.0 tiles, of which the rows see 7.75, are 12.3 of them at that
+// rate (1.7 for what nobody sees of the tiles at the edges), the rest are its ends and
+// the waits between products.
+// P is rounded to bf16 for its product with bf16 values, as in the other kernels (relative
+// 2^-8 at most per weight, as the values themselves carry); sums, maxima and outputs are
+// fp32, the output rounded once.
 // Registers: 384 threads hold 168 each at launch; the third warpgroup goes down to
 // 72, the first two up to 216 (2 x 216 + 72 = 3 x 168).
 
@@ -69,10 +73,9 @@ __device__ __forceinline__ bool partial(const AttendParams& p, const volatile It
   return c.k0 + kSub > keys || (c.k0 < w.low_rows - base && c.k0 + kSub > p.sinks - base);
 }
 
-// What depends on the part that a call's kernel takes: picked on the host.
-// (Indexed by the part in the kernel, the parameters would be copied to local
-// memory; read through an address of theirs instead, as __grid_constant__ allows,
-// an early build faulted.)
+// What depends on the part that a call's kernel takes: picked on the host, so that
+// the kernel indexes none of its parameters at run time (by value, as the others have
+// them, they would be copied to local memory for that).
 struct WindowPart {
   int prefix;    // all of the batch's rows against the prefix
   int splits;
